@@ -604,6 +604,62 @@ q8_status output_logits_f32(q8_ctx *ctx, const q8_readout_weights_f32 *ro, const
                             const float *s, const float *y_emb, const float *ctx_vec, int n_beam, int k, float *logits,
                             float *lse, float *topk_logp, int32_t *topk_idx, float *t_out);
 
+/* ---- 8-bit floating point with a scale per block (beside Section 3's integers with one scale per matrix) ----
+ * Rows of e4m3 codes (one sign, four exponent, three fraction bits, largest value 448, no infinities, 0x7f / 0xff NaN) in
+ * blocks of 128 columns, each with a power of two 2^(byte - 127): weights and vectors alike. */
+typedef struct {
+    const uint8_t *data;   /* [rows x ld] codes, pad bytes [cols, ld) zero; 16-byte aligned, ld % 16 == 0, ld <= 16384 */
+    const uint8_t *scale;  /* [rows x lds] bytes, one per block of 128 columns; 4-byte aligned, lds % 4 == 0, lds >= ceil(cols / 128);
+                              0 and 255 are no scales */
+    int rows, cols, ld, lds;
+} q8_mat_f8;
+
+/* X fp32 [rows x cols] (ld_in floats per row, any alignment) -> codes_out [rows x ld_out], pad bytes zero, and scale_out
+ * [rows x lds_out].  Per block: m = the largest finite magnitude, scale 2^e with the smallest e for which m <= 448 * 2^e, code =
+ * x 2^-e rounded to the nearest e4m3 value, ties to even (the product is exact); m < 2^-100: e = 0, codes 0.  A value that is not
+ * finite becomes NaN.  Pad bytes of a row's scales are set to 127.  rows <= 2^24.  Enqueued; nothing returns to the host. */
+q8_status q8_quantize_matrix_f8(q8_ctx *ctx, const float *X, int rows, int cols, int ld_in, uint8_t *codes_out, int ld_out,
+                                uint8_t *scale_out, int lds_out);
+
+/* Y[j][i] = sum_b 2^(..) sum_{k in block b} W[i][k] X[j][k] + bias[i] (bias [W->rows] may be NULL), the values' products and
+ * sums in fp32.  Y [n x ldy] fp32, elements past a vector's W->rows untouched.  A NaN stays with its row or vector.
+ * q8_gemm_f8: n vectors X [n x ldx] fp32 (16-byte aligned, ldx % 4 == 0), quantized in the call as above; workspace: the
+ * context's must have q8_gemm_f8_bytes(n, W->cols) bytes.  q8_gemm_codes_f8: X in codes already (n = X->rows, X->cols ==
+ * W->cols), no workspace; X and W may share memory, Y must overlap neither.  q8_gemm_f8's Y may overlap its X.
+ * 1 <= n <= 2^20, W->rows <= 2^24; any of the two may be large as long as the results number below 2^43. */
+size_t q8_gemm_f8_bytes(int n, int cols);
+q8_status q8_gemm_f8(q8_ctx *ctx, const q8_mat_f8 *W, const float *X, int n, int ldx, const float *bias, float *Y, int ldy);
+q8_status q8_gemm_codes_f8(q8_ctx *ctx, const q8_mat_f8 *W, const q8_mat_f8 *X, const float *bias, float *Y, int ldy);
+
+/* output_logits_q8 (without taps) with the vocabulary matrix in 8-bit floating point; the readout's first layer (ro, or t_in
+ * where ro == NULL) is the same.  logits [n x W_out->rows] may be NULL with k > 0.  k == 0: no selection (topk_logp, topk_idx and
+ * lse are not used), for callers that draw (q8_sample_logits); then W_out may have more than 65536 rows. */
+q8_status output_logits_f8(q8_ctx *ctx, const q8_readout_weights *ro, const q8_mat_f8 *W_out, const float *b_out, const float *s,
+                           const float *y_emb, const float *ctx_vec, const float *t_in, int n, int k, float *logits, float *lse,
+                           float *topk_logp, int32_t *topk_idx, float *t_out);
+
+/* ---- drawing a token (beside the search: one hypothesis per row, no beam) ----
+ * Row j of logits [n x ldl] (V floats) has its own temperature T, top-k, top-p and min-p (device arrays of n; NULL: T = 1,
+ * filters not in force).  The words are ordered by (logit descending, index ascending); a word whose logit is -inf or NaN is
+ * not among them (a mask).  With w_i = exp(-(max - l_i) / T):
+ *   top_k >= 1 keeps the first k words (<= 0: all); top_p < 1 the shortest prefix whose mass is at least top_p times the mass of
+ *   those (>= 1 or NaN: all); min_p > 0 the words with w_i >= min_p.  What all three keep, at least the first word, has mass Z.
+ *   tokens[j] = the first word whose cumulative mass exceeds u[j] Z (u in [0, 1); outside: the nearest of it).
+ * A temperature that is not positive takes the first word.  Masses are exact sums of weights in units of at most 2^-38 of the largest
+ * (2^-46 for V <= 65536), so that a word below half a unit is not drawn; the same inputs give the same tokens on every run.
+ * Several logits of +inf share the mass.  logp[j] (logp may be NULL) = logit - log sum exp(logits) at T = 1 without filters, as
+ * topk_logp.  A row without words: token -1, logp -inf.
+ * E_tgt [V x E] and y_emb [n x E] (both or neither): y_emb[j] = E_tgt[tokens[j]], zeros for token -1, the next step's input.
+ * n <= 65536, V <= 2^24.  Workspace: the context's must have q8_sample_bytes(n, V) bytes. */
+typedef struct {
+    const float *temperature;
+    const int32_t *top_k;
+    const float *top_p, *min_p;
+} q8_sampling;
+size_t q8_sample_bytes(int n, int V);
+q8_status q8_sample_logits(q8_ctx *ctx, const float *logits, int n, int V, int ldl, const q8_sampling *sampling, const float *u,
+                           int32_t *tokens, float *logp, const float *E_tgt, int E, float *y_emb);
+
 /* Measurement helpers (not operations of the paper).
  *
  * Between q8_profile_begin and q8_profile_end, up to max_samples launches of the

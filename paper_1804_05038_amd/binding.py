@@ -19,7 +19,8 @@ __all__ = ["Q8Error", "Context", "Mat", "Codes", "RowCodes", "GruWeights", "Cgru
            "cgru_decoder_step_f32", "output_logits_f32", "q8_translate_ensemble", "q8_translate_ensemble_bytes", "cgru_decoder_step_batch_q8", "q8_encode_batch", "q8_encode_batch_bytes", "q8_beam_init_batch",
            "q8_beam_update_batch", "q8_beam_result_batch", "q8_translate_batch", "q8_translate_batch_bytes",
            "KERNEL_CLASSES", "LIB_PATH", "source_ids",
-           "cgru_decoder_step_noalloc_q8", "q8_noalloc_setup", "q8_noalloc_scratch_bytes"]
+           "cgru_decoder_step_noalloc_q8", "q8_noalloc_setup", "q8_noalloc_scratch_bytes",
+           "MatF8", "q8_quantize_matrix_f8", "q8_gemm_f8", "q8_gemm_f8_bytes", "output_logits_f8", "q8_sample_logits", "q8_sample_bytes"]
 LIB_PATH = _LIB_PATH
 
 STATUS = {0: "Q8_OK", 1: "Q8_ERR_NULL", 2: "Q8_ERR_SHAPE", 3: "Q8_ERR_ALIGN", 4: "Q8_ERR_WORKSPACE", 5: "Q8_ERR_DEVICE"}
@@ -42,6 +43,14 @@ class _RowCodes(C.Structure):
 
 class _Codes(C.Structure):
     _fields_ = [("q", C.c_void_p), ("scale", C.c_void_p), ("ld", C.c_int), ("valid", C.c_int)]
+
+
+class _MatF8(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("scale", C.c_void_p), ("rows", C.c_int), ("cols", C.c_int), ("ld", C.c_int), ("lds", C.c_int)]
+
+
+class _Sampling(C.Structure):
+    _fields_ = [("temperature", C.c_void_p), ("top_k", C.c_void_p), ("top_p", C.c_void_p), ("min_p", C.c_void_p)]
 
 
 class _Taps(C.Structure):
@@ -154,6 +163,15 @@ def load_library():
         lib.q8_translate_batch_bytes.restype = C.c_size_t
         lib.q8_translate_batch_bytes.argtypes = [C.POINTER(_Model), ci, ci, ci, ci, ci]
         lib.q8_translate_batch.argtypes = [vp, C.POINTER(_Model), vp, ip, ci, ci, ci, ci, vp, ip, C.POINTER(C.c_float), ip]
+        lib.q8_quantize_matrix_f8.argtypes = [vp, vp, ci, ci, ci, vp, ci, vp, ci]
+        lib.q8_gemm_f8_bytes.restype = C.c_size_t
+        lib.q8_gemm_f8_bytes.argtypes = [ci, ci]
+        lib.q8_gemm_f8.argtypes = [vp, C.POINTER(_MatF8), vp, ci, ci, vp, vp, ci]
+        lib.q8_gemm_codes_f8.argtypes = [vp, C.POINTER(_MatF8), C.POINTER(_MatF8), vp, vp, ci]
+        lib.output_logits_f8.argtypes = [vp, C.POINTER(_Readout), C.POINTER(_MatF8), vp, vp, vp, vp, vp, ci, ci, vp, vp, vp, vp, vp]
+        lib.q8_sample_bytes.restype = C.c_size_t
+        lib.q8_sample_bytes.argtypes = [ci, ci]
+        lib.q8_sample_logits.argtypes = [vp, vp, ci, ci, ci, C.POINTER(_Sampling), vp, vp, vp, vp, ci, vp]
         lib.q8_profile_end.argtypes = [vp, C.POINTER(C.c_float), C.POINTER(C.c_int)]
         _lib = lib
     return _lib
@@ -929,4 +947,142 @@ def output_logits_beam_q8(ctx, ro, W_out, b_out, s, y_emb, ctx_vec, state, E_tgt
         r["keep"] = (ro, W_out, b_out, s, y_emb, ctx_vec, state, E_tgt, s_next, codes, E_codes)
         return _Bound(ctx, fn, args, r)
     ctx.check(fn(*args))
+    return r
+
+
+# ---- 8-bit floating point with a scale per block of 128 columns, and drawing of tokens ----
+
+def _rows(t, name, dtype=torch.float32, cols=None):
+    """Checks a [n, cols] device tensor whose rows are contiguous; returns its pitch."""
+    if t.dtype != dtype or t.dim() != 2 or not t.is_cuda:
+        raise ValueError("%s: expected a 2-d %s device tensor, got %s %s on %s" % (name, dtype, tuple(t.shape), t.dtype, t.device))
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError("%s: the elements of a row must be contiguous (strides %s)" % (name, t.stride()))
+    if cols is not None and t.shape[1] != cols:
+        raise ValueError("%s: expected %d columns, got %d" % (name, cols, t.shape[1]))
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+
+
+def _vector(t, name, n, dtype=torch.float32):
+    if t is not None and (t.dtype != dtype or tuple(t.shape) != (n,) or not t.is_cuda or not t.is_contiguous()):
+        raise ValueError("%s: expected %d contiguous %s on the device, got %s %s on %s" % (name, n, dtype, tuple(t.shape), t.dtype, t.device))
+
+
+class MatF8:
+    """q8_mat_f8: e4m3 codes [rows x ld] (uint8) and the bytes of their blocks' scales [rows x blocks] on the device."""
+
+    def __init__(self, data, scale_rows, cols):
+        _rows(data, "codes", torch.uint8)
+        _rows(scale_rows, "scales", torch.uint8)
+        self.data, self.cols = data, cols
+        self.rows, self.ld = data.shape
+        self.scale_rows = scale_rows                     # [rows x lds], the pitch a multiple of 4
+        self.scale = scale_rows[:, :(cols + 127) // 128]
+        if not (data.is_contiguous() and scale_rows.is_contiguous()) or scale_rows.shape[0] != self.rows:
+            raise ValueError("codes and scales must be contiguous, with as many rows each")
+        self.c = _MatF8(data.data_ptr(), scale_rows.data_ptr(), self.rows, cols, self.ld, scale_rows.shape[1])
+
+
+def q8_quantize_matrix_f8(ctx, W, ld_out=None, bind=False):
+    """Rows of W (weights or vectors) in e4m3 with a power of two per 128 columns: a MatF8."""
+    W = W if isinstance(W, torch.Tensor) and W.is_cuda and W.dtype == torch.float32 else ctx.f32(W)
+    ld_in = _rows(W, "W")
+    rows, cols = W.shape
+    ld_out = (cols + 15) // 16 * 16 if ld_out is None else ld_out
+    out = MatF8(ctx.empty(rows, ld_out, dtype=torch.uint8), ctx.empty(rows, ((cols + 127) // 128 + 3) // 4 * 4, dtype=torch.uint8), cols)
+    args = (ctx.handle, _ptr(W), rows, cols, ld_in, _ptr(out.data), ld_out, _ptr(out.scale_rows), out.scale_rows.shape[1])
+    if bind:
+        return _Bound(ctx, ctx.lib.q8_quantize_matrix_f8, args, {"W": out, "keep": W})
+    ctx.check(ctx.lib.q8_quantize_matrix_f8(*args))
+    return out
+
+
+def q8_gemm_f8_bytes(n, cols):
+    """Workspace bytes of a context for q8_gemm_f8."""
+    return load_library().q8_gemm_f8_bytes(n, cols)
+
+
+def q8_gemm_f8(ctx, W, X, bias=None, Y=None, bind=False):
+    """Y [n x W.rows] = X W^T + bias for vectors X: fp32 (quantized in the call) or a MatF8 (q8_gemm_codes_f8)."""
+    codes = isinstance(X, MatF8)
+    n = X.rows if codes else X.shape[0]
+    Y = ctx.empty(n, W.rows) if Y is None else Y
+    ldy = _rows(Y, "Y", cols=W.rows)
+    if Y.shape[0] != n:
+        raise ValueError("Y: expected %d rows, got %d" % (n, Y.shape[0]))
+    _vector(bias, "bias", W.rows)
+    if codes:
+        fn, args = ctx.lib.q8_gemm_codes_f8, (ctx.handle, C.byref(W.c), C.byref(X.c), _ptr(bias), _ptr(Y), ldy)
+    else:
+        ldx = _rows(X, "X", cols=W.cols)
+        fn, args = ctx.lib.q8_gemm_f8, (ctx.handle, C.byref(W.c), _ptr(X), n, ldx, _ptr(bias), _ptr(Y), ldy)
+    if bind:
+        return _Bound(ctx, fn, args, {"Y": Y, "keep": (W, X, bias)})
+    ctx.check(fn(*args))
+    return Y
+
+
+def output_logits_f8(ctx, ro, W_out, b_out, s=None, y_emb=None, ctx_vec=None, t_in=None, k=12, want_logits=True, logits=None, bind=False):
+    """output_logits_q8 with the vocabulary matrix a MatF8: dict(logits?, t, and for k > 0 lse, topk_logp, topk_idx)."""
+    n = (t_in if ro is None else s).shape[0]
+    V, R = W_out.rows, W_out.cols
+    if logits is None and (want_logits or k == 0):
+        logits = ctx.empty(n, V)
+    if logits is not None and (tuple(logits.shape) != (n, V) or not logits.is_contiguous()):
+        raise ValueError("logits: expected %d x %d, contiguous" % (n, V))
+    _vector(b_out, "b_out", V)
+    t = ctx.empty(n, R) if ro is not None else None
+    lse, lp, idx = (ctx.empty(n), ctx.empty(n, k), ctx.empty(n, k, dtype=torch.int32)) if k > 0 else (None, None, None)
+    args = (ctx.handle, C.byref(ro.c) if ro is not None else None, C.byref(W_out.c), _ptr(b_out), _ptr(s), _ptr(y_emb), _ptr(ctx_vec),
+            _ptr(t_in), n, k, _ptr(logits), _ptr(lse), _ptr(lp), _ptr(idx), _ptr(t))
+    r = {"logits": logits, "t": t, "lse": lse, "topk_logp": lp, "topk_idx": idx}
+    if bind:
+        r["keep"] = (ro, W_out, b_out, s, y_emb, ctx_vec, t_in)
+        return _Bound(ctx, ctx.lib.output_logits_f8, args, r)
+    ctx.check(ctx.lib.output_logits_f8(*args))
+    return r
+
+
+def q8_sample_bytes(n, V):
+    """Workspace bytes of a context for q8_sample_logits."""
+    return load_library().q8_sample_bytes(n, V)
+
+
+def q8_sample_logits(ctx, logits, u, temperature=None, top_k=None, top_p=None, min_p=None, E_tgt=None, y_emb=None, tokens=None,
+                     logp=None, bind=False):
+    """One token per row of logits [n x V] from the uniform numbers u [n]; temperature, top_p, min_p (fp32) and top_k (int32):
+    device tensors [n], one number for all rows, or None.  Returns dict(tokens, logp, y_emb); y_emb = E_tgt[tokens] where
+    E_tgt is given."""
+    ldl = _rows(logits, "logits")
+    n, V = logits.shape
+    _vector(u, "u", n)
+
+    def per_row(v, name, dtype):
+        if v is not None and not isinstance(v, torch.Tensor):
+            v = torch.full((n,), v, dtype=dtype, device=ctx.device)
+        _vector(v, name, n, dtype)
+        return v
+
+    p = [per_row(temperature, "temperature", torch.float32), per_row(top_k, "top_k", torch.int32), per_row(top_p, "top_p", torch.float32),
+         per_row(min_p, "min_p", torch.float32)]
+    sampling = _Sampling(*[t.data_ptr() if t is not None else None for t in p])
+    tokens = ctx.empty(n, dtype=torch.int32) if tokens is None else tokens
+    logp = ctx.empty(n) if logp is None else logp
+    _vector(tokens, "tokens", n, torch.int32)
+    _vector(logp, "logp", n)
+    E = 0
+    if E_tgt is not None:
+        E = E_tgt.shape[1]
+        y_emb = ctx.empty(n, E) if y_emb is None else y_emb
+        for t, name, shape in ((E_tgt, "E_tgt", (V, E)), (y_emb, "y_emb", (n, E))):
+            if t.dtype != torch.float32 or tuple(t.shape) != shape or not t.is_cuda or not t.is_contiguous():
+                raise ValueError("%s: expected a contiguous fp32 device tensor %s, got %s" % (name, shape, tuple(t.shape)))
+    elif y_emb is not None:
+        raise ValueError("y_emb without E_tgt")
+    args = (ctx.handle, _ptr(logits), n, V, ldl, C.byref(sampling), _ptr(u), _ptr(tokens), _ptr(logp), _ptr(E_tgt), E, _ptr(y_emb))
+    r = {"tokens": tokens, "logp": logp, "y_emb": y_emb}
+    if bind:
+        r["keep"] = (logits, u, p, sampling, E_tgt)
+        return _Bound(ctx, ctx.lib.q8_sample_logits, args, r)
+    ctx.check(ctx.lib.q8_sample_logits(*args))
     return r

@@ -153,6 +153,7 @@ size_t q8_workspace_bytes(int max_n, int max_l, int max_rows, int max_ld)
     const size_t nv = (size_t)(max_n > max_l ? max_n : max_l);
     size_t b = Q8_WS_HEADER;
     b += up256(nv * (size_t)max_ld) + up256(nv * 4);              // quantized vectors + scales (MFMA path)
+    b += up256(nv * (size_t)(max_ld / 128 + 4));                  // a scale per block of 128 columns (8-bit floating point)
     b += 2 * up256((size_t)max_l * max_rows * 4);                 // encoder input pre-activations, both directions
     b += 8 * up256((size_t)max_n * max_rows * 4);                 // per-hypothesis vectors of a decoder step
     b += up256((size_t)max_n * max_l * 4);                        // attention energies
@@ -1769,6 +1770,169 @@ q8_status q8_translate_batch(q8_ctx *ctx, const q8_model *m, const int32_t *src_
     if (!st) st = q8_beam_result_batch(ctx, states, n_sent, max_steps, tokens_host, len_host, score_host, steps_host);
     ctx->ws_reserved_top = 0;
     return st;
+}
+
+// ------------------------------------------------- 8-bit floating point with a scale per block ----
+
+namespace {
+const int kF8Block = 128, kF8MaxRows = 1 << 24, kF8MaxN = 1 << 20, kSampleMaxN = 65536;
+
+inline int f8_blocks(int cols) { return (cols + kF8Block - 1) / kF8Block; }
+inline int f8_pitch(int cols) { return (cols + 15) & ~15; }                  // of the vectors that a call quantizes itself
+inline int f8_scale_pitch(int cols) { return (f8_blocks(cols) + 3) & ~3; }
+
+q8_status check_mat_f8(q8_ctx *ctx, const q8_mat_f8 *W, int max_rows, const char *name)
+{
+    if (!W || !W->data || !W->scale) return q8_fail(ctx, Q8_ERR_NULL, "%s: NULL matrix", name);
+    if (W->rows <= 0 || W->rows > max_rows || W->cols <= 0 || W->ld < W->cols || W->ld > kMaxLd || W->lds < f8_blocks(W->cols) || W->lds > kMaxLd)
+        return q8_fail(ctx, Q8_ERR_SHAPE, "%s: bad shape %d x %d (ld %d, lds %d)", name, W->rows, W->cols, W->ld, W->lds);
+    if (!aligned16(W->data) || W->ld % 16 != 0 || (uintptr_t)W->scale % 4 != 0 || W->lds % 4 != 0)
+        return q8_fail(ctx, Q8_ERR_ALIGN, "%s: codes need a 16-byte aligned base and ld %% 16 == 0, scales 4 bytes and lds %% 4 == 0", name);
+    return Q8_OK;
+}
+
+q8_status check_result_f8(q8_ctx *ctx, const float *bias, const float *Y, int n, int rows, int ldy)
+{
+    if (!Y) return q8_fail(ctx, Q8_ERR_NULL, "Y: NULL");
+    if (n > 1 && ldy < rows) return q8_fail(ctx, Q8_ERR_SHAPE, "ldy %d < rows %d", ldy, rows);
+    if ((uintptr_t)Y % 4 != 0 || (uintptr_t)bias % 4 != 0) return q8_fail(ctx, Q8_ERR_ALIGN, "Y, bias: not aligned to 4 bytes");
+    if ((size_t)n * (size_t)rows >= (size_t)1 << 43) return q8_fail(ctx, Q8_ERR_SHAPE, "%d x %d results: 2^43 or more", n, rows);
+    return Q8_OK;
+}
+}  // namespace
+
+q8_status q8_quantize_matrix_f8(q8_ctx *ctx, const float *X, int rows, int cols, int ld_in, uint8_t *codes_out, int ld_out,
+                                uint8_t *scale_out, int lds_out)
+{
+    if (!ctx) return Q8_ERR_NULL;
+    if (!X) return q8_fail(ctx, Q8_ERR_NULL, "q8_quantize_matrix_f8: NULL argument");
+    const q8_mat_f8 out = {codes_out, scale_out, rows, cols, ld_out, lds_out};
+    TRY(check_mat_f8(ctx, &out, kF8MaxRows, "q8_quantize_matrix_f8"));
+    if (rows > 1 && ld_in < cols) return q8_fail(ctx, Q8_ERR_SHAPE, "q8_quantize_matrix_f8: ld_in %d < cols %d", ld_in, cols);
+    if ((uintptr_t)X % 4 != 0) return q8_fail(ctx, Q8_ERR_ALIGN, "q8_quantize_matrix_f8: X is not aligned to 4 bytes");
+    return q8i_quantize_f8(ctx, X, rows, cols, ld_in, codes_out, ld_out, scale_out, lds_out);
+}
+
+size_t q8_gemm_f8_bytes(int n, int cols)
+{
+    if (n <= 0 || n > kF8MaxN || cols <= 0 || cols > kMaxLd) return Q8_WS_HEADER;
+    return Q8_WS_HEADER + up256((size_t)n * f8_pitch(cols)) + up256((size_t)n * f8_scale_pitch(cols));
+}
+
+q8_status q8_gemm_codes_f8(q8_ctx *ctx, const q8_mat_f8 *W, const q8_mat_f8 *X, const float *bias, float *Y, int ldy)
+{
+    if (!ctx) return Q8_ERR_NULL;
+    TRY(check_mat_f8(ctx, W, kF8MaxRows, "W"));
+    TRY(check_mat_f8(ctx, X, kF8MaxN, "X"));
+    if (X->cols != W->cols) return q8_fail(ctx, Q8_ERR_SHAPE, "X has %d columns, W %d", X->cols, W->cols);
+    TRY(check_result_f8(ctx, bias, Y, X->rows, W->rows, ldy));
+    return q8i_gemm_f8(ctx, W, X, bias, Y, ldy);
+}
+
+q8_status q8_gemm_f8(q8_ctx *ctx, const q8_mat_f8 *W, const float *X, int n, int ldx, const float *bias, float *Y, int ldy)
+{
+    if (!ctx) return Q8_ERR_NULL;
+    TRY(check_mat_f8(ctx, W, kF8MaxRows, "W"));
+    if (n <= 0 || n > kF8MaxN) return q8_fail(ctx, Q8_ERR_SHAPE, "n = %d outside [1, %d]", n, kF8MaxN);
+    TRY(check_vecs(ctx, X, n == 1 ? W->cols + ((4 - W->cols % 4) % 4) : ldx, W->cols, "X"));
+    TRY(check_result_f8(ctx, bias, Y, n, W->rows, ldy));
+    Carver cv(ctx);
+    q8_mat_f8 xq = {nullptr, nullptr, n, W->cols, f8_pitch(W->cols), f8_scale_pitch(W->cols)};
+    uint8_t *codes = cv.take<uint8_t>((size_t)n * xq.ld), *scale = cv.take<uint8_t>((size_t)n * xq.lds);
+    if (!cv.ok) return q8_fail(ctx, Q8_ERR_WORKSPACE, "q8_gemm_f8: workspace too small");
+    TRY(q8i_quantize_f8(ctx, X, n, W->cols, ldx, codes, xq.ld, scale, xq.lds));
+    xq.data = codes;
+    xq.scale = scale;
+    return q8i_gemm_f8(ctx, W, &xq, bias, Y, ldy);
+}
+
+q8_status output_logits_f8(q8_ctx *ctx, const q8_readout_weights *ro, const q8_mat_f8 *W_out, const float *b_out, const float *s,
+                           const float *y_emb, const float *ctx_vec, const float *t_in, int n, int k, float *logits, float *lse,
+                           float *topk_logp, int32_t *topk_idx, float *t_out)
+{
+    if (!ctx) return Q8_ERR_NULL;
+    TRY(check_mat_f8(ctx, W_out, kF8MaxRows, "W_out"));
+    const int R = W_out->cols, V = W_out->rows;
+    if (n <= 0 || n > kMaxMfmaN) return q8_fail(ctx, Q8_ERR_SHAPE, "n = %d outside [1, %d]", n, kMaxMfmaN);
+    if (k < 0 || k > kMaxK || k > V) return q8_fail(ctx, Q8_ERR_SHAPE, "k = %d outside [0, min(%d, rows)]", k, kMaxK);
+    if (k > 0 && V > q8i_out_max_rows()) return q8_fail(ctx, Q8_ERR_SHAPE, "W_out: more than %d rows", q8i_out_max_rows());
+    if (R % 4) return q8_fail(ctx, Q8_ERR_ALIGN, "R must be a multiple of 4");
+    if (k > 0 ? !topk_logp || !topk_idx : !logits) return q8_fail(ctx, Q8_ERR_NULL, k > 0 ? "top-k outputs: NULL" : "logits: NULL");
+    if ((uintptr_t)logits % 4 != 0 || (uintptr_t)b_out % 4 != 0) return q8_fail(ctx, Q8_ERR_ALIGN, "logits, b_out: not aligned to 4 bytes");
+    if (t_out && !aligned16(t_out)) return q8_fail(ctx, Q8_ERR_ALIGN, "t_out needs 16-byte alignment");
+    Carver cv(ctx);
+    const float *T = t_in;
+    float *t = nullptr, *part[3] = {nullptr, nullptr, nullptr};
+    q8i_quant_job qj[3];
+    q8i_gemm_job gj[3];
+    if (ro) {
+        const q8_mat *M[3] = {&ro->W_s, &ro->W_y, &ro->W_c};
+        const float *X[3] = {s, y_emb, ctx_vec};
+        for (int u = 0; u < 3; ++u) TRY(check_mat(ctx, M[u], "readout matrix"));
+        for (int u = 0; u < 3; ++u) {
+            if (M[u]->rows != R) return q8_fail(ctx, Q8_ERR_SHAPE, "readout matrices must have %d rows", R);
+            if (M[u]->cols % 4) return q8_fail(ctx, Q8_ERR_ALIGN, "H, E, C must be multiples of 4");
+            TRY(check_vecs(ctx, X[u], M[u]->cols, M[u]->cols, "s, y_emb, ctx"));
+        }
+        if (n <= kMaxNarrow && (size_t)n * (ro->W_s.ld + ro->W_y.ld + ro->W_c.ld) > 65536)
+            return q8_fail(ctx, Q8_ERR_SHAPE, "n * (H + E + C) exceeds 65536");
+        t = t_out ? t_out : cv.take<float>((size_t)n * R);
+        if (n > kMaxNarrow)
+            for (int u = 0; u < 3; ++u) {
+                int8_t *xq = cv.take<int8_t>((size_t)n * M[u]->ld);
+                float *xs = cv.take<float>(n);
+                part[u] = cv.take<float>((size_t)n * R);
+                qj[u] = {X[u], M[u]->cols, M[u]->cols, M[u]->ld, xq, xs, nullptr};
+                gj[u] = {M[u], xq, xs, nullptr, part[u], R, nullptr, nullptr, nullptr, 0};
+            }
+        T = t;
+    } else {
+        TRY(check_vecs(ctx, t_in, R, R, "t_in"));
+    }
+    q8_mat_f8 tq = {nullptr, nullptr, n, R, f8_pitch(R), f8_scale_pitch(R)};
+    uint8_t *codes = cv.take<uint8_t>((size_t)n * tq.ld), *scale = cv.take<uint8_t>((size_t)n * tq.lds);
+    const size_t tiles = k > 0 ? (size_t)q8i_out_tiles(V) * n : 0;
+    float *pm = k > 0 ? cv.take<float>(tiles) : nullptr;
+    double *ps = k > 0 ? cv.take<double>(tiles) : nullptr;
+    float *lg = logits ? logits : cv.take<float>((size_t)n * V);
+    if (!cv.ok) return q8_fail(ctx, Q8_ERR_WORKSPACE, "output_logits_f8: workspace too small");
+    if (ro && n <= kMaxNarrow) {
+        TRY(q8i_readout(ctx, ro, s, y_emb, ctx_vec, n, t, nullptr));
+    } else if (ro) {
+        TRY(q8i_quantize_jobs(ctx, qj, 3, n));
+        if (q8i_gemm_ksplit3_ok(gj, n)) TRY(q8i_gemm_ksplit3(ctx, gj, n));
+        else TRY(q8i_gemm_jobs(ctx, gj, 3, n));
+        TRY(q8i_readout_combine(ctx, part[0], part[1], part[2], ro->b_t, R, n, t, 0, nullptr, nullptr, nullptr));
+    }
+    TRY(q8i_quantize_f8(ctx, T, n, R, R, codes, tq.ld, scale, tq.lds));
+    tq.data = codes;
+    tq.scale = scale;
+    TRY(q8i_gemm_f8(ctx, W_out, &tq, b_out, lg, V));
+    if (k == 0) return Q8_OK;
+    TRY(q8i_tile_stats(ctx, lg, n, V, pm, ps));
+    return q8i_select_logits(ctx, pm, ps, lg, V, n, k, lse, topk_logp, topk_idx);
+}
+
+size_t q8_sample_bytes(int n, int V)
+{
+    (void)n;
+    (void)V;
+    return Q8_WS_HEADER;
+}
+
+q8_status q8_sample_logits(q8_ctx *ctx, const float *logits, int n, int V, int ldl, const q8_sampling *sampling, const float *u,
+                           int32_t *tokens, float *logp, const float *E_tgt, int E, float *y_emb)
+{
+    if (!ctx) return Q8_ERR_NULL;
+    if (!logits || !u || !tokens) return q8_fail(ctx, Q8_ERR_NULL, "q8_sample_logits: NULL argument");
+    if ((E_tgt != nullptr) != (y_emb != nullptr)) return q8_fail(ctx, Q8_ERR_NULL, "q8_sample_logits: E_tgt and y_emb go together");
+    if (n <= 0 || n > kSampleMaxN || V <= 0 || V > kF8MaxRows || (n > 1 && ldl < V) || (E_tgt && E <= 0))
+        return q8_fail(ctx, Q8_ERR_SHAPE, "q8_sample_logits: bad shape %d x %d (ldl %d, E %d)", n, V, ldl, E);
+    const void *p4[] = {logits, u, tokens, logp, E_tgt, y_emb, sampling ? sampling->temperature : nullptr, sampling ? sampling->top_k : nullptr,
+                        sampling ? sampling->top_p : nullptr, sampling ? sampling->min_p : nullptr};
+    for (const void *p : p4)
+        if ((uintptr_t)p % 4 != 0) return q8_fail(ctx, Q8_ERR_ALIGN, "q8_sample_logits: a buffer is not aligned to 4 bytes");
+    return q8i_sample(ctx, logits, n, V, ldl, sampling, u, tokens, logp, E_tgt, E, y_emb);
 }
 
 }  // extern "C"

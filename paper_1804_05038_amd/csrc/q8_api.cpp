@@ -157,6 +157,7 @@ size_t q8_workspace_bytes(int max_n, int max_l, int max_rows, int max_ld)
     b += 2 * up256((size_t)max_l * max_rows * 4);                 // encoder input pre-activations, both directions
     b += 8 * up256((size_t)max_n * max_rows * 4);                 // per-hypothesis vectors of a decoder step
     b += up256((size_t)max_n * max_l * 4);                        // attention energies
+    b += up256(q8i_sample_bytes(max_n, max_rows));
     const size_t ngrp = (size_t)q8i_out_tiles(max_rows);
     b += up256(ngrp * max_n * 4) + up256(ngrp * max_n * 8);
     return b + 65536;
@@ -1915,9 +1916,8 @@ q8_status output_logits_f8(q8_ctx *ctx, const q8_readout_weights *ro, const q8_m
 
 size_t q8_sample_bytes(int n, int V)
 {
-    (void)n;
-    (void)V;
-    return Q8_WS_HEADER;
+    if (n <= 0 || n > kSampleMaxN || V <= 0 || V > kF8MaxRows) return Q8_WS_HEADER;
+    return Q8_WS_HEADER + up256(q8i_sample_bytes(n, V));
 }
 
 q8_status q8_sample_logits(q8_ctx *ctx, const float *logits, int n, int V, int ldl, const q8_sampling *sampling, const float *u,
@@ -1932,7 +1932,10 @@ q8_status q8_sample_logits(q8_ctx *ctx, const float *logits, int n, int V, int l
                         sampling ? sampling->top_p : nullptr, sampling ? sampling->min_p : nullptr};
     for (const void *p : p4)
         if ((uintptr_t)p % 4 != 0) return q8_fail(ctx, Q8_ERR_ALIGN, "q8_sample_logits: a buffer is not aligned to 4 bytes");
-    return q8i_sample(ctx, logits, n, V, ldl, sampling, u, tokens, logp, E_tgt, E, y_emb);
+    Carver cv(ctx);
+    char *state = cv.take<char>(q8i_sample_bytes(n, V));
+    if (!cv.ok) return q8_fail(ctx, Q8_ERR_WORKSPACE, "q8_sample_logits: workspace too small");
+    return q8i_sample(ctx, logits, n, V, ldl, sampling, u, tokens, logp, E_tgt, E, y_emb, state);
 }
 
 }  // extern "C"

@@ -348,7 +348,8 @@ q8_status q8i_quantize_f8(q8_ctx *ctx, const float *X, int rows, int cols, int l
 q8_status q8i_gemm_f8(q8_ctx *ctx, const q8_mat_f8 *W, const q8_mat_f8 *X, const float *bias, float *Y, int ldy);
 q8_status q8i_tile_stats(q8_ctx *ctx, const float *logits, int n, int V, float *part_max, double *part_sum);
 q8_status q8i_sample(q8_ctx *ctx, const float *logits, int n, int V, int ldl, const q8_sampling *s, const float *u, int32_t *tokens, float *logp,
-                     const float *E_tgt, int E, float *y_emb);
+                     const float *E_tgt, int E, float *y_emb, void *state);
+size_t q8i_sample_bytes(int n, int V);
 size_t q8i_beam_state_bytes(int max_steps);
 q8_status q8i_gather_rows(q8_ctx *ctx, const float *table, const int *idx, int n, int dim, int V, float *out);
 q8_status q8i_beam_init(q8_ctx *ctx, void *state, int beam, int max_steps, const float *s0, const float *E_tgt, int E,

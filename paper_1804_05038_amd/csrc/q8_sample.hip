@@ -3,14 +3,23 @@
 // With m the largest logit of a row, word i has the weight w_i = exp(-(m - l_i) / T).  The words are ordered by (logit
 // descending, index ascending); each filter keeps a prefix of that order: the first k words; the shortest prefix with at
 // least p of the mass of those; the words with w_i >= min_p.  With Z the mass of the shortest of these prefixes the drawn
-// token is the first word of the order whose cumulative mass exceeds u Z.  All three borders are found alike: "the first word
-// at which (count, mass) up to it satisfies a condition that stays true further down".
+// token is the first word of the order whose cumulative mass exceeds u Z.  All borders are found alike: "the first word at
+// which (count, mass) up to it satisfies a condition that stays true further down".
 //
 // Weights are whole numbers, rint(w_i 2^S): their sums are exact whatever their order, so a token does not depend on which
 // thread adds what, and the borders between tokens lie where sums in 64-bit floating point put them to about 1e-12.
 #include "q8_internal.h"
 
 #include <math.h>
+
+typedef unsigned long long u64;
+
+#define SMP_BINS 2048                        // of 1/32 octave of weight each; beyond the last one every weight rounds to zero
+#define SMP_LOG2E32 46.166241308446828384    // 32 log2(e)
+#define SMP_SMALL 8192                       // vocabularies of at most so many words: a block per row
+#define SMP_PARTS 128                        // blocks of a row
+#define SMP_ROWS 1024                        // rows of a launch
+#define SMP_LIST 1536                        // words of a row that may lie where its borders do
 
 struct SampleArgs {
     const float *logits;
@@ -24,13 +33,12 @@ struct SampleArgs {
     float *y_emb;
     int E;
     int shift;                              // S
+    // rows over several blocks
+    struct SmpRowState *state;              // [rows of the launch]
+    int parts, part_pieces, row0;           // blocks of a row, 16-byte pieces of each, first row of the launch
 };
 
-typedef unsigned long long u64;
-
-#define SMP_BINS 2048                        // of 1/32 octave of weight each; beyond the last one every weight rounds to zero
-#define SMP_LIST 1024                        // words of one bin that are ranked in LDS
-#define SMP_LOG2E32 46.166241308446828384    // 32 log2(e)
+// ------------------------------------------------------------------------------- weights ----
 
 // The distance below the largest logit, in double: two floats' difference can exceed the range of a float.
 __device__ __forceinline__ double smp_gap(float m, float v) { return (double)m - (double)v; }
@@ -46,61 +54,78 @@ __device__ __forceinline__ SmpPlace smp_place(double gap, double c)
     return {(unsigned)__double2hiint(t) - 0x41300000u, (unsigned)__double2loint(t)};
 }
 
-// 2^(S - x / 32): a table over x mod 32 and a polynomial over the fraction, exp(-f 2^-32 ln 2 / 32), which interpolates at the
-// Chebyshev points with the constant term held at 1 (within 2.9e-16; the fraction's 2^-33 is 2^-38.5 of the weight).
+__device__ const double smp_pow[32] = {         // 2^(-j / 32)
+    0x1.0000000000000p+0, 0x1.f50765b6e4540p-1, 0x1.ea4afa2a490dap-1, 0x1.dfc97337b9b5fp-1,
+    0x1.d5818dcfba487p-1, 0x1.cb720dcef9069p-1, 0x1.c199bdd85529cp-1, 0x1.b7f76f2fb5e47p-1,
+    0x1.ae89f995ad3adp-1, 0x1.a5503b23e255dp-1, 0x1.9c49182a3f090p-1, 0x1.93737b0cdc5e5p-1,
+    0x1.8ace5422aa0dbp-1, 0x1.82589994cce13p-1, 0x1.7a11473eb0187p-1, 0x1.71f75e8ec5f74p-1,
+    0x1.6a09e667f3bcdp-1, 0x1.6247eb03a5585p-1, 0x1.5ab07dd485429p-1, 0x1.5342b569d4f82p-1,
+    0x1.4bfdad5362a27p-1, 0x1.44e086061892dp-1, 0x1.3dea64c123422p-1, 0x1.371a7373aa9cbp-1,
+    0x1.306fe0a31b715p-1, 0x1.29e9df51fdee1p-1, 0x1.2387a6e756238p-1, 0x1.1d4873168b9aap-1,
+    0x1.172b83c7d517bp-1, 0x1.11301d0125b51p-1, 0x1.0b5586cf9890fp-1, 0x1.059b0d3158574p-1};
+
+// 2^(S - x / 32): a table over x mod 32 times a polynomial over the fraction, exp(-f 2^-32 ln 2 / 32), which interpolates at the
+// Chebyshev points with the constant term held at 1 (within 3.2e-13; rounding the fraction to 2^-33 is 1.7e-12).  The whole
+// octaves leave the exponent.
 __device__ __forceinline__ double smp_weight(SmpPlace p, const double *s_pow)
 {
     const double f = (double)p.frac;
-    double e = -0x1.5a647398608b2p-195;
-    e = fma(e, f, 0x1.3b27f902762c7p-155);
-    e = fma(e, f, -0x1.c6b08b7b3d711p-116);
-    e = fma(e, f, 0x1.ebfbdff7af203p-77);
-    e = fma(e, f, -0x1.62e42fefa399fp-38);
+    double e = 0x1.38731c1a7139ap-155;
+    e = fma(e, f, -0x1.c6ad294417fcap-116);
+    e = fma(e, f, 0x1.ebfbde9d1da6cp-77);
+    e = fma(e, f, -0x1.62e42fef8deebp-38);
     e = fma(e, f, 1.0);
-    return ldexp(e * s_pow[p.bin & 31u], -(int)(p.bin >> 5));
+    e *= s_pow[p.bin & 31u];
+    return __hiloint2double(__double2hiint(e) - (int)((p.bin >> 5) << 20), __double2loint(e));
 }
 // ... to the nearest whole number (below 2^47).
 __device__ __forceinline__ u64 smp_whole(double w) { return (u64)__double_as_longlong(w + 0x1p52) & 0xfffffffffffffull; }
 
-// A row of logits as a block goes through it: thread t has the pieces of four words t, t + BLOCK, ... counted from the 16-byte
-// boundary at or below the row's begin.  Words outside the row and words that cannot be drawn (NaN) appear as -inf.
-// NE > 0: NE words a thread, read once and kept in registers; NE == 0: read again on every pass.
+// exp(-gap) for the sum at T = 1: the hardware's exponential of the fraction of an octave (2^-23 off at most).
+__device__ __forceinline__ double smp_exp1(double gap)
+{
+    const double x = fmin(fma(gap, SMP_LOG2E32 / 32.0, 0x1p20), 0x1p20 + 1024.0);
+    const float f = (float)(unsigned)__double2loint(x) * -0x1p-32f;
+    return (double)ldexpf(__builtin_amdgcn_exp2f(f), -(int)((unsigned)__double2hiint(x) - 0x41300000u));
+}
+
+// ---------------------------------------------------------------------------------- rows ----
+
+// A row of logits, or a part of one, as a block goes through it: thread t has the pieces of four words t, t + BLOCK, ... of the
+// part.  Words past the row and words that cannot be drawn (NaN) appear as -inf.  NE > 0: NE words a thread, read once and kept in
+// registers; NE == 0: read again on every pass.
 template <int NE, int BLOCK> struct SmpRow {
-    const float *l;
-    int V, lead;                            // words before the row in its first piece
+    __amdgpu_buffer_rsrc_t rows;
+    int V, first, end;                      // pieces of the part
     bool top_inf;                           // the largest logit is +inf: words of +inf count as 0, others as -inf
     float v[NE ? NE : 1];
 
-    __device__ __forceinline__ float4 piece(int c) const
+    __device__ __forceinline__ v4u load(int c) const { return __builtin_amdgcn_raw_buffer_load_b128(rows, c * 16, 0, 0); }
+    __device__ __forceinline__ void clean(v4u q, int c, float (&r)[4]) const
     {
-        const int i = 4 * c - lead;
-        float4 r;
-        if (i >= 0 && i + 3 < V) {
-            r = *(const float4 *)(l + i);
-        } else {
-            r.x = i >= 0 && i < V ? l[i] : -INFINITY;
-            r.y = i >= -1 && i + 1 < V ? l[i + 1] : -INFINITY;
-            r.z = i >= -2 && i + 2 < V ? l[i + 2] : -INFINITY;
-            r.w = i >= -3 && i + 3 < V ? l[i + 3] : -INFINITY;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            r[t] = 4 * c + t < V && c < end ? fmaxf(__uint_as_float(q[t]), -INFINITY) : -INFINITY;
+            if (top_inf) r[t] = r[t] == INFINITY ? 0.0f : -INFINITY;
         }
-        r.x = fmaxf(r.x, -INFINITY); r.y = fmaxf(r.y, -INFINITY); r.z = fmaxf(r.z, -INFINITY); r.w = fmaxf(r.w, -INFINITY);
-        if (top_inf) {
-            r.x = r.x == INFINITY ? 0.0f : -INFINITY; r.y = r.y == INFINITY ? 0.0f : -INFINITY;
-            r.z = r.z == INFINITY ? 0.0f : -INFINITY; r.w = r.w == INFINITY ? 0.0f : -INFINITY;
-        }
-        return r;
     }
-    __device__ __forceinline__ void open(const float *row, int V_)
+    __device__ __forceinline__ void open(const float *row, int V_, int first_, int pieces_)
     {
-        l = row;
+        rows = q8_rsrc(row, (size_t)V_ * 4);
         V = V_;
-        lead = (int)(((uintptr_t)row & 15) >> 2);
         top_inf = false;
+        first = first_;
+        end = min(first_ + pieces_, (V_ + 3) / 4);
         if constexpr (NE > 0) {
+            v4u q[NE / 4];
+#pragma unroll
+            for (int j = 0; j < NE / 4; ++j) q[j] = load(first + j * BLOCK + (int)threadIdx.x);      // (past the row: zeros, no access)
 #pragma unroll
             for (int j = 0; j < NE / 4; ++j) {
-                const float4 r = piece(j * BLOCK + (int)threadIdx.x);
-                v[4 * j] = r.x; v[4 * j + 1] = r.y; v[4 * j + 2] = r.z; v[4 * j + 3] = r.w;
+                float r[4];
+                clean(q[j], first + j * BLOCK + (int)threadIdx.x, r);
+#pragma unroll
+                for (int t = 0; t < 4; ++t) v[4 * j + t] = r[t];
             }
         }
     }
@@ -112,308 +137,828 @@ template <int NE, int BLOCK> struct SmpRow {
             for (int e = 0; e < NE; ++e) v[e] = v[e] == INFINITY ? 0.0f : -INFINITY;
         }
     }
-    // f(four logits, index of the first), for every piece.  The logits are passed through an empty statement: what a pass computes
-    // from them is not kept for the next one, for which there are no registers.
+    // f(four logits, index of the first), for every piece.  In registers, the logits and indexes pass through empty statements: what
+    // a pass computes from them is not kept for the next one, for which there are no registers.
     template <class F> __device__ __forceinline__ void pieces(F f) const
     {
         if constexpr (NE > 0) {
-            int first = 4 * (int)threadIdx.x - lead;
-            asm volatile("" : "+v"(first));
+            int at = 4 * (first + (int)threadIdx.x);
+            asm volatile("" : "+v"(at));
+            const int mine = (end - first + BLOCK - 1) / BLOCK;
 #pragma unroll
             for (int j = 0; j < NE / 4; ++j) {
-                float r[4] = {v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]};
-                asm volatile("" : "+v"(r[0]), "+v"(r[1]), "+v"(r[2]), "+v"(r[3]));
-                f(r, first + 4 * j * BLOCK);
+                if (j < mine) {
+                    float r[4] = {v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]};
+                    asm volatile("" : "+v"(r[0]), "+v"(r[1]), "+v"(r[2]), "+v"(r[3]));
+                    f(r, at + 4 * j * BLOCK);
+                }
                 __builtin_amdgcn_sched_barrier(0);
             }
         } else {
-            const int total = (V + lead + 3) / 4;
-            for (int c = threadIdx.x; c < total; c += BLOCK) {
-                const float4 q = piece(c);
-                const float r[4] = {q.x, q.y, q.z, q.w};
-                f(r, 4 * c - lead);
+            for (int c = first + (int)threadIdx.x; c < end; c += 4 * BLOCK) {
+                v4u q[4];
+#pragma unroll
+                for (int t = 0; t < 4; ++t) q[t] = load(c + t * BLOCK);
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    float r[4];
+                    clean(q[t], c + t * BLOCK, r);
+                    f(r, 4 * (c + t * BLOCK));
+                }
             }
         }
     }
-    template <class F> __device__ __forceinline__ void each(F f) const
+    __device__ __forceinline__ float largest() const           // of the thread's words
     {
-        pieces([&](const float (&r)[4], int i) {
+        float m = -INFINITY;
+        if constexpr (NE > 0) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) f(r[e], i + e);
+            for (int e = 0; e < NE; ++e) m = fmaxf(m, v[e]);
+        } else {
+            pieces([&](const float (&r)[4], int) { m = fmaxf(fmaxf(fmaxf(m, r[0]), fmaxf(r[1], r[2])), r[3]); });
+        }
+        return m;
+    }
+    // The same words, read from memory: for passes that few rows take, so that their code is not there once per piece.
+    __device__ __forceinline__ SmpRow<0, BLOCK> stored() const
+    {
+        SmpRow<0, BLOCK> r;
+        r.rows = rows; r.V = V; r.first = first; r.end = end; r.top_inf = top_inf;
+        return r;
+    }
+    // f(key) for the words with near(logit) (cheap) and take(logit).
+    template <class N, class T, class F> __device__ __forceinline__ void some(N near, T take, F f) const
+    {
+        pieces([&](const float (&v)[4], int i) {
+            unsigned hit = 0;
+#pragma unroll
+            for (int t = 0; t < 4; ++t) hit |= near(v[t]) ? 1u << t : 0u;
+            while (hit) {
+                const int t = __ffs(hit) - 1;
+                hit &= hit - 1;
+                const float x = t == 0 ? v[0] : t == 1 ? v[1] : t == 2 ? v[2] : v[3];
+                if (take(x)) f(topk_key(x, i + t));
+            }
         });
     }
 };
 
-struct SmpShared {
-    u64 mass[SMP_BINS];                     // per bin, then up to and including it
-    unsigned count[SMP_BINS];
-    struct { u64 key, mass; } list[SMP_LIST];
+// Where a bin is in LDS: one place in nine is left out, so that threads that own eight bins each meet on few banks.
+__device__ __forceinline__ unsigned smp_at(unsigned b) { return b + (b >> 3); }
+
+template <int BLOCK> struct SmpShared {
+    u64 mass[SMP_BINS + SMP_BINS / 8];      // per bin (smp_at), then up to and including it
+    unsigned count[SMP_BINS + SMP_BINS / 8];
+    u64 list[BLOCK];                        // keys of words that are ranked
     double pow[32];                         // 2^(S - j / 32)
     u64 red_u[16];
     double red_d[16];
+    float red_f[16], red_g[16];
     unsigned red_c[16];
-    u64 above, hit_key, hit_mass;
-    unsigned listed, bin;
+    u64 sum, above, hit_key, hit_mass, k_mass;
+    unsigned listed, below, known_c, bytes[256];
 };
 
-// One block per row.  Passes over the row: the largest logit; weights, summed into bins of 1/32 octave (LDS); for each border
-// the words of the one bin that it falls into, ranked among themselves (by a histogram of their keys' bytes where there are
-// more than SMP_LIST of them).
-template <int NE, int BLOCK>
-__global__ __launch_bounds__(BLOCK) void sample_row_kernel(SampleArgs a)
-{
-    extern __shared__ __align__(16) char smem[];
-    SmpShared &s = *(SmpShared *)smem;
-    const int j = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    constexpr int WAVES = BLOCK / 64, PER = SMP_BINS / BLOCK;
-    SmpRow<NE, BLOCK> row;
-    row.open(a.logits + (size_t)j * a.ldl, a.V);
-    const float T = a.T ? a.T[j] : 1.0f, tp = a.top_p ? a.top_p[j] : 1.0f, mp = a.min_p ? a.min_p[j] : 0.0f;
-    const int k = a.top_k ? a.top_k[j] : 0;
-    float u = a.u[j];
-    u = u >= 0.0f ? fminf(u, 0x1.fffffep-1f) : 0.0f;
-#pragma unroll
-    for (int t = 0; t < PER; ++t) { s.mass[t * BLOCK + tid] = 0; s.count[t * BLOCK + tid] = 0; }
-    if (tid < 32) s.pow[tid] = ldexp(exp2(-(double)tid / 32.0), a.shift);
-    if (tid == 0) { s.above = 0; s.hit_key = ~0ull; }
+// What a row asks for.
+struct SmpAsk {
+    float T, tp, mp, u;
+    int k;
+    bool drawn, some_min;
+    double c, one, floor_w;                 // 32 log2(e) / T; 2^S; min_p 2^S
 
-    float m = -INFINITY;
-    row.each([&](float v, int) { m = fmaxf(m, v); });
-    m = wave_max_f(m);
-    if (lane == 0) s.red_d[wave] = (double)m;
-    __syncthreads();
-    m = (float)s.red_d[0];
-#pragma unroll
-    for (int w = 1; w < WAVES; ++w) m = fmaxf(m, (float)s.red_d[w]);
-    __syncthreads();
-
-    int token = -1;
-    float logp = -INFINITY;
-    if (m > -INFINITY) {                                        // else: no word can be drawn
-        if (m == INFINITY) { row.share_inf(); m = 0.0f; }
-        const bool drawn = T > 0.0f;
-        const double one = (double)(1ull << a.shift);
+    __device__ __forceinline__ void open(const SampleArgs &a, int j)
+    {
+        T = a.T ? a.T[j] : 1.0f;
+        tp = a.top_p ? a.top_p[j] : 1.0f;
+        mp = a.min_p ? a.min_p[j] : 0.0f;
+        k = a.top_k ? max(a.top_k[j], 0) : 0;
+        u = a.u[j];
+        u = u >= 0.0f ? fminf(u, 0x1.fffffep-1f) : 0.0f;
+        drawn = T > 0.0f;
+        some_min = drawn && mp > 0.0f;
+        one = (double)(1ull << a.shift);
         // (T = inf: every finite distance counts as none, an infinite one still as infinite)
-        const double c = fmax(SMP_LOG2E32 / (drawn ? (double)T : 1.0), 1e-300);
-        const bool own_sum = a.logp && (T != 1.0f), some_min = drawn && mp > 0.0f;
-        const double floor_w = (double)mp * one;
-        double e = 0.0;
-        u64 above = 0;
-        row.pieces([&](const float (&v)[4], int) {
-            double gap[4];
-#pragma unroll
-            for (int t = 0; t < 4; ++t) gap[t] = smp_gap(m, v[t]);
-            if (drawn) {
-                SmpPlace p[4];
-                double w[4];
-#pragma unroll
-                for (int t = 0; t < 4; ++t) p[t] = smp_place(gap[t], c);
-#pragma unroll
-                for (int t = 0; t < 4; ++t) w[t] = smp_weight(p[t], s.pow);
-#pragma unroll
-                for (int t = 0; t < 4; ++t)
-                    if (p[t].bin < SMP_BINS) {
-                        const u64 q = smp_whole(w[t]);
-                        atomicAdd(&s.mass[p[t].bin], q);
-                        atomicAdd(&s.count[p[t].bin], 1u);
-                        if (some_min && w[t] >= floor_w) above += q;
-                    }
-            }
-            if (own_sum) {                                      // sum of exp at T = 1: hardware exponential of the fraction of an octave
-#pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    const double x = fmin(fma(gap[t], SMP_LOG2E32 / 32.0, 0x1p20), 0x1p20 + 1024.0);
-                    const float f = (float)(unsigned)__double2loint(x) * -0x1p-32f;
-                    e += (double)ldexpf(__builtin_amdgcn_exp2f(f), -(int)((unsigned)__double2hiint(x) - 0x41300000u));
-                }
-            }
-        });
-        if (own_sum) e = wave_sum_d(e);
-        if (lane == 0) s.red_d[wave] = e;
-        if (some_min && above) atomicAdd(&s.above, above);
-        __syncthreads();
+        c = fmax(SMP_LOG2E32 / (drawn ? (double)T : 1.0), 1e-300);
+        floor_w = (double)mp * one;
+    }
+};
 
-        u64 Z = 0;
-        if (drawn) {
-            // ---- counts and masses up to and including each bin
-            u64 mm[PER], sm = 0;
-            unsigned cc[PER], sc = 0;
+template <int BLOCK> __device__ __forceinline__ float smp_block_max(float v, float *red)
+{
+    v = wave_max_f(v);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = red[0];
 #pragma unroll
-            for (int t = 0; t < PER; ++t) {
-                sm += s.mass[PER * tid + t]; mm[t] = sm;
-                sc += s.count[PER * tid + t]; cc[t] = sc;
-            }
-            u64 im = sm;
-            unsigned ic = sc;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const u64 om = __shfl_up(im, d);
-                const unsigned oc = __shfl_up(ic, d);
-                if (lane >= d) { im += om; ic += oc; }
-            }
-            if (lane == 63) { s.red_u[wave] = im; s.red_c[wave] = ic; }
-            __syncthreads();
-            im -= sm;
-            ic -= sc;
-            for (int w = 0; w < wave; ++w) { im += s.red_u[w]; ic += s.red_c[w]; }
-#pragma unroll
-            for (int t = 0; t < PER; ++t) { s.mass[PER * tid + t] = mm[t] + im; s.count[PER * tid + t] = cc[t] + ic; }
-            __syncthreads();
-            Z = s.mass[SMP_BINS - 1];
-        }
-        if (a.logp) {
-            if (own_sum) {
-                e = 0.0;
-                for (int w = 0; w < WAVES; ++w) e += s.red_d[w];
-            } else {
-                e = (double)Z / one;
-            }
-        }
+    for (int w = 1; w < BLOCK / 64; ++w) v = fmaxf(v, red[w]);
+    return v;
+}
 
-        // ---- the borders: 0 of the k best, 1 of top-p among them, 2 the drawn word (for T <= 0: the first word)
-        for (int stage = 0; stage < 3; ++stage) {
-            double need = 0.0;
-            if (!drawn) {
-                if (stage < 2) continue;
-            } else if (stage == 0) {
-                if (k <= 0 || (unsigned)k >= s.count[SMP_BINS - 1]) continue;
-            } else if (stage == 1) {
-                if (!(tp < 1.0f)) continue;
-                need = fmax((double)tp * (double)Z, 0.5);       // (the first word is kept at top_p <= 0, too)
-            } else {
-                if (some_min && s.above < Z) Z = s.above;
-                if (Z < (1ull << a.shift)) Z = 1ull << a.shift;
-                need = (double)u * (double)Z;
-            }
-            auto cond = [&](unsigned cnt, u64 mass) { return stage == 0 ? cnt >= (unsigned)k : stage == 1 ? (double)mass >= need : (double)mass > need; };
-            if (!drawn) {
-                u64 best = 0;
-                row.each([&](float v, int i) { if (v == m) { const u64 key = topk_key(v, i); best = key > best ? key : best; } });
-                best = wave_max_u64(best);
-                if (lane == 0) s.red_u[wave] = best;
-                __syncthreads();
-                for (int w = 0; w < WAVES; ++w) best = s.red_u[w] > best ? s.red_u[w] : best;
-                token = topk_key_idx(best);
-                logp = (float)-log(e);
-                break;
-            }
-            // the bin
+__device__ __forceinline__ u64 smp_wave_scan(u64 v)             // up to and including each lane
+{
+    const int lane = threadIdx.x & 63;
 #pragma unroll
-            for (int t = 0; t < PER; ++t) {
-                const int b = PER * tid + t;
-                if (cond(s.count[b], s.mass[b]) && (b == 0 || !cond(s.count[b - 1], s.mass[b - 1]))) s.bin = (unsigned)b;
-            }
-            if (tid == 0) s.listed = 0;
-            __syncthreads();
-            const unsigned bin = s.bin;
-            const u64 before_m = bin ? s.mass[bin - 1] : 0;
-            const unsigned before_c = bin ? s.count[bin - 1] : 0, members = s.count[bin] - before_c;
-            if (members <= SMP_LIST) {
-                row.each([&](float v, int i) {
-                    const SmpPlace p = smp_place(smp_gap(m, v), c);
-                    if (p.bin == bin) {
-                        const unsigned at = atomicAdd(&s.listed, 1u);
-                        s.list[at].key = topk_key(v, i);
-                        s.list[at].mass = smp_whole(smp_weight(p, s.pow));
-                    }
-                });
-                __syncthreads();
-                // each word against all of the list, by `parts` threads
-                int lg = 0;
-                while (lg < 6 && (members << (lg + 1)) <= (unsigned)BLOCK) ++lg;
-                const int parts = 1 << lg, part = tid & (parts - 1);
-                for (unsigned e0 = 0; e0 < members; e0 += BLOCK >> lg) {
-                    const unsigned x = e0 + ((unsigned)tid >> lg);
-                    const u64 key = x < members ? s.list[x].key : ~0ull;
-                    u64 ms = 0;
-                    unsigned cs = 0;
-                    if (x < members)
-                        for (unsigned o = part; o < members; o += parts)
-                            if (s.list[o].key >= key) { ms += s.list[o].mass; ++cs; }
-                    for (int d = 1; d < parts; d <<= 1) { ms += __shfl_xor(ms, d); cs += __shfl_xor(cs, d); }
-                    if (x < members && part == 0) {
-                        ms += before_m;
-                        cs += before_c;
-                        if (cond(cs, ms) && !cond(cs - 1, ms - s.list[x].mass)) { s.hit_key = key; s.hit_mass = ms; }
-                    }
-                }
-                __syncthreads();
-            } else {
-                // the key's bytes from the top: a histogram of one byte of the bin's words that agree with what is known
-                u64 known = 0, bm = before_m;
-                unsigned bc = before_c;
-                u64 *h_m = (u64 *)s.list;                       // [256]
-                unsigned *h_c = (unsigned *)(h_m + 256);        // [256]
-                for (int level = 7; level >= 0; --level) {
-                    __syncthreads();
-                    for (int d = tid; d < 256; d += BLOCK) { h_m[d] = 0; h_c[d] = 0; }
-                    __syncthreads();
-                    row.each([&](float v, int i) {
-                        const SmpPlace p = smp_place(smp_gap(m, v), c);
-                        if (p.bin != bin) return;
-                        const u64 key = topk_key(v, i);
-                        if (level < 7 && (key >> (8 * level + 8)) != (known >> (8 * level + 8))) return;
-                        const int d = (int)(key >> (8 * level)) & 255;
-                        atomicAdd(&h_m[d], smp_whole(smp_weight(p, s.pow)));
-                        atomicAdd(&h_c[d], 1u);
-                    });
-                    __syncthreads();
-                    if (tid == 0) {
-                        u64 cm = bm;
-                        unsigned ccnt = bc;
-                        for (int d = 255; d >= 0; --d)
-                            if (h_c[d]) {
-                                if (cond(ccnt + h_c[d], cm + h_m[d])) {
-                                    s.hit_key = known | ((u64)d << (8 * level));
-                                    s.hit_mass = level ? cm : cm + h_m[d];
-                                    s.listed = ccnt;
-                                    break;
-                                }
-                                cm += h_m[d];
-                                ccnt += h_c[d];
-                            }
-                    }
-                    __syncthreads();
-                    known = s.hit_key;
-                    bm = s.hit_mass;
-                    bc = s.listed;
-                }
-            }
-            if (stage < 2) {
-                Z = s.hit_mass;
-            } else {
-                token = topk_key_idx(s.hit_key);
-                logp = (float)(-smp_gap(m, topk_key_val(s.hit_key)) - log(e));
-            }
-            __syncthreads();
+    for (int d = 1; d < 64; d <<= 1) {
+        const u64 o = __shfl_up(v, d);
+        if (lane >= d) v += o;
+    }
+    return v;
+}
+
+// Counts and masses per bin -> up to and including each bin.
+template <int BLOCK> __device__ __forceinline__ void smp_scan(SmpShared<BLOCK> &s, bool counts)
+{
+    constexpr int PER = SMP_BINS / BLOCK;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    u64 mm[PER], sm = 0;
+    unsigned cc[PER], sc = 0;
+#pragma unroll
+    for (int t = 0; t < PER; ++t) {
+        sm += s.mass[smp_at(PER * tid + t)]; mm[t] = sm;
+        sc += counts ? s.count[smp_at(PER * tid + t)] : 0; cc[t] = sc;
+    }
+    u64 im = smp_wave_scan(sm);
+    unsigned ic = sc;
+    if (counts) {
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const unsigned oc = __shfl_up(ic, d);
+            if (lane >= d) ic += oc;
         }
     }
-    if (tid == 0) {
+    if (lane == 63) { s.red_u[wave] = im; s.red_c[wave] = ic; }
+    __syncthreads();
+    im -= sm;
+    ic -= sc;
+    for (int w = 0; w < wave; ++w) { im += s.red_u[w]; ic += s.red_c[w]; }
+#pragma unroll
+    for (int t = 0; t < PER; ++t) {
+        s.mass[smp_at(PER * tid + t)] = mm[t] + im;
+        if (counts) s.count[smp_at(PER * tid + t)] = cc[t] + ic;
+    }
+    __syncthreads();
+}
+
+// ---- the words of s.list in their order ----
+
+template <int J> __device__ __forceinline__ u64 smp_trade(u64 key, int lane, bool keep_larger)
+{
+    const unsigned lo = (unsigned)lane_xor_i<J>((int)(unsigned)key, lane), hi = (unsigned)lane_xor_i<J>((int)(unsigned)(key >> 32), lane);
+    const u64 o = ((u64)hi << 32) | lo;
+    return (key > o) == keep_larger ? key : o;
+}
+template <int J> __device__ __forceinline__ u64 smp_merge(u64 key, int tid, bool down)        // distances J, J / 2, ... 1
+{
+    key = smp_trade<J>(key, tid & 63, ((tid & J) == 0) == down);
+    if constexpr (J > 1) key = smp_merge<J / 2>(key, tid, down);
+    return key;
+}
+
+// The keys of s.list (s.listed of them, at most BLOCK) in descending order, one per thread (0 past the last), by a bitonic
+// network: lanes trade by register moves, waves through LDS.
+template <int BLOCK> __device__ __forceinline__ u64 smp_sorted(SmpShared<BLOCK> &s)
+{
+    const int tid = threadIdx.x;
+    const unsigned members = s.listed;
+    u64 key = (unsigned)tid < members ? s.list[tid] : 0;
+    unsigned n = 64;
+    while (n < members) n *= 2;
+    if ((unsigned)(tid & ~63) < n) {
+        key = smp_merge<1>(key, tid, (tid & 2) == 0);
+        key = smp_merge<2>(key, tid, (tid & 4) == 0);
+        key = smp_merge<4>(key, tid, (tid & 8) == 0);
+        key = smp_merge<8>(key, tid, (tid & 16) == 0);
+        key = smp_merge<16>(key, tid, (tid & 32) == 0);
+        key = smp_merge<32>(key, tid, (tid & 64) == 0);
+    }
+    for (unsigned k = 128; k <= n; k *= 2) {
+        const bool down = ((unsigned)tid & k) == 0;
+        for (unsigned j = k / 2; j >= 64; j /= 2) {
+            __syncthreads();
+            s.list[tid] = key;
+            __syncthreads();
+            const u64 o = s.list[(unsigned)tid ^ j];
+            key = (key > o) == ((((unsigned)tid & j) == 0) == down) ? key : o;
+        }
+        if ((unsigned)(tid & ~63) < n) key = smp_merge<32>(key, tid, down);
+    }
+    return key;
+}
+
+// Masses up to and including each thread's.
+template <int BLOCK> __device__ __forceinline__ u64 smp_prefix(SmpShared<BLOCK> &s, u64 own)
+{
+    const int wave = threadIdx.x >> 6;
+    u64 m = smp_wave_scan(own);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 63) s.red_u[wave] = m;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) m += s.red_u[w];
+    return m;
+}
+
+// ---------------------------------------------------------------------- borders by bins ----
+
+// Histogram of the weights of (a part of) a row, and per thread the mass of its words at or above the border of min_p.
+template <int BLOCK, class Row>
+__device__ __forceinline__ u64 smp_histogram(const Row &row, SmpShared<BLOCK> &s, const SmpAsk &q, float m)
+{
+    u64 above = 0;
+    row.pieces([&](const float (&v)[4], int) {
+        SmpPlace p[4];
+        double w[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) p[t] = smp_place(smp_gap(m, v[t]), q.c);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) w[t] = smp_weight(p[t], s.pow);
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+            if (p[t].bin < SMP_BINS) {
+                const u64 x = smp_whole(w[t]);
+                atomicAdd(&s.mass[smp_at(p[t].bin)], x);
+                if (q.k > 0) atomicAdd(&s.count[smp_at(p[t].bin)], 1u);
+                if (w[t] >= q.floor_w) above += x;
+            }
+    });
+    return above;
+}
+
+__device__ __forceinline__ u64 smp_mass_of(u64 key, float m, double c, const double *s_pow)
+{
+    const SmpPlace p = smp_place(smp_gap(m, topk_key_val(key)), c);
+    return p.bin < SMP_BINS ? smp_whole(smp_weight(p, s_pow)) : 0;
+}
+
+__device__ __forceinline__ u64 smp_lane(u64 v, unsigned lane)
+{
+    return ((u64)(unsigned)__builtin_amdgcn_readlane((int)(unsigned)(v >> 32), (int)lane) << 32) | (unsigned)__builtin_amdgcn_readlane((int)(unsigned)v, (int)lane);
+}
+
+// The first bin at which cond(count, mass up to and including it) is true; SMP_BINS - 1 if none.  By every wave for itself.
+template <int BLOCK, class Cond> __device__ __forceinline__ unsigned smp_find(const SmpShared<BLOCK> &s, bool counts, Cond cond)
+{
+    const int lane = threadIdx.x & 63;
+    constexpr int STEP = SMP_BINS / 64;
+    const unsigned a = smp_at(STEP * lane + STEP - 1);
+    const u64 far = __ballot(cond(counts ? s.count[a] : 0u, s.mass[a]));
+    const int group = far ? __ffsll((long long)far) - 1 : 63;
+    const unsigned b = smp_at(STEP * group + min(lane, STEP - 1));
+    const u64 close = __ballot(cond(counts ? s.count[b] : 0u, s.mass[b]));
+    return (unsigned)(STEP * group + (close ? min(__ffsll((long long)close) - 1, STEP - 1) : STEP - 1));
+}
+
+// The logits of the bins from b0 to b1, a little wider: what rounding there is, is below 2^-20 of the largest logit and the distance.
+struct SmpWindow {
+    unsigned b0, b1;
+    float low, high;
+    __device__ __forceinline__ void open(unsigned first, unsigned last, float m, double c)
+    {
+        b0 = first;
+        b1 = last;
+        const double gap0 = (double)first / c, gap1 = ((double)last + 1.0) / c, am = fabs((double)m);
+        high = (float)((double)m - gap0 + 1e-6 * (am + gap0));
+        low = (float)((double)m - gap1 - 1e-6 * (am + gap1));
+    }
+    __device__ __forceinline__ bool near(float v) const { return v >= low && v <= high; }
+    __device__ __forceinline__ bool has(unsigned bin) const { return bin >= b0 && bin <= b1; }
+};
+
+// The drawn word of a row whose bins are in s.mass / s.count (up to and including each; counts only if top-k is in force) and
+// whose mass of words at or above the min_p border is s.above: for each border the one bin that it falls into, then the
+// words of that bin in their order.  words(window, f) calls f(key) for every word of a bin.  While there are more than BLOCK, a
+// histogram over 256 even parts of the range of their keys says in which of them the border lies.
+template <int BLOCK, class Words>
+__device__ __forceinline__ u64 smp_borders(Words words, SmpShared<BLOCK> &s, const SmpAsk &q, float m, int shift)
+{
+    const int tid = threadIdx.x;
+    u64 Z = s.mass[smp_at(SMP_BINS - 1)], found = 0, found_m = 0;
+#pragma unroll 1
+    for (int stage = 0; stage < 3; ++stage) {                  // 0: of the k best, 1: of top-p among them, 2: the drawn word
+        double need = 0.0;
+        if (stage == 0) {
+            if (q.k <= 0 || (unsigned)q.k >= s.count[smp_at(SMP_BINS - 1)]) continue;
+        } else if (stage == 1) {
+            if (!(q.tp < 1.0f)) continue;
+            need = fmax((double)q.tp * (double)Z, 0.5);         // (the first word is kept at top_p <= 0, too)
+        } else {
+            if (q.some_min && s.above < Z) Z = s.above;
+            if (Z < (1ull << shift)) Z = 1ull << shift;
+            need = (double)q.u * (double)Z;
+        }
+        auto cond = [&](unsigned cnt, u64 mass) { return stage == 0 ? cnt >= (unsigned)q.k : stage == 1 ? (double)mass >= need : (double)mass > need; };
+        const unsigned bin = smp_find<BLOCK>(s, stage == 0, cond);
+        u64 before_m = bin ? s.mass[smp_at(bin - 1)] : 0;
+        unsigned before_c = stage == 0 && bin ? s.count[smp_at(bin - 1)] : 0;
+        SmpWindow win;
+        win.open(bin, bin, m, q.c);
+        u64 lowest = topk_key(win.low, 0x7fffffff), highest = topk_key(win.high, 0);
+        for (;;) {
+            if (tid == 0) s.listed = 0;
+            __syncthreads();
+            words(win, [&](u64 key) {
+                if (key < lowest || key > highest) return;
+                const unsigned at = atomicAdd(&s.listed, 1u);
+                if (at < BLOCK) s.list[at] = key;
+            });
+            __syncthreads();
+            const unsigned members = s.listed;
+            if (members <= 64) {                                // few: every wave for itself, each lane's word against all others
+                const int lane = tid & 63;
+                const u64 key = (unsigned)lane < members ? s.list[lane] : 0;
+                const u64 own = key ? smp_mass_of(key, m, q.c, s.pow) : 0;
+                u64 ms = before_m;
+                unsigned cs = before_c;
+                for (unsigned o = 0; o < members; ++o) {
+                    const u64 ko = smp_lane(key, o), mo = smp_lane(own, o);
+                    if (ko >= key) { ms += mo; ++cs; }
+                }
+                const u64 hit = __ballot(key && cond(cs, ms) && !cond(cs - 1, ms - own));
+                const int at = hit ? __ffsll((long long)hit) - 1 : 0;
+                found = smp_lane(key, at);
+                found_m = smp_lane(ms, at);
+                break;
+            }
+            if (members <= BLOCK) {
+                const u64 key = smp_sorted<BLOCK>(s);
+                const u64 own = key ? smp_mass_of(key, m, q.c, s.pow) : 0;
+                const u64 ms = before_m + smp_prefix<BLOCK>(s, own);
+                const unsigned cs = before_c + tid + 1;
+                if (key && cond(cs, ms) && !cond(cs - 1, ms - own)) { s.hit_key = key; s.hit_mass = ms; }
+                __syncthreads();
+                found = s.hit_key;
+                found_m = s.hit_mass;
+                break;
+            }
+            __syncthreads();
+            u64 *h_m = s.list;                                  // [256], the block has at least as many threads
+            const int sh = max(0, 64 - 8 - __clzll((long long)(highest - lowest)));
+            if (tid < 256) { h_m[tid] = 0; s.bytes[tid] = 0; }
+            __syncthreads();
+            words(win, [&](u64 key) {
+                if (key < lowest || key > highest) return;
+                const unsigned d = (unsigned)((key - lowest) >> sh);
+                atomicAdd(&h_m[d], smp_mass_of(key, m, q.c, s.pow));
+                atomicAdd(&s.bytes[d], 1u);
+            });
+            __syncthreads();
+            const unsigned d = 255u - (unsigned)tid;            // from the top
+            const u64 own = tid < 256 ? h_m[d] : 0;
+            const unsigned own_c = tid < 256 ? s.bytes[d] : 0;
+            const u64 ms = before_m + smp_prefix<BLOCK>(s, own);
+            const unsigned cs = before_c + (unsigned)smp_prefix<BLOCK>(s, own_c);
+            if (own_c && cond(cs, ms) && !cond(cs - own_c, ms - own)) { s.hit_key = lowest + ((u64)d << sh); s.hit_mass = ms - own; s.known_c = cs - own_c; }
+            __syncthreads();
+            lowest = s.hit_key;
+            highest = lowest + ((1ull << sh) - 1);
+            before_m = s.hit_mass;
+            before_c = s.known_c;
+            __syncthreads();
+        }
+        if (stage < 2) Z = found_m;
+        __syncthreads();
+    }
+    return found;
+}
+
+// ---------------------------------------------------------------------- borders by a list ----
+
+// The words of s.list (s.listed of them, at most BLOCK): a prefix of the row's order, all of the row's words if `whole`.
+// total: the mass of the row, 0 where it was not summed (then top-k makes it unnecessary, or no other filter and a list of all
+// words at or above the min_p border).  Returns the drawn word's key; 0 if a border lies below the list.
+template <int BLOCK>
+__device__ __forceinline__ u64 smp_borders_of_list(SmpShared<BLOCK> &s, const SmpAsk &q, float m, u64 total, bool whole, int shift)
+{
+    const int tid = threadIdx.x;
+    const unsigned members = s.listed;
+    if (members == 0) return 0;
+    if (tid == 0) { s.k_mass = 0; s.hit_key = 0; s.above = 0; s.below = 0; }
+    const u64 key = smp_sorted<BLOCK>(s);
+    const bool mine = (unsigned)tid < members;
+    const SmpPlace p = smp_place(smp_gap(m, topk_key_val(key)), q.c);
+    const double w = mine && p.bin < SMP_BINS ? smp_weight(p, s.pow) : 0.0;
+    const u64 own = smp_whole(w), ms = smp_prefix<BLOCK>(s, own);
+    if ((unsigned)tid == members - 1) s.sum = ms;
+    if (q.k > 0 && mine && tid == q.k - 1) s.k_mass = ms;
+    if (q.some_min && mine) {                            // what min_p keeps ends at the last word at or above its border
+        if (w >= q.floor_w) atomicMax(&s.above, ms);
+        else s.below = 1;
+    }
+    __syncthreads();
+    const u64 have = s.sum;
+    u64 Z = total;
+    if (q.k > 0) Z = s.k_mass ? s.k_mass : whole ? have : 0;
+    else if (!total) Z = max(s.above, 1ull << shift);
+    const bool min_known = q.some_min && (s.below || whole || (!q.k && !total));
+    if (Z == 0) return 0;                                // the k-th word lies below the list
+    if (q.tp < 1.0f) {
+        const double need = fmax((double)q.tp * (double)Z, 0.5);
+        if ((double)have < need) return 0;
+        if (mine && (double)ms >= need && !((double)(ms - own) >= need)) s.hit_mass = ms;
+        __syncthreads();
+        Z = s.hit_mass;
+    }
+    if (q.some_min) {
+        if (min_known) Z = s.above < Z ? s.above : Z;
+        else if (Z > have) return 0;
+    }
+    if (Z < (1ull << shift)) Z = 1ull << shift;
+    const double need = (double)q.u * (double)Z;
+    if (!((double)have > need)) return 0;
+    if (mine && (double)ms > need && !((double)(ms - own) > need)) s.hit_key = key;
+    __syncthreads();
+    return s.hit_key;
+}
+
+__device__ __forceinline__ void smp_write(const SampleArgs &a, int j, int token, float logp, int block)
+{
+    if (threadIdx.x == 0) {
         a.tokens[j] = token;
         if (a.logp) a.logp[j] = logp;
     }
     if (a.E_tgt)
-        for (int i = tid; i < a.E; i += BLOCK) a.y_emb[(size_t)j * a.E + i] = token >= 0 ? a.E_tgt[(size_t)token * a.E + i] : 0.0f;
+        for (int i = threadIdx.x; i < a.E; i += block) a.y_emb[(size_t)j * a.E + i] = token >= 0 ? a.E_tgt[(size_t)token * a.E + i] : 0.0f;
 }
 
-q8_status q8i_sample(q8_ctx *ctx, const float *logits, int n, int V, int ldl, const q8_sampling *s, const float *u, int32_t *tokens, float *logp,
-                     const float *E_tgt, int E, float *y_emb)
+// ------------------------------------------------------------------------- a block per row ----
+
+// The row in registers.  Most rows are settled by the words at their top: with the s-th largest of each wave's 64 thread maxima,
+// the least of these over the waves has at least s words of every wave at or above it; these words are collected and sorted.
+// Only where a border lies below them (flat rows), the weights go into bins.
+template <int NE, int BLOCK>
+__global__ __launch_bounds__(BLOCK) void sample_row_kernel(SampleArgs a)
 {
-    SampleArgs a = {logits, (size_t)ldl, V, u, nullptr, nullptr, nullptr, nullptr, tokens, logp, E_tgt, y_emb, E, 0};
+    extern __shared__ __align__(16) char smem[];
+    SmpShared<BLOCK> &s = *(SmpShared<BLOCK> *)smem;
+    const int j = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    constexpr int WAVES = BLOCK / 64, PER = SMP_BINS / BLOCK;
+    SmpRow<NE, BLOCK> row;
+    row.open(a.logits + (size_t)j * a.ldl, a.V, 0, 0x7fffffff / 4);
+    SmpAsk q;
+    q.open(a, j);
+    if (tid < 32) s.pow[tid] = smp_pow[tid] * q.one;
+    if (tid == 0) { s.sum = 0; s.listed = 0; }
+
+    float tm = row.largest();
+    float m = smp_block_max<BLOCK>(tm, s.red_f);
+    if (m == -INFINITY) { smp_write(a, j, -1, -INFINITY, BLOCK); return; }              // no word can be drawn
+    if (m == INFINITY) {
+        row.share_inf();
+        m = 0.0f;
+        tm = row.largest();
+    }
+    // ---- how far down the words are collected
+    const int full = min(max((a.V + 3) / 256, 1), WAVES);                                // waves whose threads all have words
+    const bool short_list = q.k > 0 && q.k <= 16 * full;                                 // top-k from the list alone
+    const int rank = min(short_list ? (q.k + full - 1) / full : 64 / full, 64);
+    const float sorted = wave_sort_desc_f(tm, lane);
+    if (lane == rank - 1) s.red_g[wave] = sorted;
+    __syncthreads();
+    float thr = s.red_g[0];
+    for (int w = 1; w < full; ++w) thr = fminf(thr, s.red_g[w]);
+    const bool min_only = q.some_min && !q.k && !(q.tp < 1.0f);
+    if (min_only)                                                                        // a little below the border of min_p
+        thr = (float)((double)m + fmin(log((double)q.mp), 0.0) * (double)q.T * 1.000001 - 1e-6 - 1e-6 * fabs((double)m));
+    if (!q.drawn) thr = m;
+    const bool need_total = q.drawn && !short_list && !min_only, own_sum = a.logp && !(need_total && q.T == 1.0f);
+
+    row.some([&](float v) { return v >= thr; }, [&](float v) { return v > -INFINITY; }, [&](u64 key) {
+        const unsigned at = atomicAdd(&s.listed, 1u);
+        if (at < BLOCK) s.list[at] = key;
+    });
+    double e = 0.0;
+    if (need_total) {
+        u64 sum = 0;
+        row.pieces([&](const float (&v)[4], int) {
+            SmpPlace p[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) p[t] = smp_place(smp_gap(m, v[t]), q.c);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) sum += smp_whole(smp_weight(p[t], s.pow));       // (zero past the bins)
+        });
+        if (sum) atomicAdd(&s.sum, sum);
+    }
+    if (own_sum) {
+        row.pieces([&](const float (&v)[4], int) {
+#pragma unroll
+            for (int t = 0; t < 4; t += 2) e += (double)(exp_le0(v[t] - m) + exp_le0(v[t + 1] - m));      // as the vocabulary layer's selection
+        });
+        e = wave_sum_d(e);
+        if (lane == 0) s.red_d[wave] = e;
+    }
+    __syncthreads();
+    const u64 total = need_total ? s.sum : 0;
+    const unsigned listed = s.listed;
+    if (own_sum) {
+        e = 0.0;
+        for (int w = 0; w < WAVES; ++w) e += s.red_d[w];
+    } else {
+        e = (double)total / q.one;
+    }
+    __syncthreads();
+
+    u64 key = 0;
+    if (listed <= BLOCK) {
+        if (q.drawn) {
+            key = smp_borders_of_list<BLOCK>(s, q, m, total, thr == -INFINITY, a.shift);
+        } else {                                        // the list: the words with the largest logit
+            key = smp_sorted<BLOCK>(s);
+            if (tid == 0) s.hit_key = key;
+            __syncthreads();
+            key = s.hit_key;
+        }
+    } else if (!q.drawn) {
+        u64 best = 0;
+        row.stored().pieces([&](const float (&v)[4], int i) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                if (v[t] == m) best = max(best, topk_key(v[t], i + t));
+        });
+        best = wave_max_u64(best);
+        if (lane == 0) s.red_u[wave] = best;
+        __syncthreads();
+        for (int w = 0; w < WAVES; ++w) key = max(key, s.red_u[w]);
+    }
+    if (key == 0) {
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < PER; ++t) { s.mass[smp_at(t * BLOCK + tid)] = 0; s.count[smp_at(t * BLOCK + tid)] = 0; }
+        if (tid == 0) s.above = 0;
+        __syncthreads();
+        const u64 above = smp_histogram<BLOCK>(row, s, q, m);
+        if (q.some_min && above) atomicAdd(&s.above, above);
+        __syncthreads();
+        smp_scan<BLOCK>(s, q.k > 0);
+        const auto stored = row.stored();
+        key = smp_borders<BLOCK>([&](const SmpWindow &win, auto f) {
+            stored.some([&](float v) { return win.near(v); }, [&](float v) { return smp_place(smp_gap(m, v), q.c).bin == win.b0; }, f);
+        }, s, q, m, a.shift);
+    }
+    smp_write(a, j, topk_key_idx(key), (float)(-smp_gap(m, topk_key_val(key)) - log(e)), BLOCK);
+}
+
+// ---------------------------------------------------------------------- rows over several blocks ----
+
+// What the launches leave for each other.
+struct SmpRowState {
+    u64 mass[SMP_BINS];
+    unsigned count[SMP_BINS];
+    u64 list[SMP_LIST];
+    double e[SMP_PARTS];                    // sum of exp at T = 1 of a part
+    float top[SMP_PARTS];                   // its largest logit
+    u64 above;
+    unsigned listed, arrived;
+};
+
+// 1. The largest logit of each part; the row's sums are set to zero.
+__global__ __launch_bounds__(256) void sample_top_kernel(SampleArgs a)
+{
+    __shared__ float red[4];
+    const int j = a.row0 + blockIdx.y, part = blockIdx.x, tid = threadIdx.x;
+    SmpRowState &st = a.state[blockIdx.y];
+    SmpRow<0, 256> row;
+    row.open(a.logits + (size_t)j * a.ldl, a.V, part * a.part_pieces, a.part_pieces);
+    for (int b = part * 256 + tid; b < SMP_BINS; b += 256 * a.parts) { st.mass[b] = 0; st.count[b] = 0; }
+    if (part == 0 && tid == 0) { st.above = 0; st.listed = 0; st.arrived = 0; }
+    const float m = smp_block_max<256>(row.largest(), red);
+    if (tid == 0) st.top[part] = m;
+}
+
+__device__ __forceinline__ float smp_row_top(const SampleArgs &a, const SmpRowState &st)       // by every wave for itself
+{
+    float m = -INFINITY;
+    for (int p = threadIdx.x & 63; p < a.parts; p += 64) m = fmaxf(m, st.top[p]);
+    return wave_max_f(m);
+}
+
+// The sum of the parts' sums, in one order, by every wave for itself.
+__device__ __forceinline__ double smp_row_e(const SampleArgs &a, const SmpRowState &st)
+{
+    double e = 0.0;
+    for (int p = threadIdx.x & 63; p < a.parts; p += 64) e += st.e[p];
+    return wave_sum_d(e);
+}
+
+// 2. The weights of each part into bins, and the bins into the row's.
+template <int NE>
+__global__ __launch_bounds__(256) void sample_bins_kernel(SampleArgs a)
+{
+    extern __shared__ __align__(16) char smem[];
+    SmpShared<256> &s = *(SmpShared<256> *)smem;
+    const int j = a.row0 + blockIdx.y, part = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    SmpRowState &st = a.state[blockIdx.y];
+    SmpRow<NE, 256> row;
+    row.open(a.logits + (size_t)j * a.ldl, a.V, part * a.part_pieces, a.part_pieces);
+    SmpAsk q;
+    q.open(a, j);
+    float m = smp_row_top(a, st);
+    if (tid < 32) s.pow[tid] = smp_pow[tid] * q.one;
+    if (m == -INFINITY) return;
+    if (m == INFINITY) { row.share_inf(); m = 0.0f; }
+    if (q.drawn) {
+#pragma unroll
+        for (int t = 0; t < SMP_BINS / 256; ++t) { s.mass[smp_at(t * 256 + tid)] = 0; s.count[smp_at(t * 256 + tid)] = 0; }
+    }
+    __syncthreads();
+    const bool own_sum = a.logp && q.T != 1.0f;
+    if (own_sum) {
+        double e = 0.0;
+        row.pieces([&](const float (&v)[4], int) {
+#pragma unroll
+            for (int t = 0; t < 4; t += 2) e += (double)(exp_le0(v[t] - m) + exp_le0(v[t + 1] - m));      // as the vocabulary layer's selection
+        });
+        e = wave_sum_d(e);
+        if (lane == 0) s.red_d[wave] = e;
+    }
+    u64 above = 0;
+    if (q.drawn) above = smp_histogram<256>(row, s, q, m);
+    __syncthreads();
+    if (tid == 0 && own_sum) st.e[part] = (s.red_d[0] + s.red_d[1]) + (s.red_d[2] + s.red_d[3]);
+    if (!q.drawn) return;
+    if (q.some_min && above) atomicAdd(&st.above, above);
+#pragma unroll
+    for (int t = 0; t < SMP_BINS / 256; ++t) {
+        const int b = t * 256 + tid;
+        const u64 x = s.mass[smp_at(b)];
+        if (x) atomicAdd(&st.mass[b], x);
+        const unsigned c = q.k > 0 ? s.count[smp_at(b)] : 0;
+        if (c) atomicAdd(&st.count[b], c);
+    }
+}
+
+// 3. The bins that the borders fall into, as far as the bins alone tell (a border's mass is known to one bin, and what depends on
+// it to the bins that both ends give); the words of these bins, from every part; and the last part to be done finds the
+// borders among them.
+template <int NE>
+__global__ __launch_bounds__(256) void sample_draw_kernel(SampleArgs a)
+{
+    extern __shared__ __align__(16) char smem[];
+    SmpShared<256> &s = *(SmpShared<256> *)smem;
+    __shared__ u64 s_found[SMP_LIST];
+    __shared__ unsigned s_n, s_at, s_last;
+    const int j = a.row0 + blockIdx.y, part = blockIdx.x, tid = threadIdx.x;
+    SmpRowState &st = a.state[blockIdx.y];
+    SmpRow<NE, 256> row;
+    SmpAsk q;
+    q.open(a, j);
+    // (requested before anything is waited for)
+    u64 mass[SMP_BINS / 256];
+    unsigned count[SMP_BINS / 256];
+#pragma unroll
+    for (int t = 0; t < SMP_BINS / 256; ++t) { mass[t] = st.mass[t * 256 + tid]; count[t] = st.count[t * 256 + tid]; }
+    const u64 above = st.above;
+    const double e_parts = smp_row_e(a, st);
+    row.open(a.logits + (size_t)j * a.ldl, a.V, part * a.part_pieces, a.part_pieces);
+    float m = smp_row_top(a, st);
+    if (m == -INFINITY) {                               // no word can be drawn
+        if (part == 0) smp_write(a, j, -1, -INFINITY, 256);
+        return;
+    }
+    if (m == INFINITY) { row.share_inf(); m = 0.0f; }
+    if (tid < 32) s.pow[tid] = smp_pow[tid] * q.one;
+    if (tid == 0) { s_n = 0; s.above = above; }
+    SmpWindow w[3];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) { w[i].b0 = 1; w[i].b1 = 0; w[i].low = INFINITY; w[i].high = -INFINITY; }
+    if (q.drawn) {
+#pragma unroll
+        for (int t = 0; t < SMP_BINS / 256; ++t) { s.mass[smp_at(t * 256 + tid)] = mass[t]; s.count[smp_at(t * 256 + tid)] = count[t]; }
+        __syncthreads();
+        smp_scan<256>(s, q.k > 0);
+        u64 low = s.mass[smp_at(SMP_BINS - 1)], high = low;
+        if (q.k > 0 && (unsigned)q.k < s.count[smp_at(SMP_BINS - 1)]) {
+            const unsigned b = smp_find<256>(s, true, [&](unsigned c, u64) { return c >= (unsigned)q.k; });
+            w[0].open(b, b, m, q.c);
+            low = b ? s.mass[smp_at(b - 1)] : 0;
+            high = s.mass[smp_at(b)];
+        }
+        if (q.tp < 1.0f) {
+            const double n0 = fmax((double)q.tp * (double)low, 0.5), n1 = fmax((double)q.tp * (double)high, 0.5);
+            const unsigned b0 = smp_find<256>(s, false, [&](unsigned, u64 x) { return (double)x >= n0; }), b1 = smp_find<256>(s, false, [&](unsigned, u64 x) { return (double)x >= n1; });
+            w[1].open(b0, b1, m, q.c);
+            low = b0 ? s.mass[smp_at(b0 - 1)] : 0;
+            high = s.mass[smp_at(b1)];
+        }
+        if (q.some_min) { low = min(low, above); high = min(high, above); }
+        const u64 first = 1ull << a.shift;
+        const double n0 = (double)q.u * (double)max(low, first), n1 = (double)q.u * (double)max(high, first);
+        w[2].open(smp_find<256>(s, false, [&](unsigned, u64 x) { return (double)x > n0; }), smp_find<256>(s, false, [&](unsigned, u64 x) { return (double)x > n1; }), m, q.c);
+    } else {
+        w[2].low = w[2].high = m;
+        w[2].b0 = 0; w[2].b1 = SMP_BINS;
+        __syncthreads();
+    }
+    // ---- the words of those bins
+    const bool use0 = w[0].b0 <= w[0].b1, use1 = w[1].b0 <= w[1].b1;
+    row.some([&](float v) {
+                 bool n = w[2].near(v);
+                 if (use0) n = n || w[0].near(v);
+                 if (use1) n = n || w[1].near(v);
+                 return n;
+             },
+             [&](float v) {
+                 const unsigned b = smp_place(smp_gap(m, v), q.c).bin;
+                 return w[0].has(b) || w[1].has(b) || w[2].has(b);
+             },
+             [&](u64 key) {
+                 const unsigned at = atomicAdd(&s_n, 1u);
+                 if (at < SMP_LIST) s_found[at] = key;
+             });
+    __syncthreads();
+    const unsigned found = s_n;
+    if (tid == 0) s_at = found ? atomicAdd(&st.listed, found <= SMP_LIST ? found : SMP_LIST + 1) : 0u;
+    __syncthreads();
+    for (unsigned x = tid; x < min(found, (unsigned)SMP_LIST); x += 256)
+        if (s_at + x < SMP_LIST) __hip_atomic_store(&st.list[s_at + x], s_found[x], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    q8_stores_performed();
+    __syncthreads();
+    if (tid == 0) s_last = __hip_atomic_fetch_add(&st.arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)a.parts - 1 ? 1u : 0u;
+    __syncthreads();
+    if (!s_last) return;
+
+    // ---- the last part: the borders
+    const unsigned listed = __hip_atomic_load(&st.listed, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    SmpRow<0, 256> whole;
+    whole.open(a.logits + (size_t)j * a.ldl, a.V, 0, 0x7fffffff / 4);
+    whole.top_inf = row.top_inf;
+    if (listed <= SMP_LIST) {                           // from here on in LDS
+        for (unsigned x = tid; x < listed; x += 256) s_found[x] = __hip_atomic_load(&st.list[x], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __syncthreads();
+    }
+    u64 key;
+    if (q.drawn) {
+        key = smp_borders<256>([&](const SmpWindow &win, auto f) {
+            auto in = [&](float v) { return smp_place(smp_gap(m, v), q.c).bin == win.b0; };
+            if (listed > SMP_LIST) {
+                whole.some([&](float v) { return win.near(v); }, in, f);
+                return;
+            }
+            for (unsigned x = tid; x < listed; x += 256)
+                if (in(topk_key_val(s_found[x]))) f(s_found[x]);
+        }, s, q, m, a.shift);
+    } else {
+        u64 best = 0;
+        if (listed > SMP_LIST) {
+            whole.pieces([&](const float (&v)[4], int i) {
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+                    if (v[t] == m) best = max(best, topk_key(v[t], i + t));
+            });
+        } else {
+            for (unsigned x = tid; x < listed; x += 256) best = max(best, s_found[x]);
+        }
+        best = wave_max_u64(best);
+        if ((tid & 63) == 0) s.red_u[tid >> 6] = best;
+        __syncthreads();
+        key = max(max(s.red_u[0], s.red_u[1]), max(s.red_u[2], s.red_u[3]));
+    }
+    const double e = q.T == 1.0f ? (double)s.mass[smp_at(SMP_BINS - 1)] / q.one : e_parts;
+    smp_write(a, j, topk_key_idx(key), (float)(-smp_gap(m, topk_key_val(key)) - log(e)), 256);
+}
+
+static int sample_rows(int n) { return n < SMP_ROWS ? n : SMP_ROWS; }
+
+size_t q8i_sample_bytes(int n, int V) { return V <= SMP_SMALL ? 0 : (size_t)sample_rows(n) * sizeof(SmpRowState); }
+
+q8_status q8i_sample(q8_ctx *ctx, const float *logits, int n, int V, int ldl, const q8_sampling *s, const float *u, int32_t *tokens, float *logp,
+                     const float *E_tgt, int E, float *y_emb, void *state)
+{
+    SampleArgs a;
+    memset(&a, 0, sizeof(a));
+    a.logits = logits; a.ldl = (size_t)ldl; a.V = V; a.u = u; a.tokens = tokens; a.logp = logp; a.E_tgt = E_tgt; a.E = E; a.y_emb = y_emb;
     if (s) { a.T = s->temperature; a.top_k = s->top_k; a.top_p = s->top_p; a.min_p = s->min_p; }
     int bits = 0;
     while (((size_t)1 << bits) < (size_t)V) ++bits;
     a.shift = 62 - bits < 46 ? 62 - bits : 46;                // the sum of V weights stays below 2^63
-    const size_t smem = sizeof(SmpShared);
-    // registers for the whole row (up to three words before it in its first piece) where a block has enough
-#define SMP_GO(NE, BLOCK) hipLaunchKernelGGL((sample_row_kernel<NE, BLOCK>), dim3(n), dim3(BLOCK), smem, ctx->stream, a)
-    const int words = V + 3;
-    if (words <= 256 * 8) SMP_GO(8, 256);
-    else if (words <= 1024 * 8) SMP_GO(8, 1024);
-    else if (words <= 1024 * 24) SMP_GO(24, 1024);
-    else if (words <= 1024 * 52) SMP_GO(52, 1024);
-    else if (words <= 1024 * 64) SMP_GO(64, 1024);
-    else SMP_GO(0, 1024);
-#undef SMP_GO
-    return q8i_launch_check(ctx, "sample");
+    const size_t smem = sizeof(SmpShared<256>);
+    // A block per row while its threads hold eight words each at most: 5 rows of 2500 / 8001 words 12.9 / 13.5 us against 19.8 / 19.7 over
+    // several blocks, of 50000 words 25 to 29 against 18 to 23 (1 to 8 rows; 64 rows 41 against 38).
+    if (V <= SMP_SMALL) {
+        if (V <= SMP_SMALL / 4) hipLaunchKernelGGL((sample_row_kernel<8, 256>), dim3(n), dim3(256), smem, ctx->stream, a);
+        else hipLaunchKernelGGL((sample_row_kernel<8, 1024>), dim3(n), dim3(1024), sizeof(SmpShared<1024>), ctx->stream, a);
+        return q8i_launch_check(ctx, "sample");
+    }
+    a.state = (SmpRowState *)state;
+    const int pieces = (V + 3) / 4;
+    for (a.row0 = 0; a.row0 < n; a.row0 += SMP_ROWS) {
+        const int rows = n - a.row0 < SMP_ROWS ? n - a.row0 : SMP_ROWS;
+        // three blocks a compute unit, which is what it holds of them, none of less than 2048 words: 64 rows of 50000 words 44.6 / 38.9 / 37.6
+        // / 40.6 us with 1024 / 768 / 512 / 256 blocks, 12 of 250001 32.5 / 26.3 / 30.3 / 33.3
+        int parts = (768 + rows - 1) / rows;
+        if (parts > (pieces + 511) / 512) parts = (pieces + 511) / 512;
+        if (parts > SMP_PARTS) parts = SMP_PARTS;
+        a.part_pieces = (pieces + parts - 1) / parts;
+        a.parts = (pieces + a.part_pieces - 1) / a.part_pieces;
+        const dim3 grid(a.parts, rows);
+        hipLaunchKernelGGL(sample_top_kernel, grid, dim3(256), 0, ctx->stream, a);
+        if (a.part_pieces <= 1024) {
+            hipLaunchKernelGGL(sample_bins_kernel<16>, grid, dim3(256), smem, ctx->stream, a);
+            hipLaunchKernelGGL(sample_draw_kernel<16>, grid, dim3(256), smem, ctx->stream, a);
+        } else {
+            hipLaunchKernelGGL(sample_bins_kernel<0>, grid, dim3(256), smem, ctx->stream, a);
+            hipLaunchKernelGGL(sample_draw_kernel<0>, grid, dim3(256), smem, ctx->stream, a);
+        }
+        const q8_status st = q8i_launch_check(ctx, "sample");
+        if (st) return st;
+    }
+    return Q8_OK;
 }

@@ -59,3 +59,5 @@ def test_calls_without_a_context_return_the_null_code():
     assert q.q8_sample_bytes(1, 1) > 0
     for n, cols in ((1, 16384), (1024, 16384), (1024, 16), (700, 620)):
         assert q.q8_workspace_bytes(n, 1, 1, (cols + 15) // 16 * 16) >= q.q8_gemm_f8_bytes(n, cols)
+    for n, V in ((1, 8193), (1024, 9000), (1, 1 << 24)):
+        assert q.q8_workspace_bytes(n, 1, V, 16) >= q.q8_sample_bytes(n, V)

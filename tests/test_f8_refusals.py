@@ -103,6 +103,7 @@ def test_draws(lib):
     assert call(lg=None) == call(u=None) == call(tok=None) == call(e=P, E=8) == call(y=P, E=8) == NULL
     assert call(n=0) == call(n=65537) == call(V=0) == call(V=(1 << 24) + 1, ld=1 << 25) == call(ld=99) == call(e=P, E=0, y=P) == SHAPE
     assert call(lg=P + 2) == call(u=P + 1) == call(tok=P + 2) == call(lp=P + 2) == call(e=P + 1, E=8, y=P) == ALIGN
+    assert call(V=9000, ld=9000) == WORKSPACE and lib.q8_sample_bytes(4, 9000) > lib.q8_sample_bytes(4, 100)
     for k in range(4):
         assert call(s=C.byref(_Sampling(*[P + 2 if i == k else None for i in range(4)]))) == ALIGN
     assert call() == call(s=C.byref(_Sampling(P, P, P, P)), e=P, E=8, y=P, lp=P) == call(n=1, ld=0) == DEVICE

@@ -1827,7 +1827,7 @@ q8_status q8_gemm_codes_f8(q8_ctx *ctx, const q8_mat_f8 *W, const q8_mat_f8 *X, 
     TRY(check_mat_f8(ctx, X, kF8MaxN, "X"));
     if (X->cols != W->cols) return q8_fail(ctx, Q8_ERR_SHAPE, "X has %d columns, W %d", X->cols, W->cols);
     TRY(check_result_f8(ctx, bias, Y, X->rows, W->rows, ldy));
-    return q8i_gemm_f8(ctx, W, X, bias, Y, ldy);
+    return q8i_gemm_f8(ctx, W, X, nullptr, 0, bias, Y, ldy);
 }
 
 q8_status q8_gemm_f8(q8_ctx *ctx, const q8_mat_f8 *W, const float *X, int n, int ldx, const float *bias, float *Y, int ldy)
@@ -1841,10 +1841,9 @@ q8_status q8_gemm_f8(q8_ctx *ctx, const q8_mat_f8 *W, const float *X, int n, int
     q8_mat_f8 xq = {nullptr, nullptr, n, W->cols, f8_pitch(W->cols), f8_scale_pitch(W->cols)};
     uint8_t *codes = cv.take<uint8_t>((size_t)n * xq.ld), *scale = cv.take<uint8_t>((size_t)n * xq.lds);
     if (!cv.ok) return q8_fail(ctx, Q8_ERR_WORKSPACE, "q8_gemm_f8: workspace too small");
-    TRY(q8i_quantize_f8(ctx, X, n, W->cols, ldx, codes, xq.ld, scale, xq.lds));
     xq.data = codes;
     xq.scale = scale;
-    return q8i_gemm_f8(ctx, W, &xq, bias, Y, ldy);
+    return q8i_gemm_f8(ctx, W, &xq, X, ldx, bias, Y, ldy);
 }
 
 q8_status output_logits_f8(q8_ctx *ctx, const q8_readout_weights *ro, const q8_mat_f8 *W_out, const float *b_out, const float *s,
@@ -1905,10 +1904,9 @@ q8_status output_logits_f8(q8_ctx *ctx, const q8_readout_weights *ro, const q8_m
         else TRY(q8i_gemm_jobs(ctx, gj, 3, n));
         TRY(q8i_readout_combine(ctx, part[0], part[1], part[2], ro->b_t, R, n, t, 0, nullptr, nullptr, nullptr));
     }
-    TRY(q8i_quantize_f8(ctx, T, n, R, R, codes, tq.ld, scale, tq.lds));
     tq.data = codes;
     tq.scale = scale;
-    TRY(q8i_gemm_f8(ctx, W_out, &tq, b_out, lg, V));
+    TRY(q8i_gemm_f8(ctx, W_out, &tq, T, R, b_out, lg, V));
     if (k == 0) return Q8_OK;
     TRY(q8i_tile_stats(ctx, lg, n, V, pm, ps));
     return q8i_select_logits(ctx, pm, ps, lg, V, n, k, lse, topk_logp, topk_idx);

@@ -3,7 +3,6 @@
 #include "q8_internal.h"
 
 #include <math.h>
-#include <type_traits>
 
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v16f __attribute__((ext_vector_type(16)));
@@ -127,19 +126,24 @@ struct F8GemmArgs {
     float *Y;
     int rows, n, cols, ldw, ldx, ldsw, ldsx, ldy;
     int row_tiles, col_tiles;
-    int vec;                         // results in whole 16-byte pieces
+    unsigned magic, shift;
 };
 
 // The tile of a block.  Consecutive blocks run on different XCDs, each with an L2 cache of its own: each XCD gets a range of
 // the tiles in a row, and these go through eight row tiles for each column tile, so that the tiles that run on an XCD at one
-// time share rows and vectors.
-__device__ __forceinline__ void f8_tile_of(unsigned block, int row_tiles, int col_tiles, int &tr, int &tc)
+// time share rows and vectors.  (magic, shift: division by 8 col_tiles, see launch_f8.)
+__device__ __forceinline__ void f8_tile_of(const F8GemmArgs &a, int &tr, int &tc)
 {
-    const unsigned total = gridDim.x, per = total / 8, over = total % 8, xcd = block % 8, idx = block / 8;
-    const unsigned t = xcd * per + min(xcd, over) + idx;
-    const unsigned band = t / (8u * (unsigned)col_tiles), in = t - band * 8u * (unsigned)col_tiles, height = min(8u, (unsigned)row_tiles - 8u * band);
-    tc = (int)(in / height);
-    tr = (int)(8u * band + in % height);
+    const unsigned block = blockIdx.x, total = gridDim.x, per = total / 8, over = total % 8, xcd = block % 8, idx = block / 8;
+    const unsigned t = xcd * per + min(xcd, over) + idx, wide = 8u * (unsigned)a.col_tiles;
+    const unsigned band = (unsigned)(((unsigned long long)t * a.magic) >> 32) >> a.shift, in = t - band * wide, height = (unsigned)a.row_tiles - 8u * band;
+    if (height >= 8u) {
+        tc = (int)(in >> 3);
+        tr = (int)(8u * band + (in & 7u));
+    } else {
+        tc = (int)(in / height);
+        tr = (int)(8u * band + in % height);
+    }
 }
 
 // Sixteen codes times their block's scale as bf16, exactly: an e4m3 value has 4 significant bits, and the scale is a power of two.
@@ -155,10 +159,8 @@ __device__ __forceinline__ void f8_expand(v4i c, float s, v8bf &lo, v8bf &hi)
 }
 
 // Where a row's 16-byte pieces of a stage of 128 columns lie in LDS: exchanged by this number, so that the eight lanes that read
-// together (rows 0-3 and 16-19 of a group of 32, or 4-7 and 20-23, ...) find theirs on different banks.
-__device__ __forceinline__ int f8_twist(int row) { return (row & 3) | ((row >> 2) & 4); }
-// The row of a group of 32 that lane i multiplies: then lane (i, h) ends up with the results of 16 rows in a row, 16 h ...
-__device__ __forceinline__ int f8_row(int i) { return 16 * ((i >> 2) & 1) + 4 * (i >> 3) + (i & 3); }
+// together (eight rows) find theirs on different banks.
+__device__ __forceinline__ int f8_twist(int row) { return row & 7; }
 
 // Sixteen bytes a lane from memory to LDS at `at` + 16 lane (a wave's address), without passing through registers.
 __device__ __forceinline__ void f8_to_lds(__amdgpu_buffer_rsrc_t rsrc, uint8_t *at, unsigned offset, int step)
@@ -175,17 +177,20 @@ __device__ __forceinline__ void f8_to_lds(__amdgpu_buffer_rsrc_t rsrc, uint8_t *
 // codes 1e-5 of the result in the 2-norm, bf16 3e-8).  They are converted on their way from LDS to the matrix cores: two codes
 // an instruction, which the matrix cores' time covers (24 conversions beside 8 products of 32 x 32 x 16).  The order of k
 // inside a block is the same for both operands, which is all that it has to be: lane half h takes the 16-byte pieces 2 j + h.
-template <int WM, int WN, int TM, int TN>
-__global__ __launch_bounds__(64 * WM * WN) void f8_gemm_kernel(F8GemmArgs a)
+// KS > 1: KS such groups of waves take turns at the stages; their sums meet in LDS, in one order.
+template <int WM, int WN, int TM, int TN, int KS>
+__global__ __launch_bounds__(64 * WM * WN * KS) void f8_gemm_kernel(F8GemmArgs a)
 {
     constexpr int ROWS = 32 * WM * TM, VECS = 32 * WN * TN, THREADS = 64 * WM * WN, STAGE = (ROWS + VECS) * F8_BLOCK;
     constexpr int LW = ROWS * 8 / THREADS, LX = VECS * 8 / THREADS;                    // 16-byte pieces a thread requests
     static_assert(ROWS * 8 % THREADS == 0 && VECS * 8 % THREADS == 0, "even shares of a stage");
-    extern __shared__ __align__(16) uint8_t s_f8[];                                    // [2][STAGE]
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave % WM, wn = wave / WM, i = lane & 31, h = lane >> 5;
+    extern __shared__ __align__(16) uint8_t s_all[];                                   // [KS][2][STAGE]
+    const int group = KS > 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x / THREADS) : 0, tid = (int)threadIdx.x - group * THREADS;
+    uint8_t *s_f8 = s_all + group * 2 * STAGE;
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave % WM, wn = wave / WM, i = lane & 31, h = lane >> 5;
     int tr, tc;
-    f8_tile_of(blockIdx.x, a.row_tiles, a.col_tiles, tr, tc);
-    const int r0 = tr * ROWS, c0 = tc * VECS, steps = (a.cols + F8_BLOCK - 1) / F8_BLOCK, kend = (a.cols + 15) & ~15;
+    f8_tile_of(a, tr, tc);
+    const int r0 = tr * ROWS, c0 = tc * VECS, steps = (a.cols + F8_BLOCK - 1) / F8_BLOCK, turns = (steps + KS - 1) / KS, kend = (a.cols + 15) & ~15;
     const int left_r = min(ROWS, a.rows - r0), left_c = min(VECS, a.n - c0);
     const __amdgpu_buffer_rsrc_t rw = q8_rsrc(a.W + (size_t)r0 * a.ldw, (size_t)left_r * a.ldw), rx = q8_rsrc(a.X + (size_t)c0 * a.ldx, (size_t)left_c * a.ldx);
     // piece p of a stage: row p / 8 (beyond the matrix: the last row again), the columns that the twist puts at place p % 8
@@ -203,21 +208,30 @@ __global__ __launch_bounds__(64 * WM * WN) void f8_gemm_kernel(F8GemmArgs a)
     const int full = kend / F8_BLOCK;                                                  // stages that are all columns of the matrix
     auto request = [&](int step, int stage) {
         uint8_t *at = s_f8 + stage * STAGE + wave * 1024;
-        // (of the last one's pieces that lie past the columns, the row's first piece takes the place)
-        auto past = [&](int p) { return step >= full && step * F8_BLOCK + 16 * ((p & 7) ^ f8_twist(p >> 3)) >= kend ? 16u * (unsigned)((p & 7) ^ f8_twist(p >> 3)) + step * F8_BLOCK : 0u; };
+        if (step < full) {
 #pragma unroll
-        for (int u = 0; u < LW; ++u)
-            f8_to_lds(rw, at + u * THREADS * 16, ow[u] - past(u * THREADS + tid), step * F8_BLOCK);
+            for (int u = 0; u < LW; ++u) f8_to_lds(rw, at + u * THREADS * 16, ow[u], step * F8_BLOCK);
 #pragma unroll
-        for (int u = 0; u < LX; ++u)
-            f8_to_lds(rx, at + ROWS * F8_BLOCK + u * THREADS * 16, ox[u] - past(u * THREADS + tid), step * F8_BLOCK);
+            for (int u = 0; u < LX; ++u) f8_to_lds(rx, at + ROWS * F8_BLOCK + u * THREADS * 16, ox[u], step * F8_BLOCK);
+        } else {                                                            // pieces past the columns: the row's first in their place
+#pragma unroll
+            for (int u = 0; u < LW; ++u) {
+                const int p = u * THREADS + tid, c = 16 * ((p & 7) ^ f8_twist(p >> 3));
+                f8_to_lds(rw, at + u * THREADS * 16, step * F8_BLOCK + c < kend ? ow[u] + step * F8_BLOCK : ow[u] - c, 0);
+            }
+#pragma unroll
+            for (int u = 0; u < LX; ++u) {
+                const int p = u * THREADS + tid, c = 16 * ((p & 7) ^ f8_twist(p >> 3));
+                f8_to_lds(rx, at + ROWS * F8_BLOCK + u * THREADS * 16, step * F8_BLOCK + c < kend ? ox[u] + step * F8_BLOCK : ox[u] - c, 0);
+            }
+        }
     };
     // scales: four steps' bytes at a time
     const uint8_t *pw[TM], *px[TN];
 #pragma unroll
-    for (int t = 0; t < TM; ++t) pw[t] = a.sw + (size_t)min(r0 + 32 * (wm * TM + t) + f8_row(i), a.rows - 1) * a.ldsw;
+    for (int t = 0; t < TM; ++t) pw[t] = a.sw + (size_t)min(r0 + 32 * (wm * TM + t) + i, a.rows - 1) * a.ldsw;
 #pragma unroll
-    for (int t = 0; t < TN; ++t) px[t] = a.sx + (size_t)min(c0 + 32 * (wn * TN + t) + f8_row(i), a.n - 1) * a.ldsx;
+    for (int t = 0; t < TN; ++t) px[t] = a.sx + (size_t)min(c0 + 32 * (wn * TN + t) + i, a.n - 1) * a.ldsx;
     unsigned ew[TM], ex[TN];
     v16f acc[TM][TN];
 #pragma unroll
@@ -226,115 +240,298 @@ __global__ __launch_bounds__(64 * WM * WN) void f8_gemm_kernel(F8GemmArgs a)
         for (int u = 0; u < TN; ++u)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[t][u][e] = 0.0f;
-    const int lw = (32 * wm * TM + f8_row(i)) * F8_BLOCK, lx = ROWS * F8_BLOCK + (32 * wn * TN + f8_row(i)) * F8_BLOCK, twist = f8_twist(f8_row(i));
+    const int lw = (32 * wm * TM + i) * F8_BLOCK, lx = ROWS * F8_BLOCK + (32 * wn * TN + i) * F8_BLOCK, twist = f8_twist(i);
 
     auto scales = [&](int step) {
-        if ((step & 3) == 0) {
 #pragma unroll
-            for (int t = 0; t < TM; ++t) ew[t] = *(const unsigned *)(pw[t] + step);
+        for (int t = 0; t < TM; ++t) ew[t] = *(const unsigned *)(pw[t] + (step & ~3));
 #pragma unroll
-            for (int t = 0; t < TN; ++t) ex[t] = *(const unsigned *)(px[t] + step);
-        }
+        for (int t = 0; t < TN; ++t) ex[t] = *(const unsigned *)(px[t] + (step & ~3));
     };
-    auto multiply = [&](int step, auto cut) {
-        const uint8_t *st = s_f8 + (step & 1) * STAGE;
+    auto multiply = [&](int step, int stage) {
+        const uint8_t *pw = s_f8 + stage * STAGE + lw, *px = s_f8 + stage * STAGE + lx;
         float fw[TM], fx[TN];
 #pragma unroll
         for (int t = 0; t < TM; ++t) fw[t] = __uint_as_float(((ew[t] >> (8 * (step & 3))) & 255u) << 23);
 #pragma unroll
         for (int t = 0; t < TN; ++t) fx[t] = __uint_as_float(((ex[t] >> (8 * (step & 3))) & 255u) << 23);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            v4i w[TM], x[TN];
+        v4i w[2][TM], x[2][TN];                                             // the next 32 columns are on their way while these are multiplied
+        auto load = [&](int j) {
             const int piece = 16 * ((2 * j + h) ^ twist);
 #pragma unroll
-            for (int t = 0; t < TM; ++t) w[t] = *(const v4i *)(st + lw + t * 32 * F8_BLOCK + piece);
+            for (int t = 0; t < TN; ++t) x[j & 1][t] = *(const v4i *)(px + t * 32 * F8_BLOCK + piece);
 #pragma unroll
-            for (int t = 0; t < TN; ++t) x[t] = *(const v4i *)(st + lx + t * 32 * F8_BLOCK + piece);
-            if constexpr (decltype(cut)::value) {                           // what lies past the columns counts as zeros
-                const int keep = step * F8_BLOCK + 16 * (2 * j + h) < kend ? -1 : 0;
+            for (int t = 0; t < TM; ++t) w[j & 1][t] = *(const v4i *)(pw + t * 32 * F8_BLOCK + piece);
+        };
+        load(0);
 #pragma unroll
-                for (int t = 0; t < TM; ++t) w[t] &= keep;
-#pragma unroll
-                for (int t = 0; t < TN; ++t) x[t] &= keep;
-            }
+        for (int j = 0; j < 4; ++j) {
+            if (j < 3) load(j + 1);
+            __builtin_amdgcn_sched_barrier(0);
             v8bf xl[TN], xh[TN];
 #pragma unroll
-            for (int t = 0; t < TN; ++t) f8_expand(x[t], fx[t], xl[t], xh[t]);
+            for (int t = 0; t < TN; ++t) f8_expand(x[j & 1][t], fx[t], xl[t], xh[t]);
 #pragma unroll
             for (int t = 0; t < TM; ++t) {
                 v8bf wl, wh;
-                f8_expand(w[t], fw[t], wl, wh);
+                f8_expand(w[j & 1][t], fw[t], wl, wh);
 #pragma unroll
-                for (int u = 0; u < TN; ++u) acc[t][u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wl, xl[u], acc[t][u], 0, 0, 0);
+                for (int u = 0; u < TN; ++u) acc[t][u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xl[u], wl, acc[t][u], 0, 0, 0);
 #pragma unroll
-                for (int u = 0; u < TN; ++u) acc[t][u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(wh, xh[u], acc[t][u], 0, 0, 0);
+                for (int u = 0; u < TN; ++u) acc[t][u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(xh[u], wh, acc[t][u], 0, 0, 0);
             }
         }
     };
-    request(0, 0);
-    for (int step = 0; step < full; ++step) {
-        scales(step);
-        __syncthreads();                                                    // this step's stage is there, the other one is free
-        if (step + 1 < steps) request(step + 1, (step + 1) & 1);
-        multiply(step, std::false_type());
+    if (group < steps) request(group, 0);
+#pragma unroll 1
+    for (int turn = 0; turn < turns; ++turn) {
+        const int step = turn * KS + group;
+        if ((KS > 1 || (step & 3) == 0) && step < steps) scales(step);
+        __syncthreads();                                                    // this turn's stages are there, the other ones are free
+        if (step + KS < steps) request(step + KS, (turn + 1) & 1);
+        if (turn == turns - 1 && full < steps) {                            // what lies past the columns counts as zeros
+            if (step == full) {
+#pragma unroll
+                for (int u = 0; u < LW + LX; ++u) {
+                    const int p = u * THREADS + tid;
+                    if (step * F8_BLOCK + 16 * ((p & 7) ^ f8_twist(p >> 3)) >= kend) *(v4i *)(s_f8 + (turn & 1) * STAGE + 16 * p) = (v4i){0, 0, 0, 0};
+                }
+            }
+            __syncthreads();
+        }
+        if (step < steps) multiply(step, turn & 1);
     }
-    if (full < steps) {
-        scales(full);
+    if constexpr (KS > 1) {
+        // the groups' sums, one group's place per stage buffer: [wave][t][u][e][lane]
+        static_assert(STAGE * 2 >= TM * TN * 16 * THREADS * 4, "a group's sums fit where its stages were");
         __syncthreads();
-        multiply(full, std::true_type());
+        float *mine = (float *)s_f8 + wave * TM * TN * 1024 + lane;
+        if (group > 0) {
+#pragma unroll
+            for (int t = 0; t < TM; ++t)
+#pragma unroll
+                for (int u = 0; u < TN; ++u)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) mine[((t * TN + u) * 16 + e) * 64] = acc[t][u][e];
+        }
+        __syncthreads();
+        if (group > 0) return;
+#pragma unroll
+        for (int g = 1; g < KS; ++g) {
+            const float *o = (const float *)(s_all + g * 2 * STAGE) + wave * TM * TN * 1024 + lane;
+#pragma unroll
+            for (int t = 0; t < TM; ++t)
+#pragma unroll
+                for (int u = 0; u < TN; ++u)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) acc[t][u][e] += o[((t * TN + u) * 16 + e) * 64];
+        }
     }
-    // lane (i, h): rows 16 h + (0 .. 15) of each group, vector f8_row(i)
+    // lane (i, h): row i of each group, vectors 8 q + 4 h + (0 .. 3): 128 contiguous bytes of a vector a half wave
 #pragma unroll
     for (int t = 0; t < TM; ++t) {
-        const int row = r0 + 32 * (wm * TM + t) + 16 * h;
-        float b[16];
-#pragma unroll
-        for (int e = 0; e < 16; ++e) b[e] = a.bias && row + e < a.rows ? a.bias[row + e] : 0.0f;
+        const int row = r0 + 32 * (wm * TM + t) + i;
+        if (row >= a.rows) continue;
+        const float b = a.bias ? a.bias[row] : 0.0f;
 #pragma unroll
         for (int u = 0; u < TN; ++u) {
-            const int vec = c0 + 32 * (wn * TN + u) + f8_row(i);
-            if (vec >= a.n) continue;
+            const int vec = c0 + 32 * (wn * TN + u) + 4 * h;
             float *out = a.Y + (size_t)vec * a.ldy + row;
-            const bool plain = !a.bias;                                     // (y + 0 would turn -0 into 0)
-            if (a.vec && row + 15 < a.rows) {
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    float4 y = make_float4(acc[t][u][4 * q], acc[t][u][4 * q + 1], acc[t][u][4 * q + 2], acc[t][u][4 * q + 3]);
-                    if (!plain) y = make_float4(y.x + b[4 * q], y.y + b[4 * q + 1], y.z + b[4 * q + 2], y.w + b[4 * q + 3]);
-                    *(float4 *)(out + 4 * q) = y;
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if (row + e < a.rows) out[e] = plain ? acc[t][u][e] : acc[t][u][e] + b[e];
+            for (int e = 0; e < 16; ++e) {
+                const int v = 8 * (e >> 2) + (e & 3);
+                if (vec + v < a.n) __builtin_nontemporal_store(a.bias ? acc[t][u][e] + b : acc[t][u][e], &out[(size_t)v * a.ldy]);      // (y + 0 would turn -0 into 0)
             }
         }
     }
 }
 
-template <int WM, int WN, int TM, int TN> static q8_status launch_f8(q8_ctx *ctx, F8GemmArgs &a)
+template <int WM, int WN, int TM, int TN, int KS = 1> static q8_status launch_f8(q8_ctx *ctx, F8GemmArgs &a)
 {
     static Q8OncePerDevice once;
-    const size_t smem = (size_t)2 * 32 * (WM * TM + WN * TN) * F8_BLOCK;
+    const size_t smem = (size_t)KS * 2 * 32 * (WM * TM + WN * TN) * F8_BLOCK;
     a.row_tiles = (a.rows + 32 * WM * TM - 1) / (32 * WM * TM);
     a.col_tiles = (a.n + 32 * WN * TN - 1) / (32 * WN * TN);
     const size_t tiles = (size_t)a.row_tiles * a.col_tiles;
+    // t / d for t < 2^31 as (t magic / 2^32) / 2^shift: magic = ceil(2^(32 + shift) / d) with 2^shift < d <= 2^(shift + 1) is below 2^32, and
+    // its excess over the quotient, less than 1, adds less than t / 2^(32 + shift) < 1 / d
+    const unsigned long long d = 8ull * a.col_tiles;
+    for (a.shift = 0; (2ull << a.shift) < d; ++a.shift) {}
+    a.magic = (unsigned)(((1ull << (32 + a.shift)) + d - 1) / d);
     if (tiles > 0x7fffffffu) return q8_fail(ctx, Q8_ERR_SHAPE, "f8 product: %d x %d results are too many for a launch", a.rows, a.n);
-    const q8_status st = q8i_lds(ctx, once, (const void *)f8_gemm_kernel<WM, WN, TM, TN>, smem, "f8 product");
+    const q8_status st = q8i_lds(ctx, once, (const void *)f8_gemm_kernel<WM, WN, TM, TN, KS>, smem, "f8 product");
     if (st) return st;
-    hipLaunchKernelGGL((f8_gemm_kernel<WM, WN, TM, TN>), dim3((unsigned)tiles), dim3(64 * WM * WN), smem, ctx->stream, a);
+    hipLaunchKernelGGL((f8_gemm_kernel<WM, WN, TM, TN, KS>), dim3((unsigned)tiles), dim3(64 * WM * WN * KS), smem, ctx->stream, a);
     return q8i_launch_check(ctx, "product f8");
 }
 
-q8_status q8i_gemm_f8(q8_ctx *ctx, const q8_mat_f8 *W, const q8_mat_f8 *X, const float *bias, float *Y, int ldy)
+// Tiles by what each costs (us; rows x columns x vectors): 256 x 256 where they are about one round or more and long enough that
+// reading counts most (8192 x 8192 x 8192 917 against 1061 in 128 x 64, 4096 x 1024 x 4096 45.5 against 50.9; 50000 x 512 x 1024, four
+// stages a tile, 114 against 82); 128 x 32 for up to 32 vectors; 128 x 96 for 65 to 96 (63644 x 620 x 77 20.1 against 25.5 in 64 x 64 and
+// 28.5 in 128 x 64); 64 x 32 with four groups in turns at the stages where 64 x 64 would leave compute units without any (1024 x 8192 x
+// 64 22.9 against 35.1, 512 x 4096 x 17 10.2 against 17.2); else 128 x 64 where these are two rounds (50000 x 640 x 320 35.1 against 39.0),
+// and 64 x 64 (50000 x 512 x 64 9.4 against 11.0, 1024 x 2048 x 1024 12.6 against 17.1).
+static q8_status gemm_f8_tiles(q8_ctx *ctx, F8GemmArgs &a)
 {
-    F8GemmArgs a = {W->data, X->data, W->scale, X->scale, bias, Y, W->rows, X->rows, W->cols, W->ld, X->ld, W->lds, X->lds, ldy, 0, 0, 0};
-    a.vec = ldy % 4 == 0 && ((uintptr_t)Y & 15) == 0;
-    const size_t big = (size_t)((a.rows + 255) / 256) * ((a.n + 255) / 256);
-    if (big >= 200 && a.cols > 1024) return launch_f8<2, 4, 4, 2>(ctx, a);
-    if (a.n <= 64) return launch_f8<4, 1, 1, 2>(ctx, a);
-    return launch_f8<2, 2, 2, 2>(ctx, a);
+    auto tiles = [&](int r, int v) { return (long long)((a.rows + r - 1) / r) * ((a.n + v - 1) / v); };
+    if (tiles(256, 256) >= 200 && a.cols >= 1024) return launch_f8<2, 4, 4, 2>(ctx, a);
+    if (tiles(64, 64) < 128 && a.cols >= 512) return launch_f8<2, 1, 1, 1, 4>(ctx, a);
+    if (a.n <= 32) return launch_f8<4, 1, 1, 1>(ctx, a);
+    if (a.n > 64 && a.n <= 96 && tiles(128, 96) >= 128) return launch_f8<4, 1, 1, 3>(ctx, a);
+    if (tiles(128, 64) >= 512) return launch_f8<2, 2, 2, 1>(ctx, a);
+    return launch_f8<2, 2, 1, 1>(ctx, a);
+}
+
+// ------------------------------------------------------------------------- few vectors ----
+
+struct F8StreamArgs {
+    F8GemmArgs g;
+    const float *Xf;                 // the vectors in fp32 [n x ldxf], quantized here; or NULL: g.X, g.sx
+    int ldxf, vec;                   // vec: the vectors begin at 16-byte boundaries
+    int nb, pitch;                   // blocks of 128 columns; bytes of a vector in LDS
+};
+
+// Up to 16 vectors: the weights go from memory to registers once, requested before anything is waited for; the vectors lie in LDS as
+// bf16 values, put there by every block for itself.  A wave multiplies 16 rows; KS waves share them, each with its range of the
+// columns.  Lane (i, g) has row i and of every 128 columns the 16-byte pieces g and g + 4.
+template <int KS>
+__global__ __launch_bounds__(256) void f8_stream_kernel(F8StreamArgs a)
+{
+    extern __shared__ __align__(16) uint8_t s_x[];                          // [n][pitch], then the waves' sums
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, g = lane >> 4;
+    const F8GemmArgs &m = a.g;
+    const int tile = (int)blockIdx.x * (4 / KS) + wave / KS, r0 = tile * 16, kend = (m.cols + 15) & ~15, n = m.n;
+    const int span = (a.nb + KS - 1) / KS, b0 = wave % KS * span, b1 = min(b0 + span, a.nb);
+    const bool have = r0 < m.rows;
+    const int left = have ? min(16, m.rows - r0) : 1;
+    const __amdgpu_buffer_rsrc_t rw = q8_rsrc(m.W + (size_t)(have ? r0 : 0) * m.ldw, (size_t)left * m.ldw), rs = q8_rsrc(m.sw + (size_t)(have ? r0 : 0) * m.ldsw, (size_t)left * m.ldsw);
+    const unsigned row_at = have && i < left ? (unsigned)i * (unsigned)m.ldw : Q8_OOB, scale_at = have && i < left ? (unsigned)i * (unsigned)m.ldsw : Q8_OOB;
+    v4i w[8];
+    unsigned e[4];
+    auto request = [&](int b) {                                             // four blocks of columns (past the matrix: zeros, no access)
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+            const int k = (b + (s >> 1)) * F8_BLOCK + 64 * (s & 1) + 16 * g;
+            w[s] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(rw, (int)(b + (s >> 1) < b1 && k < kend && row_at != Q8_OOB ? row_at + k : Q8_OOB), 0, 0));
+        }
+#pragma unroll
+        for (int s = 0; s < 4; ++s) e[s] = __builtin_amdgcn_raw_buffer_load_b8(rs, (int)(b + s < b1 && scale_at != Q8_OOB ? scale_at + b + s : Q8_OOB), 0, 0);
+    };
+    request(b0);
+    const float bias = m.bias && have && i < left ? m.bias[r0 + i] : 0.0f;
+
+    // ---- the vectors, a half wave per block of 128 columns, four values a lane
+    const int half = tid >> 5, q = lane & 31, units = n * a.nb;
+    for (int u0 = half; u0 < units; u0 += 32) {
+        float4 v[4];
+        unsigned c[4], se[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int u = u0 + 8 * t, j = u / a.nb, k = (u - j * a.nb) * F8_BLOCK + 4 * q;
+            v[t] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            c[t] = 0;
+            se[t] = 127;
+            if (u >= units) continue;
+            if (a.Xf) {
+                const float *x = a.Xf + (size_t)j * a.ldxf + k;
+                if (k + 3 < m.cols) {
+                    if (a.vec) v[t] = *(const float4 *)x;
+                    else v[t] = make_float4(x[0], x[1], x[2], x[3]);
+                } else {
+                    if (k < m.cols) v[t].x = x[0];
+                    if (k + 1 < m.cols) v[t].y = x[1];
+                    if (k + 2 < m.cols) v[t].z = x[2];
+                }
+            } else {
+                if (k < kend) c[t] = *(const unsigned *)(m.X + (size_t)j * m.ldx + k);
+                se[t] = m.sx[(size_t)j * m.ldsx + u - j * a.nb];
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int u = u0 + 8 * t, j = u / a.nb, k = (u - j * a.nb) * F8_BLOCK + 4 * q;
+            if (a.Xf) {
+                const float top = f8_half_max(fmaxf(fmaxf(f8_finite_abs(v[t].x), f8_finite_abs(v[t].y)), fmaxf(f8_finite_abs(v[t].z), f8_finite_abs(v[t].w))));
+                float inv;
+                se[t] = f8_scale_of(top, inv);
+                c[t] = f8_codes4(v[t], inv);
+            }
+            if (u >= units) continue;
+            const float s = __uint_as_float(se[t] << 23);
+            union { v2bf h[2]; unsigned long long d; } p;
+            p.h[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[t], s, false);
+            p.h[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[t], s, true);
+            *(unsigned long long *)(s_x + (size_t)j * a.pitch + 2 * k) = p.d;
+        }
+    }
+    __syncthreads();
+
+    v4f acc[2];                                                             // two chains: a dependent matrix operation waits longer
+    acc[0] = acc[1] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
+    const v8bf none = {};
+    for (int b = b0; b < b1; b += 4) {
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+            v8bf wl, wh, xl = none, xh = none;
+            f8_expand(w[s], __uint_as_float(e[s >> 1] << 23), wl, wh);
+            if (i < n && b + (s >> 1) < b1) {
+                const uint8_t *x = s_x + (size_t)i * a.pitch + 2 * ((b + (s >> 1)) * F8_BLOCK + 64 * (s & 1) + 16 * g);
+                xl = *(const v8bf *)x;
+                xh = *(const v8bf *)(x + 16);
+            }
+            acc[s & 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xl, wl, acc[s & 1], 0, 0, 0);
+            acc[s & 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xh, wh, acc[s & 1], 0, 0, 0);
+        }
+        if (b + 4 < b1) request(b + 4);
+    }
+    v4f sum = acc[0] + acc[1];
+    if constexpr (KS > 1) {                                                 // the ranges' sums, in one order
+        v4f *s_sum = (v4f *)(s_x + (size_t)n * a.pitch);                    // [4][64]
+        s_sum[wave * 64 + lane] = sum;
+        __syncthreads();
+        if (wave % KS) return;
+#pragma unroll
+        for (int k = 1; k < KS; ++k) sum += s_sum[(wave + k) * 64 + lane];
+    }
+    // lane (i, g): row i, vectors 4 g + (0 .. 3)
+    if (!have || i >= left) return;
+#pragma unroll
+    for (int v = 0; v < 4; ++v)
+        if (4 * g + v < n) m.Y[(size_t)(4 * g + v) * m.ldy + r0 + i] = m.bias ? sum[v] + bias : sum[v];
+}
+
+template <int KS> static q8_status launch_stream(q8_ctx *ctx, const F8StreamArgs &a)
+{
+    const int tiles = (a.g.rows + 15) / 16, per = 4 / KS;
+    hipLaunchKernelGGL(f8_stream_kernel<KS>, dim3((tiles + per - 1) / per), dim3(256), (size_t)a.g.n * a.pitch + (KS > 1 ? 4096 : 0), ctx->stream, a);
+    return q8i_launch_check(ctx, "product f8");
+}
+
+static bool gemm_f8_streams(int n, int cols) { return n <= 16 && (size_t)n * (((cols + F8_BLOCK - 1) / F8_BLOCK) * 2 * F8_BLOCK + 16) <= 61440; }
+
+// X in codes, or Xf [n x ldxf] in fp32 with X the room for its codes (rows, cols, ld, lds and memory), used where they are needed.
+q8_status q8i_gemm_f8(q8_ctx *ctx, const q8_mat_f8 *W, const q8_mat_f8 *X, const float *Xf, int ldxf, const float *bias, float *Y, int ldy)
+{
+    F8GemmArgs a = {W->data, X->data, W->scale, X->scale, bias, Y, W->rows, X->rows, W->cols, W->ld, X->ld, W->lds, X->lds, ldy, 0, 0, 0, 0};
+    const bool streams = gemm_f8_streams(a.n, a.cols);
+    // (results over the vectors: these are quantized first, as a whole)
+    const char *x0 = (const char *)Xf, *x1 = (const char *)(Xf + (size_t)(a.n - 1) * ldxf + a.cols), *y0 = (const char *)Y, *y1 = (const char *)(Y + (size_t)(a.n - 1) * ldy + a.rows);
+    if (Xf && (!streams || (x0 < y1 && y0 < x1))) {
+        const q8_status st = q8i_quantize_f8(ctx, Xf, a.n, a.cols, ldxf, (uint8_t *)X->data, X->ld, (uint8_t *)X->scale, X->lds);
+        if (st) return st;
+        Xf = nullptr;
+    }
+    if (streams) {
+        F8StreamArgs s = {a, Xf, ldxf, 0, (a.cols + F8_BLOCK - 1) / F8_BLOCK, 0};
+        s.vec = ldxf % 4 == 0 && ((uintptr_t)Xf & 15) == 0;
+        s.pitch = s.nb * 2 * F8_BLOCK + 16;
+        // the columns in parts where the rows alone make few waves
+        const int tiles = (a.rows + 15) / 16;
+        if (tiles <= 512 && s.nb >= 4) return launch_stream<4>(ctx, s);
+        if (tiles <= 1024 && s.nb >= 2) return launch_stream<2>(ctx, s);
+        return launch_stream<1>(ctx, s);
+    }
+    return gemm_f8_tiles(ctx, a);
 }
 
 // ------------------------------------------------------------ statistics of the logits' tiles ----

@@ -345,7 +345,8 @@ q8_status q8i_select_logits(q8_ctx *ctx, const float *part_max, const double *pa
                             int k, float *lse, float *topk_logp, int32_t *topk_idx);
 // 8-bit floating point with a scale per block of 128 columns
 q8_status q8i_quantize_f8(q8_ctx *ctx, const float *X, int rows, int cols, int ldx, uint8_t *codes, int ld, uint8_t *scale, int lds);
-q8_status q8i_gemm_f8(q8_ctx *ctx, const q8_mat_f8 *W, const q8_mat_f8 *X, const float *bias, float *Y, int ldy);
+// X in codes, or Xf in fp32 with X the room for its codes
+q8_status q8i_gemm_f8(q8_ctx *ctx, const q8_mat_f8 *W, const q8_mat_f8 *X, const float *Xf, int ldxf, const float *bias, float *Y, int ldy);
 q8_status q8i_tile_stats(q8_ctx *ctx, const float *logits, int n, int V, float *part_max, double *part_sum);
 q8_status q8i_sample(q8_ctx *ctx, const float *logits, int n, int V, int ldl, const q8_sampling *s, const float *u, int32_t *tokens, float *logp,
                      const float *E_tgt, int E, float *y_emb, void *state);

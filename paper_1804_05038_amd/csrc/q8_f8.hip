@@ -389,45 +389,52 @@ struct F8StreamArgs {
     const float *Xf;                 // the vectors in fp32 [n x ldxf], quantized here; or NULL: g.X, g.sx
     int ldxf, vec;                   // vec: the vectors begin at 16-byte boundaries
     int nb, pitch;                   // blocks of 128 columns; bytes of a vector in LDS
+    int split, span;                 // waves for a row's columns, blocks of columns of each
 };
 
-// Up to 16 vectors: the weights go from memory to registers once, requested before anything is waited for; the vectors lie in LDS as
-// bf16 values, put there by every block for itself.  A wave multiplies 16 rows; KS waves share them, each with its range of the
-// columns.  Lane (i, g) has row i and of every 128 columns the 16-byte pieces g and g + 4.
-template <int KS>
-__global__ __launch_bounds__(256) void f8_stream_kernel(F8StreamArgs a)
+// Up to 16 vectors: the weights go from memory to registers once, requested before anything else is waited for and again as
+// soon as a register is free; the vectors lie in LDS as bf16 values, put there by every block for itself.  A wave multiplies 16
+// rows at a time; `split` waves share them, each with its range of the columns.  Lane (i, g) has row i and of every 128 columns
+// the 16-byte pieces g and g + 4.
+__global__ __launch_bounds__(512) void f8_stream_kernel(F8StreamArgs a)
 {
-    extern __shared__ __align__(16) uint8_t s_x[];                          // [n][pitch], then the waves' sums
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, g = lane >> 4;
+    extern __shared__ __align__(16) uint8_t s_x[];                          // [n][pitch], then the waves' sums [waves][64]
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6, i = lane & 15, g = lane >> 4;
     const F8GemmArgs &m = a.g;
-    const int tile = (int)blockIdx.x * (4 / KS) + wave / KS, r0 = tile * 16, kend = (m.cols + 15) & ~15, n = m.n;
-    const int span = (a.nb + KS - 1) / KS, b0 = wave % KS * span, b1 = min(b0 + span, a.nb);
-    const bool have = r0 < m.rows;
-    const int left = have ? min(16, m.rows - r0) : 1;
-    const __amdgpu_buffer_rsrc_t rw = q8_rsrc(m.W + (size_t)(have ? r0 : 0) * m.ldw, (size_t)left * m.ldw), rs = q8_rsrc(m.sw + (size_t)(have ? r0 : 0) * m.ldsw, (size_t)left * m.ldsw);
-    const unsigned row_at = have && i < left ? (unsigned)i * (unsigned)m.ldw : Q8_OOB, scale_at = have && i < left ? (unsigned)i * (unsigned)m.ldsw : Q8_OOB;
-    v4i w[8];
-    unsigned e[4];
-    auto request = [&](int b) {                                             // four blocks of columns (past the matrix: zeros, no access)
-#pragma unroll
-        for (int s = 0; s < 8; ++s) {
-            const int k = (b + (s >> 1)) * F8_BLOCK + 64 * (s & 1) + 16 * g;
-            w[s] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(rw, (int)(b + (s >> 1) < b1 && k < kend && row_at != Q8_OOB ? row_at + k : Q8_OOB), 0, 0));
-        }
-#pragma unroll
-        for (int s = 0; s < 4; ++s) e[s] = __builtin_amdgcn_raw_buffer_load_b8(rs, (int)(b + s < b1 && scale_at != Q8_OOB ? scale_at + b + s : Q8_OOB), 0, 0);
+    const int split = a.split, part = wave & (split - 1), tiles = (m.rows + 15) >> 4, per = waves / split, stride = gridDim.x * per;
+    const int kend = (m.cols + 15) & ~15, n = m.n, b0 = part * a.span, b1 = min(b0 + a.span, a.nb);
+    int tile = blockIdx.x + gridDim.x * (wave / split), b = b0;
+    __amdgpu_buffer_rsrc_t rw, rs;
+    unsigned row_at, scale_at;
+    float bias;
+    auto rows_of = [&](int t) {                                             // no rows: every access past the end
+        const int r0 = 16 * min(t, tiles - 1), left = t < tiles && b0 < b1 ? min(16, m.rows - r0) : 0;
+        rw = q8_rsrc(m.W + (size_t)r0 * m.ldw, (size_t)left * m.ldw);
+        rs = q8_rsrc(m.sw + (size_t)r0 * m.ldsw, (size_t)left * m.ldsw);
+        row_at = i < left ? (unsigned)i * (unsigned)m.ldw + 16 * g : Q8_OOB;
+        scale_at = i < left ? (unsigned)i * (unsigned)m.ldsw : Q8_OOB;
+        bias = m.bias && i < left ? m.bias[r0 + i] : 0.0f;
     };
-    request(b0);
-    const float bias = m.bias && have && i < left ? m.bias[r0 + i] : 0.0f;
+    v4i w[8];
+    unsigned e;
+    auto codes = [&](int s) {                                               // four blocks of columns, 64 columns each time
+        const int k = (b + (s >> 1)) * F8_BLOCK + 64 * (s & 1);
+        return __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(rw, (int)(b + (s >> 1) < b1 && k + 16 * g < kend && row_at != Q8_OOB ? row_at + k : Q8_OOB), 0, 0));
+    };
+    auto scale = [&] { return __builtin_amdgcn_raw_buffer_load_b32(rs, (int)(scale_at == Q8_OOB ? Q8_OOB : scale_at + b), 0, 0); };
+    rows_of(tile);
+#pragma unroll
+    for (int s = 0; s < 8; ++s) w[s] = codes(s);
+    e = scale();
 
     // ---- the vectors, a half wave per block of 128 columns, four values a lane
-    const int half = tid >> 5, q = lane & 31, units = n * a.nb;
-    for (int u0 = half; u0 < units; u0 += 32) {
-        float4 v[4];
-        unsigned c[4], se[4];
+    const int q = lane & 31, units = n * a.nb, halves = 2 * waves;
+    for (int u0 = tid >> 5; u0 < units; u0 += 2 * halves) {
+        float4 v[2];
+        unsigned c[2], se[2];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int u = u0 + 8 * t, j = u / a.nb, k = (u - j * a.nb) * F8_BLOCK + 4 * q;
+        for (int t = 0; t < 2; ++t) {
+            const int u = u0 + halves * t, j = u / a.nb, k = (u - j * a.nb) * F8_BLOCK + 4 * q;
             v[t] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             c[t] = 0;
             se[t] = 127;
@@ -448,15 +455,15 @@ __global__ __launch_bounds__(256) void f8_stream_kernel(F8StreamArgs a)
             }
         }
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int u = u0 + 8 * t, j = u / a.nb, k = (u - j * a.nb) * F8_BLOCK + 4 * q;
+        for (int t = 0; t < 2; ++t) {
+            const int u = u0 + halves * t, j = u / a.nb, k = (u - j * a.nb) * F8_BLOCK + 4 * q;
+            if (u >= units) continue;                                       // (a half wave as one)
             if (a.Xf) {
                 const float top = f8_half_max(fmaxf(fmaxf(f8_finite_abs(v[t].x), f8_finite_abs(v[t].y)), fmaxf(f8_finite_abs(v[t].z), f8_finite_abs(v[t].w))));
                 float inv;
                 se[t] = f8_scale_of(top, inv);
                 c[t] = f8_codes4(v[t], inv);
             }
-            if (u >= units) continue;
             const float s = __uint_as_float(se[t] << 23);
             union { v2bf h[2]; unsigned long long d; } p;
             p.h[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[t], s, false);
@@ -466,54 +473,81 @@ __global__ __launch_bounds__(256) void f8_stream_kernel(F8StreamArgs a)
     }
     __syncthreads();
 
+    v4f *s_sum = (v4f *)(s_x + (size_t)n * a.pitch);
     v4f acc[2];                                                             // two chains: a dependent matrix operation waits longer
     acc[0] = acc[1] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
     const v8bf none = {};
-    for (int b = b0; b < b1; b += 4) {
+    const uint8_t *px = s_x + (size_t)min(i, n - 1) * a.pitch + 32 * g;
+    while (tile < tiles) {
+        const int at = b, from = tile;
+        const unsigned es = e;
+        const float add = bias;
+        b += 4;
+        const bool last = b >= b1;
+        if (last) {
+            b = b0;
+            tile += stride;
+            rows_of(tile);
+        }
+        e = scale();
 #pragma unroll
         for (int s = 0; s < 8; ++s) {
             v8bf wl, wh, xl = none, xh = none;
-            f8_expand(w[s], __uint_as_float(e[s >> 1] << 23), wl, wh);
-            if (i < n && b + (s >> 1) < b1) {
-                const uint8_t *x = s_x + (size_t)i * a.pitch + 2 * ((b + (s >> 1)) * F8_BLOCK + 64 * (s & 1) + 16 * g);
+            f8_expand(w[s], __uint_as_float(((es >> (8 * (s >> 1))) & 255u) << 23), wl, wh);
+            w[s] = codes(s);
+            if (i < n && at + (s >> 1) < b1) {
+                const uint8_t *x = px + 2 * (at * F8_BLOCK + 64 * s);
                 xl = *(const v8bf *)x;
                 xh = *(const v8bf *)(x + 16);
             }
             acc[s & 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xl, wl, acc[s & 1], 0, 0, 0);
             acc[s & 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xh, wh, acc[s & 1], 0, 0, 0);
         }
-        if (b + 4 < b1) request(b + 4);
-    }
-    v4f sum = acc[0] + acc[1];
-    if constexpr (KS > 1) {                                                 // the ranges' sums, in one order
-        v4f *s_sum = (v4f *)(s_x + (size_t)n * a.pitch);                    // [4][64]
-        s_sum[wave * 64 + lane] = sum;
-        __syncthreads();
-        if (wave % KS) return;
+        if (!last) continue;
+        const v4f sum = acc[0] + acc[1];
+        acc[0] = acc[1] = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
+        if (split > 1) { s_sum[wave * 64 + lane] = sum; break; }
+        // lane (i, g): row i, vectors 4 g + (0 .. 3)
+        const int r = 16 * from + i;
 #pragma unroll
-        for (int k = 1; k < KS; ++k) sum += s_sum[(wave + k) * 64 + lane];
+        for (int v = 0; v < 4; ++v)
+            if (r < m.rows && 4 * g + v < n) m.Y[(size_t)(4 * g + v) * m.ldy + r] = m.bias ? sum[v] + add : sum[v];
     }
-    // lane (i, g): row i, vectors 4 g + (0 .. 3)
-    if (!have || i >= left) return;
+    if (split == 1) return;
+    __syncthreads();                                                        // the ranges' sums, in one order
+    const int from = blockIdx.x + gridDim.x * (wave / split), r = 16 * from + i;
+    if (part || r >= m.rows) return;
+    v4f sum = s_sum[wave * 64 + lane];
+    for (int p = 1; p < split; ++p) sum += s_sum[(wave + p) * 64 + lane];
+    const float add = m.bias ? m.bias[r] : 0.0f;
 #pragma unroll
     for (int v = 0; v < 4; ++v)
-        if (4 * g + v < n) m.Y[(size_t)(4 * g + v) * m.ldy + r0 + i] = m.bias ? sum[v] + bias : sum[v];
+        if (4 * g + v < n) m.Y[(size_t)(4 * g + v) * m.ldy + r] = m.bias ? sum[v] + add : sum[v];
 }
 
-template <int KS> static q8_status launch_stream(q8_ctx *ctx, const F8StreamArgs &a)
+// split: waves for a row's columns, a power of two, at most `waves`; every one has columns, a multiple of four blocks of them.
+static q8_status launch_stream(q8_ctx *ctx, F8StreamArgs &a, int waves, int split)
 {
-    const int tiles = (a.g.rows + 15) / 16, per = 4 / KS;
-    hipLaunchKernelGGL(f8_stream_kernel<KS>, dim3((tiles + per - 1) / per), dim3(256), (size_t)a.g.n * a.pitch + (KS > 1 ? 4096 : 0), ctx->stream, a);
+    a.split = split;
+    a.span = ((a.nb + split - 1) / split + 3) / 4 * 4;
+    const int tiles = (a.g.rows + 15) / 16, per = waves / split;
+    int blocks = (tiles + per - 1) / per;
+    if (split == 1 && blocks > 256) blocks = 256;
+    hipLaunchKernelGGL(f8_stream_kernel, dim3(blocks), dim3(64 * waves), (size_t)a.g.n * a.pitch + (split > 1 ? 1024 * waves : 0), ctx->stream, a);
     return q8i_launch_check(ctx, "product f8");
 }
 
-static bool gemm_f8_streams(int n, int cols) { return n <= 16 && (size_t)n * (((cols + F8_BLOCK - 1) / F8_BLOCK) * 2 * F8_BLOCK + 16) <= 61440; }
+// Every block turns the vectors into bf16 values for itself, which saves a launch and costs time with their number (us; here and in
+// two launches with 128 x 32 or 64 x 32 tiles): 50000 x 512 x 8 8.3 and 8.4, x 16 9.7 and 8.9; 300 x 300 x 16 5.5 and 7.5;
+// 2048 x 2048 x 3 7.2 and 9.2; 512 x 8192 x 1 9.4 and 19.0, x 2 11.3 and 19.0; 1024 x 1024 x 16 9.3 and 8.1.
+static bool gemm_f8_streams(int n, int nb) { return n <= 16 && (long long)n * nb <= (n <= 4 ? 160 : 56); }
 
 // X in codes, or Xf [n x ldxf] in fp32 with X the room for its codes (rows, cols, ld, lds and memory), used where they are needed.
 q8_status q8i_gemm_f8(q8_ctx *ctx, const q8_mat_f8 *W, const q8_mat_f8 *X, const float *Xf, int ldxf, const float *bias, float *Y, int ldy)
 {
     F8GemmArgs a = {W->data, X->data, W->scale, X->scale, bias, Y, W->rows, X->rows, W->cols, W->ld, X->ld, W->lds, X->lds, ldy, 0, 0, 0, 0};
-    const bool streams = gemm_f8_streams(a.n, a.cols);
+    const int nb = (a.cols + F8_BLOCK - 1) / F8_BLOCK;
+    const bool streams = gemm_f8_streams(a.n, nb);
     // (results over the vectors: these are quantized first, as a whole)
     const char *x0 = (const char *)Xf, *x1 = (const char *)(Xf + (size_t)(a.n - 1) * ldxf + a.cols), *y0 = (const char *)Y, *y1 = (const char *)(Y + (size_t)(a.n - 1) * ldy + a.rows);
     if (Xf && (!streams || (x0 < y1 && y0 < x1))) {
@@ -522,14 +556,16 @@ q8_status q8i_gemm_f8(q8_ctx *ctx, const q8_mat_f8 *W, const q8_mat_f8 *X, const
         Xf = nullptr;
     }
     if (streams) {
-        F8StreamArgs s = {a, Xf, ldxf, 0, (a.cols + F8_BLOCK - 1) / F8_BLOCK, 0};
+        F8StreamArgs s = {a, Xf, ldxf, 0, nb, 0, 0, 0};
         s.vec = ldxf % 4 == 0 && ((uintptr_t)Xf & 15) == 0;
         s.pitch = s.nb * 2 * F8_BLOCK + 16;
-        // the columns in parts where the rows alone make few waves
+        // the columns in parts where the rows alone make few waves: 512 x 8192 x 1 9.4 in 8 parts against 23.3 us, 16384 x 2048 x 3
+        // 10.1 in two against 11.0 and 11.9 in four; blocks of four waves spread few rows wider (768 x 256 x 1 3.7 against 4.4)
         const int tiles = (a.rows + 15) / 16;
-        if (tiles <= 512 && s.nb >= 4) return launch_stream<4>(ctx, s);
-        if (tiles <= 1024 && s.nb >= 2) return launch_stream<2>(ctx, s);
-        return launch_stream<1>(ctx, s);
+        int split = 1;
+        while (split < 8 && s.nb > 4 * split && tiles * split < 2048) split *= 2;
+        const int waves = tiles < 1024 && split == 1 ? 4 : 8;
+        return launch_stream(ctx, s, waves, split);
     }
     return gemm_f8_tiles(ctx, a);
 }

@@ -10,6 +10,7 @@
 // thread adds what, and the borders between tokens lie where sums in 64-bit floating point put them to about 1e-12.
 #include "q8_internal.h"
 
+#include <algorithm>
 #include <math.h>
 
 typedef unsigned long long u64;
@@ -18,8 +19,9 @@ typedef unsigned long long u64;
 #define SMP_LOG2E32 46.166241308446828384    // 32 log2(e)
 #define SMP_SMALL 8192                       // vocabularies of at most so many words: a block per row
 #define SMP_PARTS 128                        // blocks of a row
+#define SMP_BLOCK 256                        // threads of these
 #define SMP_ROWS 1024                        // rows of a launch
-#define SMP_LIST 1536                        // words of a row that may lie where its borders do
+#define SMP_LIST 1536                        // words in LDS of those that lie where a row's borders do
 
 struct SampleArgs {
     const float *logits;
@@ -35,6 +37,8 @@ struct SampleArgs {
     int shift;                              // S
     // rows over several blocks
     struct SmpRowState *state;              // [rows of the launch]
+    u64 *lists;                             // [rows of the launch x list_words]: a row's words that lie where its borders do
+    int list_words;
     int parts, part_pieces, row0;           // blocks of a row, 16-byte pieces of each, first row of the launch
 };
 
@@ -101,12 +105,13 @@ template <int NE, int BLOCK> struct SmpRow {
     float v[NE ? NE : 1];
 
     __device__ __forceinline__ v4u load(int c) const { return __builtin_amdgcn_raw_buffer_load_b128(rows, c * 16, 0, 0); }
-    __device__ __forceinline__ void clean(v4u q, int c, float (&r)[4]) const
+    template <bool CHECK = true> __device__ __forceinline__ void clean(v4u q, int c, float (&r)[4]) const
     {
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-            r[t] = 4 * c + t < V && c < end ? fmaxf(__uint_as_float(q[t]), -INFINITY) : -INFINITY;
-            if (top_inf) r[t] = r[t] == INFINITY ? 0.0f : -INFINITY;
+            r[t] = fmaxf(__uint_as_float(q[t]), -INFINITY);
+            if (CHECK) r[t] = 4 * c + t < V && c < end ? r[t] : -INFINITY;
+            if (CHECK && top_inf) r[t] = r[t] == INFINITY ? 0.0f : -INFINITY;
         }
     }
     __device__ __forceinline__ void open(const float *row, int V_, int first_, int pieces_)
@@ -155,7 +160,30 @@ template <int NE, int BLOCK> struct SmpRow {
                 __builtin_amdgcn_sched_barrier(0);
             }
         } else {
-            for (int c = first + (int)threadIdx.x; c < end; c += 4 * BLOCK) {
+            int c = first + (int)threadIdx.x;
+            if (!top_inf) {                             // as long as every thread has four whole pieces
+                const int whole = min(end, V / 4);
+                v4u q[4];
+                int at = first;
+                if (at + 4 * BLOCK <= whole) {
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) q[t] = load(c + t * BLOCK);
+                }
+                for (; at + 4 * BLOCK <= whole; at += 4 * BLOCK, c += 4 * BLOCK) {
+                    v4u now[4];
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) now[t] = q[t];
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) q[t] = load(c + (4 + t) * BLOCK);
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        float r[4];
+                        clean<false>(now[t], c + t * BLOCK, r);
+                        f(r, 4 * (c + t * BLOCK));
+                    }
+                }
+            }
+            for (; c < end; c += 4 * BLOCK) {
                 v4u q[4];
 #pragma unroll
                 for (int t = 0; t < 4; ++t) q[t] = load(c + t * BLOCK);
@@ -203,12 +231,12 @@ template <int NE, int BLOCK> struct SmpRow {
     }
 };
 
-// Where a bin is in LDS: one place in nine is left out, so that threads that own eight bins each meet on few banks.
-__device__ __forceinline__ unsigned smp_at(unsigned b) { return b + (b >> 3); }
+// Where a bin is in LDS: exchanged so that 32 threads that own eight bins each, or two, find theirs on different banks.
+__device__ __forceinline__ unsigned smp_at(unsigned b) { return b ^ ((b >> 3) & 31u); }
 
 template <int BLOCK> struct SmpShared {
-    u64 mass[SMP_BINS + SMP_BINS / 8];      // per bin (smp_at), then up to and including it
-    unsigned count[SMP_BINS + SMP_BINS / 8];
+    u64 mass[SMP_BINS];      // per bin (smp_at), then up to and including it
+    unsigned count[SMP_BINS];
     u64 list[BLOCK];                        // keys of words that are ranked
     double pow[32];                         // 2^(S - j / 32)
     u64 red_u[16];
@@ -360,11 +388,16 @@ template <int BLOCK> __device__ __forceinline__ u64 smp_prefix(SmpShared<BLOCK> 
 // ---------------------------------------------------------------------- borders by bins ----
 
 // Histogram of the weights of (a part of) a row, and per thread the mass of its words at or above the border of min_p.
-template <int BLOCK, class Row>
-__device__ __forceinline__ u64 smp_histogram(const Row &row, SmpShared<BLOCK> &s, const SmpAsk &q, float m)
+// With SUM, e: the sum of the exponentials at T = 1 as well.
+template <bool SUM, int BLOCK, class Row>
+__device__ __forceinline__ u64 smp_histogram(const Row &row, SmpShared<BLOCK> &s, const SmpAsk &q, float m, double &e)
 {
     u64 above = 0;
     row.pieces([&](const float (&v)[4], int) {
+        if (SUM) {
+#pragma unroll
+            for (int t = 0; t < 4; t += 2) e += (double)(exp_le0(v[t] - m) + exp_le0(v[t + 1] - m));      // as the vocabulary layer's selection
+        }
         SmpPlace p[4];
         double w[4];
 #pragma unroll
@@ -684,7 +717,7 @@ __global__ __launch_bounds__(BLOCK) void sample_row_kernel(SampleArgs a)
         for (int t = 0; t < PER; ++t) { s.mass[smp_at(t * BLOCK + tid)] = 0; s.count[smp_at(t * BLOCK + tid)] = 0; }
         if (tid == 0) s.above = 0;
         __syncthreads();
-        const u64 above = smp_histogram<BLOCK>(row, s, q, m);
+        const u64 above = smp_histogram<false, BLOCK>(row, s, q, m, e);
         if (q.some_min && above) atomicAdd(&s.above, above);
         __syncthreads();
         smp_scan<BLOCK>(s, q.k > 0);
@@ -702,7 +735,6 @@ __global__ __launch_bounds__(BLOCK) void sample_row_kernel(SampleArgs a)
 struct SmpRowState {
     u64 mass[SMP_BINS];
     unsigned count[SMP_BINS];
-    u64 list[SMP_LIST];
     double e[SMP_PARTS];                    // sum of exp at T = 1 of a part
     float top[SMP_PARTS];                   // its largest logit
     u64 above;
@@ -710,16 +742,16 @@ struct SmpRowState {
 };
 
 // 1. The largest logit of each part; the row's sums are set to zero.
-__global__ __launch_bounds__(256) void sample_top_kernel(SampleArgs a)
+__global__ __launch_bounds__(SMP_BLOCK) void sample_top_kernel(SampleArgs a)
 {
-    __shared__ float red[4];
+    __shared__ float red[SMP_BLOCK / 64];
     const int j = a.row0 + blockIdx.y, part = blockIdx.x, tid = threadIdx.x;
     SmpRowState &st = a.state[blockIdx.y];
-    SmpRow<0, 256> row;
+    SmpRow<0, SMP_BLOCK> row;
     row.open(a.logits + (size_t)j * a.ldl, a.V, part * a.part_pieces, a.part_pieces);
-    for (int b = part * 256 + tid; b < SMP_BINS; b += 256 * a.parts) { st.mass[b] = 0; st.count[b] = 0; }
+    for (int b = part * SMP_BLOCK + tid; b < SMP_BINS; b += SMP_BLOCK * a.parts) { st.mass[b] = 0; st.count[b] = 0; }
     if (part == 0 && tid == 0) { st.above = 0; st.listed = 0; st.arrived = 0; }
-    const float m = smp_block_max<256>(row.largest(), red);
+    const float m = smp_block_max<SMP_BLOCK>(row.largest(), red);
     if (tid == 0) st.top[part] = m;
 }
 
@@ -740,13 +772,13 @@ __device__ __forceinline__ double smp_row_e(const SampleArgs &a, const SmpRowSta
 
 // 2. The weights of each part into bins, and the bins into the row's.
 template <int NE>
-__global__ __launch_bounds__(256) void sample_bins_kernel(SampleArgs a)
+__global__ __launch_bounds__(SMP_BLOCK) void sample_bins_kernel(SampleArgs a)
 {
     extern __shared__ __align__(16) char smem[];
-    SmpShared<256> &s = *(SmpShared<256> *)smem;
+    SmpShared<SMP_BLOCK> &s = *(SmpShared<SMP_BLOCK> *)smem;
     const int j = a.row0 + blockIdx.y, part = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     SmpRowState &st = a.state[blockIdx.y];
-    SmpRow<NE, 256> row;
+    SmpRow<NE, SMP_BLOCK> row;
     row.open(a.logits + (size_t)j * a.ldl, a.V, part * a.part_pieces, a.part_pieces);
     SmpAsk q;
     q.open(a, j);
@@ -756,28 +788,37 @@ __global__ __launch_bounds__(256) void sample_bins_kernel(SampleArgs a)
     if (m == INFINITY) { row.share_inf(); m = 0.0f; }
     if (q.drawn) {
 #pragma unroll
-        for (int t = 0; t < SMP_BINS / 256; ++t) { s.mass[smp_at(t * 256 + tid)] = 0; s.count[smp_at(t * 256 + tid)] = 0; }
+        for (int t = 0; t < SMP_BINS / SMP_BLOCK; ++t) { s.mass[smp_at(t * SMP_BLOCK + tid)] = 0; s.count[smp_at(t * SMP_BLOCK + tid)] = 0; }
     }
     __syncthreads();
     const bool own_sum = a.logp && q.T != 1.0f;
+    double e = 0.0;
+    u64 above = 0;
     if (own_sum) {
-        double e = 0.0;
-        row.pieces([&](const float (&v)[4], int) {
+        if (q.drawn) {
+            above = smp_histogram<true, SMP_BLOCK>(row, s, q, m, e);
+        } else {
+            row.pieces([&](const float (&v)[4], int) {
 #pragma unroll
-            for (int t = 0; t < 4; t += 2) e += (double)(exp_le0(v[t] - m) + exp_le0(v[t + 1] - m));      // as the vocabulary layer's selection
-        });
+                for (int t = 0; t < 4; t += 2) e += (double)(exp_le0(v[t] - m) + exp_le0(v[t + 1] - m));
+            });
+        }
         e = wave_sum_d(e);
         if (lane == 0) s.red_d[wave] = e;
+    } else if (q.drawn) {
+        above = smp_histogram<false, SMP_BLOCK>(row, s, q, m, e);
     }
-    u64 above = 0;
-    if (q.drawn) above = smp_histogram<256>(row, s, q, m);
     __syncthreads();
-    if (tid == 0 && own_sum) st.e[part] = (s.red_d[0] + s.red_d[1]) + (s.red_d[2] + s.red_d[3]);
+    if (tid == 0 && own_sum) {
+        e = s.red_d[0];
+        for (int w = 1; w < SMP_BLOCK / 64; ++w) e += s.red_d[w];
+        st.e[part] = e;
+    }
     if (!q.drawn) return;
     if (q.some_min && above) atomicAdd(&st.above, above);
 #pragma unroll
-    for (int t = 0; t < SMP_BINS / 256; ++t) {
-        const int b = t * 256 + tid;
+    for (int t = 0; t < SMP_BINS / SMP_BLOCK; ++t) {
+        const int b = t * SMP_BLOCK + tid;
         const u64 x = s.mass[smp_at(b)];
         if (x) atomicAdd(&st.mass[b], x);
         const unsigned c = q.k > 0 ? s.count[smp_at(b)] : 0;
@@ -789,51 +830,51 @@ __global__ __launch_bounds__(256) void sample_bins_kernel(SampleArgs a)
 // it to the bins that both ends give); the words of these bins, from every part; and the last part to be done finds the
 // borders among them.
 template <int NE>
-__global__ __launch_bounds__(256) void sample_draw_kernel(SampleArgs a)
+__global__ __launch_bounds__(SMP_BLOCK) void sample_draw_kernel(SampleArgs a)
 {
     extern __shared__ __align__(16) char smem[];
-    SmpShared<256> &s = *(SmpShared<256> *)smem;
+    SmpShared<SMP_BLOCK> &s = *(SmpShared<SMP_BLOCK> *)smem;
     __shared__ u64 s_found[SMP_LIST];
-    __shared__ unsigned s_n, s_at, s_last;
+    __shared__ unsigned s_at, s_last;
     const int j = a.row0 + blockIdx.y, part = blockIdx.x, tid = threadIdx.x;
     SmpRowState &st = a.state[blockIdx.y];
-    SmpRow<NE, 256> row;
+    SmpRow<NE, SMP_BLOCK> row;
     SmpAsk q;
     q.open(a, j);
     // (requested before anything is waited for)
-    u64 mass[SMP_BINS / 256];
-    unsigned count[SMP_BINS / 256];
+    u64 mass[SMP_BINS / SMP_BLOCK];
+    unsigned count[SMP_BINS / SMP_BLOCK];
 #pragma unroll
-    for (int t = 0; t < SMP_BINS / 256; ++t) { mass[t] = st.mass[t * 256 + tid]; count[t] = st.count[t * 256 + tid]; }
+    for (int t = 0; t < SMP_BINS / SMP_BLOCK; ++t) { mass[t] = st.mass[t * SMP_BLOCK + tid]; count[t] = st.count[t * SMP_BLOCK + tid]; }
     const u64 above = st.above;
     const double e_parts = smp_row_e(a, st);
     row.open(a.logits + (size_t)j * a.ldl, a.V, part * a.part_pieces, a.part_pieces);
     float m = smp_row_top(a, st);
     if (m == -INFINITY) {                               // no word can be drawn
-        if (part == 0) smp_write(a, j, -1, -INFINITY, 256);
+        if (part == 0) smp_write(a, j, -1, -INFINITY, SMP_BLOCK);
         return;
     }
     if (m == INFINITY) { row.share_inf(); m = 0.0f; }
     if (tid < 32) s.pow[tid] = smp_pow[tid] * q.one;
-    if (tid == 0) { s_n = 0; s.above = above; }
+    if (tid == 0) s.above = above;
     SmpWindow w[3];
 #pragma unroll
     for (int i = 0; i < 3; ++i) { w[i].b0 = 1; w[i].b1 = 0; w[i].low = INFINITY; w[i].high = -INFINITY; }
     if (q.drawn) {
 #pragma unroll
-        for (int t = 0; t < SMP_BINS / 256; ++t) { s.mass[smp_at(t * 256 + tid)] = mass[t]; s.count[smp_at(t * 256 + tid)] = count[t]; }
+        for (int t = 0; t < SMP_BINS / SMP_BLOCK; ++t) { s.mass[smp_at(t * SMP_BLOCK + tid)] = mass[t]; s.count[smp_at(t * SMP_BLOCK + tid)] = count[t]; }
         __syncthreads();
-        smp_scan<256>(s, q.k > 0);
+        smp_scan<SMP_BLOCK>(s, q.k > 0);
         u64 low = s.mass[smp_at(SMP_BINS - 1)], high = low;
         if (q.k > 0 && (unsigned)q.k < s.count[smp_at(SMP_BINS - 1)]) {
-            const unsigned b = smp_find<256>(s, true, [&](unsigned c, u64) { return c >= (unsigned)q.k; });
+            const unsigned b = smp_find<SMP_BLOCK>(s, true, [&](unsigned c, u64) { return c >= (unsigned)q.k; });
             w[0].open(b, b, m, q.c);
             low = b ? s.mass[smp_at(b - 1)] : 0;
             high = s.mass[smp_at(b)];
         }
         if (q.tp < 1.0f) {
             const double n0 = fmax((double)q.tp * (double)low, 0.5), n1 = fmax((double)q.tp * (double)high, 0.5);
-            const unsigned b0 = smp_find<256>(s, false, [&](unsigned, u64 x) { return (double)x >= n0; }), b1 = smp_find<256>(s, false, [&](unsigned, u64 x) { return (double)x >= n1; });
+            const unsigned b0 = smp_find<SMP_BLOCK>(s, false, [&](unsigned, u64 x) { return (double)x >= n0; }), b1 = smp_find<SMP_BLOCK>(s, false, [&](unsigned, u64 x) { return (double)x >= n1; });
             w[1].open(b0, b1, m, q.c);
             low = b0 ? s.mass[smp_at(b0 - 1)] : 0;
             high = s.mass[smp_at(b1)];
@@ -841,34 +882,69 @@ __global__ __launch_bounds__(256) void sample_draw_kernel(SampleArgs a)
         if (q.some_min) { low = min(low, above); high = min(high, above); }
         const u64 first = 1ull << a.shift;
         const double n0 = (double)q.u * (double)max(low, first), n1 = (double)q.u * (double)max(high, first);
-        w[2].open(smp_find<256>(s, false, [&](unsigned, u64 x) { return (double)x > n0; }), smp_find<256>(s, false, [&](unsigned, u64 x) { return (double)x > n1; }), m, q.c);
+        w[2].open(smp_find<SMP_BLOCK>(s, false, [&](unsigned, u64 x) { return (double)x > n0; }), smp_find<SMP_BLOCK>(s, false, [&](unsigned, u64 x) { return (double)x > n1; }), m, q.c);
     } else {
         w[2].low = w[2].high = m;
         w[2].b0 = 0; w[2].b1 = SMP_BINS;
         __syncthreads();
     }
-    // ---- the words of those bins
+    // ---- the words of those bins (and few beside them, which the borders pass over): every wave has a list of its own, and puts it
+    // into the row's when it is full
     const bool use0 = w[0].b0 <= w[0].b1, use1 = w[1].b0 <= w[1].b1;
-    row.some([&](float v) {
-                 bool n = w[2].near(v);
-                 if (use0) n = n || w[0].near(v);
-                 if (use1) n = n || w[1].near(v);
-                 return n;
-             },
-             [&](float v) {
-                 const unsigned b = smp_place(smp_gap(m, v), q.c).bin;
-                 return w[0].has(b) || w[1].has(b) || w[2].has(b);
-             },
-             [&](u64 key) {
-                 const unsigned at = atomicAdd(&s_n, 1u);
-                 if (at < SMP_LIST) s_found[at] = key;
-             });
+    const int wave = tid >> 6;
+    constexpr unsigned LIST = SMP_LIST / (SMP_BLOCK / 64);
+    u64 *list = a.lists + (size_t)blockIdx.y * a.list_words;
+    const unsigned room = (unsigned)a.list_words;
+    unsigned mine = 0;                                  // (the same in all lanes that are at work; lane 0 is to the end)
+    auto rank = [](u64 mask) { return __builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0)); };
+    row.pieces([&](const float (&v)[4], int i) {
+        bool n[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) n[t] = w[2].near(v[t]);
+        if (use0) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t) n[t] = n[t] | w[0].near(v[t]);
+        }
+        if (use1) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t) n[t] = n[t] | w[1].near(v[t]);
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const u64 mask = __ballot(n[t]);
+            if (mask) {
+                const unsigned more = (unsigned)__popcll(mask);
+                if (mine + more > LIST) {
+                    const u64 active = __ballot(true);
+                    const unsigned me = rank(active);
+                    unsigned at = 0;
+                    if (me == 0) at = atomicAdd(&st.listed, mine);
+                    at = __builtin_amdgcn_readfirstlane(at);
+                    __builtin_amdgcn_wave_barrier();
+                    for (unsigned x = me; x < mine; x += (unsigned)__popcll(active))
+                        if (at + x < room) __hip_atomic_store(&list[at + x], s_found[wave * LIST + x], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    __builtin_amdgcn_wave_barrier();
+                    mine = 0;
+                }
+                if (n[t]) s_found[wave * LIST + mine + rank(mask)] = topk_key(v[t], i + t);
+                mine += more;
+            }
+        }
+    });
+    mine = __builtin_amdgcn_readfirstlane(mine);
+    if ((tid & 63) == 0) s.red_c[wave] = mine;
     __syncthreads();
-    const unsigned found = s_n;
-    if (tid == 0) s_at = found ? atomicAdd(&st.listed, found <= SMP_LIST ? found : SMP_LIST + 1) : 0u;
+    unsigned found = 0, before = 0;
+#pragma unroll
+    for (int o = 0; o < SMP_BLOCK / 64; ++o) {
+        const unsigned c = s.red_c[o];
+        if (o < wave) before += c;
+        found += c;
+    }
+    if (tid == 0) s_at = found ? atomicAdd(&st.listed, found) : 0u;
     __syncthreads();
-    for (unsigned x = tid; x < min(found, (unsigned)SMP_LIST); x += 256)
-        if (s_at + x < SMP_LIST) __hip_atomic_store(&st.list[s_at + x], s_found[x], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    for (unsigned x = tid & 63; x < mine; x += 64)
+        if (s_at + before + x < room) __hip_atomic_store(&list[s_at + before + x], s_found[wave * LIST + x], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     q8_stores_performed();
     __syncthreads();
     if (tid == 0) s_last = __hip_atomic_fetch_add(&st.arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (unsigned)a.parts - 1 ? 1u : 0u;
@@ -877,22 +953,33 @@ __global__ __launch_bounds__(256) void sample_draw_kernel(SampleArgs a)
 
     // ---- the last part: the borders
     const unsigned listed = __hip_atomic_load(&st.listed, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    SmpRow<0, 256> whole;
+    SmpRow<0, SMP_BLOCK> whole;
     whole.open(a.logits + (size_t)j * a.ldl, a.V, 0, 0x7fffffff / 4);
     whole.top_inf = row.top_inf;
     if (listed <= SMP_LIST) {                           // from here on in LDS
-        for (unsigned x = tid; x < listed; x += 256) s_found[x] = __hip_atomic_load(&st.list[x], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        for (unsigned x = tid; x < listed; x += SMP_BLOCK) s_found[x] = __hip_atomic_load(&list[x], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         __syncthreads();
     }
     u64 key;
     if (q.drawn) {
-        key = smp_borders<256>([&](const SmpWindow &win, auto f) {
+        key = smp_borders<SMP_BLOCK>([&](const SmpWindow &win, auto f) {
             auto in = [&](float v) { return smp_place(smp_gap(m, v), q.c).bin == win.b0; };
-            if (listed > SMP_LIST) {
+            if (listed > room) {
                 whole.some([&](float v) { return win.near(v); }, in, f);
                 return;
             }
-            for (unsigned x = tid; x < listed; x += 256)
+            if (listed > SMP_LIST) {
+                for (unsigned x0 = tid; x0 < listed; x0 += 4 * SMP_BLOCK) {
+                    u64 k[4];
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) k[t] = x0 + t * SMP_BLOCK < listed ? __hip_atomic_load(&list[x0 + t * SMP_BLOCK], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+                        if (k[t] && win.near(topk_key_val(k[t])) && in(topk_key_val(k[t]))) f(k[t]);
+                }
+                return;
+            }
+            for (unsigned x = tid; x < listed; x += SMP_BLOCK)
                 if (in(topk_key_val(s_found[x]))) f(s_found[x]);
         }, s, q, m, a.shift);
     } else {
@@ -904,20 +991,25 @@ __global__ __launch_bounds__(256) void sample_draw_kernel(SampleArgs a)
                     if (v[t] == m) best = max(best, topk_key(v[t], i + t));
             });
         } else {
-            for (unsigned x = tid; x < listed; x += 256) best = max(best, s_found[x]);
+            for (unsigned x = tid; x < listed; x += SMP_BLOCK) best = max(best, s_found[x]);
         }
         best = wave_max_u64(best);
         if ((tid & 63) == 0) s.red_u[tid >> 6] = best;
         __syncthreads();
-        key = max(max(s.red_u[0], s.red_u[1]), max(s.red_u[2], s.red_u[3]));
+        key = s.red_u[0];
+        for (int w = 1; w < SMP_BLOCK / 64; ++w) key = max(key, s.red_u[w]);
     }
     const double e = q.T == 1.0f ? (double)s.mass[smp_at(SMP_BINS - 1)] / q.one : e_parts;
-    smp_write(a, j, topk_key_idx(key), (float)(-smp_gap(m, topk_key_val(key)) - log(e)), 256);
+    smp_write(a, j, topk_key_idx(key), (float)(-smp_gap(m, topk_key_val(key)) - log(e)), SMP_BLOCK);
 }
 
 static int sample_rows(int n) { return n < SMP_ROWS ? n : SMP_ROWS; }
 
-size_t q8i_sample_bytes(int n, int V) { return V <= SMP_SMALL ? 0 : (size_t)sample_rows(n) * sizeof(SmpRowState); }
+// Words that a row's list holds: of Gaussian logits 0.6 % lie in the fullest bin (row of 1.4 nat deviation), and there are three.
+// Where there are more, one block goes through the row again for every border (12 rows of 250001 words 108 us instead of 26).
+static int sample_list_words(int V) { return std::min(std::max(SMP_LIST, (V / 32 + 63) & ~63), 16384); }
+
+size_t q8i_sample_bytes(int n, int V) { return V <= SMP_SMALL ? 0 : (size_t)sample_rows(n) * (sizeof(SmpRowState) + sizeof(u64) * sample_list_words(V)); }
 
 q8_status q8i_sample(q8_ctx *ctx, const float *logits, int n, int V, int ldl, const q8_sampling *s, const float *u, int32_t *tokens, float *logp,
                      const float *E_tgt, int E, float *y_emb, void *state)
@@ -938,24 +1030,26 @@ q8_status q8i_sample(q8_ctx *ctx, const float *logits, int n, int V, int ldl, co
         return q8i_launch_check(ctx, "sample");
     }
     a.state = (SmpRowState *)state;
+    a.list_words = sample_list_words(V);
+    a.lists = (u64 *)(a.state + sample_rows(n));
     const int pieces = (V + 3) / 4;
     for (a.row0 = 0; a.row0 < n; a.row0 += SMP_ROWS) {
         const int rows = n - a.row0 < SMP_ROWS ? n - a.row0 : SMP_ROWS;
-        // three blocks a compute unit, which is what it holds of them, none of less than 2048 words: 64 rows of 50000 words 44.6 / 38.9 / 37.6
-        // / 40.6 us with 1024 / 768 / 512 / 256 blocks, 12 of 250001 32.5 / 26.3 / 30.3 / 33.3
+        // three blocks a compute unit, none of less than 2048 words: 64 rows of 50000 words 36.5 / 37.2 / 47 us with 768 / 1024 / 1536
+        // blocks, 12 of 250001 26.4 / 31.6 / 40, 200 of 33658 53.9 / 58.4 / 67
         int parts = (768 + rows - 1) / rows;
         if (parts > (pieces + 511) / 512) parts = (pieces + 511) / 512;
         if (parts > SMP_PARTS) parts = SMP_PARTS;
         a.part_pieces = (pieces + parts - 1) / parts;
         a.parts = (pieces + a.part_pieces - 1) / a.part_pieces;
-        const dim3 grid(a.parts, rows);
-        hipLaunchKernelGGL(sample_top_kernel, grid, dim3(256), 0, ctx->stream, a);
-        if (a.part_pieces <= 1024) {
-            hipLaunchKernelGGL(sample_bins_kernel<16>, grid, dim3(256), smem, ctx->stream, a);
-            hipLaunchKernelGGL(sample_draw_kernel<16>, grid, dim3(256), smem, ctx->stream, a);
+        const dim3 grid(a.parts, rows), block(SMP_BLOCK);
+        hipLaunchKernelGGL(sample_top_kernel, grid, block, 0, ctx->stream, a);
+        if (a.part_pieces <= 4 * SMP_BLOCK) {
+            hipLaunchKernelGGL(sample_bins_kernel<16>, grid, block, smem, ctx->stream, a);
+            hipLaunchKernelGGL(sample_draw_kernel<16>, grid, block, smem, ctx->stream, a);
         } else {
-            hipLaunchKernelGGL(sample_bins_kernel<0>, grid, dim3(256), smem, ctx->stream, a);
-            hipLaunchKernelGGL(sample_draw_kernel<0>, grid, dim3(256), smem, ctx->stream, a);
+            hipLaunchKernelGGL(sample_bins_kernel<0>, grid, block, smem, ctx->stream, a);
+            hipLaunchKernelGGL(sample_draw_kernel<0>, grid, block, smem, ctx->stream, a);
         }
         const q8_status st = q8i_launch_check(ctx, "sample");
         if (st) return st;

@@ -99,6 +99,24 @@ def test_rows_of_equal_logits(q, ctx, V):
     _check(q, ctx, lg, u, min_p=np.full(n, 1.0, np.float32), T=np.full(n, 0.5, np.float32))
 
 
+@pytest.mark.parametrize("n,V", [(3, 250001), (2, 600000), (900, 9001)])
+@pytest.mark.parametrize("words", [300, 1500, 3000, 7000])
+@pytest.mark.parametrize("apart", [1, 31])
+def test_many_words_of_nearly_the_same_weight(q, ctx, n, V, words, apart):
+    """Borders among many words within 1/64 nat, next to each other or spread over the row."""
+    if words * apart > V:
+        pytest.skip("more words than the row has")
+    rng = np.random.default_rng(words + apart)
+    lg = np.full((n, V), -30.0, np.float32)
+    for j in range(n):
+        at = int(rng.integers(0, V - words * apart + 1))
+        lg[j, at:at + words * apart:apart] = 2.0 + rng.random(words) / 64
+    u = rng.random(n).astype(np.float32).clip(0, TOP)
+    _check(q, ctx, lg, u)
+    _check(q, ctx, lg, u, top_k=rng.integers(1, words, n).astype(np.int32), top_p=rng.random(n).astype(np.float32))
+    _check(q, ctx, lg, u, T=np.full(n, 0.4, np.float32), top_p=rng.random(n).astype(np.float32), min_p=np.full(n, 0.97, np.float32))
+
+
 def test_two_values_that_many_words_share(q, ctx):
     rng = np.random.default_rng(2)
     lg = rng.choice(np.array([1.0, 1.0000001, 0.9999999], np.float32), (8, 40000))

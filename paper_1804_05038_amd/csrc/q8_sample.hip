@@ -48,13 +48,15 @@ struct SampleArgs {
 __device__ __forceinline__ double smp_gap(float m, float v) { return (double)m - (double)v; }
 
 // A word's place in units of 1/32 octave of weight, x = gap c with c = 32 log2(e) / T, in fixed point: the sum with 2^20
-// keeps the whole part in the high word and 32 bits of fraction in the low word.  Monotone in the logit.
+// keeps the whole part in the high word and 32 bits of fraction in the low word.  Monotone in the logit.  LIMIT: to SMP_BINS, where
+// weights round to zero; else a place past the bins is some number that is not below SMP_BINS.
 struct SmpPlace {
     unsigned bin, frac;
 };
-__device__ __forceinline__ SmpPlace smp_place(double gap, double c)
+template <bool LIMIT = true> __device__ __forceinline__ SmpPlace smp_place(double gap, double c)
 {
-    const double t = fmin(fma(gap, c, 0x1p20), 0x1p20 + SMP_BINS);
+    double t = fma(gap, c, 0x1p20);
+    if (LIMIT) t = fmin(t, 0x1p20 + SMP_BINS);
     return {(unsigned)__double2hiint(t) - 0x41300000u, (unsigned)__double2loint(t)};
 }
 
@@ -84,14 +86,6 @@ __device__ __forceinline__ double smp_weight(SmpPlace p, const double *s_pow)
 }
 // ... to the nearest whole number (below 2^47).
 __device__ __forceinline__ u64 smp_whole(double w) { return (u64)__double_as_longlong(w + 0x1p52) & 0xfffffffffffffull; }
-
-// exp(-gap) for the sum at T = 1: the hardware's exponential of the fraction of an octave (2^-23 off at most).
-__device__ __forceinline__ double smp_exp1(double gap)
-{
-    const double x = fmin(fma(gap, SMP_LOG2E32 / 32.0, 0x1p20), 0x1p20 + 1024.0);
-    const float f = (float)(unsigned)__double2loint(x) * -0x1p-32f;
-    return (double)ldexpf(__builtin_amdgcn_exp2f(f), -(int)((unsigned)__double2hiint(x) - 0x41300000u));
-}
 
 // ---------------------------------------------------------------------------------- rows ----
 
@@ -252,7 +246,7 @@ struct SmpAsk {
     float T, tp, mp, u;
     int k;
     bool drawn, some_min;
-    double c, one, floor_w;                 // 32 log2(e) / T; 2^S; min_p 2^S
+    double c, inv, one, floor_w;            // 32 log2(e) / T; 1 / c; 2^S; min_p 2^S
 
     __device__ __forceinline__ void open(const SampleArgs &a, int j)
     {
@@ -267,6 +261,7 @@ struct SmpAsk {
         one = (double)(1ull << a.shift);
         // (T = inf: every finite distance counts as none, an infinite one still as infinite)
         c = fmax(SMP_LOG2E32 / (drawn ? (double)T : 1.0), 1e-300);
+        inv = 1.0 / c;
         floor_w = (double)mp * one;
     }
 };
@@ -282,38 +277,38 @@ template <int BLOCK> __device__ __forceinline__ float smp_block_max(float v, flo
     return v;
 }
 
-__device__ __forceinline__ u64 smp_wave_scan(u64 v)             // up to and including each lane
+template <int CTRL, int ROWS> __device__ __forceinline__ u64 smp_from_below(u64 v)           // zero where there is no such lane
 {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const u64 o = __shfl_up(v, d);
-        if (lane >= d) v += o;
-    }
+    const unsigned lo = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)v, CTRL, ROWS, 0xf, false);
+    const unsigned hi = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)(v >> 32), CTRL, ROWS, 0xf, false);
+    return ((u64)hi << 32) | lo;
+}
+__device__ __forceinline__ u64 smp_wave_scan(u64 v)             // up to and including each lane: within rows of 16, then over the rows
+{
+    v += smp_from_below<0x111, 0xf>(v);
+    v += smp_from_below<0x112, 0xf>(v);
+    v += smp_from_below<0x114, 0xf>(v);
+    v += smp_from_below<0x118, 0xf>(v);
+    v += smp_from_below<0x142, 0xa>(v);
+    v += smp_from_below<0x143, 0xc>(v);
     return v;
 }
 
-// Counts and masses per bin -> up to and including each bin.
-template <int BLOCK> __device__ __forceinline__ void smp_scan(SmpShared<BLOCK> &s, bool counts)
+// Masses and counts of the bins that each thread has, SMP_BINS / BLOCK in a row, -> s.mass, s.count: up to and including each bin.
+template <int BLOCK> __device__ __forceinline__ void smp_scan(SmpShared<BLOCK> &s, u64 (&mm)[SMP_BINS / BLOCK], unsigned (&cc)[SMP_BINS / BLOCK], bool counts)
 {
     constexpr int PER = SMP_BINS / BLOCK;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    u64 mm[PER], sm = 0;
-    unsigned cc[PER], sc = 0;
+    u64 sm = 0;
+    unsigned sc = 0;
 #pragma unroll
     for (int t = 0; t < PER; ++t) {
-        sm += s.mass[smp_at(PER * tid + t)]; mm[t] = sm;
-        sc += counts ? s.count[smp_at(PER * tid + t)] : 0; cc[t] = sc;
+        sm += mm[t]; mm[t] = sm;
+        sc += cc[t]; cc[t] = sc;
     }
     u64 im = smp_wave_scan(sm);
     unsigned ic = sc;
-    if (counts) {
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const unsigned oc = __shfl_up(ic, d);
-            if (lane >= d) ic += oc;
-        }
-    }
+    if (counts) ic = (unsigned)smp_wave_scan(sc);
     if (lane == 63) { s.red_u[wave] = im; s.red_c[wave] = ic; }
     __syncthreads();
     im -= sm;
@@ -401,7 +396,7 @@ __device__ __forceinline__ u64 smp_histogram(const Row &row, SmpShared<BLOCK> &s
         SmpPlace p[4];
         double w[4];
 #pragma unroll
-        for (int t = 0; t < 4; ++t) p[t] = smp_place(smp_gap(m, v[t]), q.c);
+        for (int t = 0; t < 4; ++t) p[t] = smp_place<false>(smp_gap(m, v[t]), q.c);
 #pragma unroll
         for (int t = 0; t < 4; ++t) w[t] = smp_weight(p[t], s.pow);
 #pragma unroll
@@ -410,8 +405,11 @@ __device__ __forceinline__ u64 smp_histogram(const Row &row, SmpShared<BLOCK> &s
                 const u64 x = smp_whole(w[t]);
                 atomicAdd(&s.mass[smp_at(p[t].bin)], x);
                 if (q.k > 0) atomicAdd(&s.count[smp_at(p[t].bin)], 1u);
-                if (w[t] >= q.floor_w) above += x;
             }
+        if (q.some_min) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t) above += p[t].bin < SMP_BINS && w[t] >= q.floor_w ? smp_whole(w[t]) : 0;
+        }
     });
     return above;
 }
@@ -444,11 +442,11 @@ template <int BLOCK, class Cond> __device__ __forceinline__ unsigned smp_find(co
 struct SmpWindow {
     unsigned b0, b1;
     float low, high;
-    __device__ __forceinline__ void open(unsigned first, unsigned last, float m, double c)
+    __device__ __forceinline__ void open(unsigned first, unsigned last, float m, double inv)
     {
         b0 = first;
         b1 = last;
-        const double gap0 = (double)first / c, gap1 = ((double)last + 1.0) / c, am = fabs((double)m);
+        const double gap0 = (double)first * inv, gap1 = ((double)last + 1.0) * inv, am = fabs((double)m);
         high = (float)((double)m - gap0 + 1e-6 * (am + gap0));
         low = (float)((double)m - gap1 - 1e-6 * (am + gap1));
     }
@@ -458,7 +456,7 @@ struct SmpWindow {
 
 // The drawn word of a row whose bins are in s.mass / s.count (up to and including each; counts only if top-k is in force) and
 // whose mass of words at or above the min_p border is s.above: for each border the one bin that it falls into, then the
-// words of that bin in their order.  words(window, f) calls f(key) for every word of a bin.  While there are more than BLOCK, a
+// words of that bin in their order.  words(window, f) calls f(key) for every word of a bin.  While there are more than 64, a
 // histogram over 256 even parts of the range of their keys says in which of them the border lies.
 template <int BLOCK, class Words>
 __device__ __forceinline__ u64 smp_borders(Words words, SmpShared<BLOCK> &s, const SmpAsk &q, float m, int shift)
@@ -483,7 +481,7 @@ __device__ __forceinline__ u64 smp_borders(Words words, SmpShared<BLOCK> &s, con
         u64 before_m = bin ? s.mass[smp_at(bin - 1)] : 0;
         unsigned before_c = stage == 0 && bin ? s.count[smp_at(bin - 1)] : 0;
         SmpWindow win;
-        win.open(bin, bin, m, q.c);
+        win.open(bin, bin, m, q.inv);
         u64 lowest = topk_key(win.low, 0x7fffffff), highest = topk_key(win.high, 0);
         for (;;) {
             if (tid == 0) s.listed = 0;
@@ -511,17 +509,6 @@ __device__ __forceinline__ u64 smp_borders(Words words, SmpShared<BLOCK> &s, con
                 found_m = smp_lane(ms, at);
                 break;
             }
-            if (members <= BLOCK) {
-                const u64 key = smp_sorted<BLOCK>(s);
-                const u64 own = key ? smp_mass_of(key, m, q.c, s.pow) : 0;
-                const u64 ms = before_m + smp_prefix<BLOCK>(s, own);
-                const unsigned cs = before_c + tid + 1;
-                if (key && cond(cs, ms) && !cond(cs - 1, ms - own)) { s.hit_key = key; s.hit_mass = ms; }
-                __syncthreads();
-                found = s.hit_key;
-                found_m = s.hit_mass;
-                break;
-            }
             __syncthreads();
             u64 *h_m = s.list;                                  // [256], the block has at least as many threads
             const int sh = max(0, 64 - 8 - __clzll((long long)(highest - lowest)));
@@ -538,7 +525,7 @@ __device__ __forceinline__ u64 smp_borders(Words words, SmpShared<BLOCK> &s, con
             const u64 own = tid < 256 ? h_m[d] : 0;
             const unsigned own_c = tid < 256 ? s.bytes[d] : 0;
             const u64 ms = before_m + smp_prefix<BLOCK>(s, own);
-            const unsigned cs = before_c + (unsigned)smp_prefix<BLOCK>(s, own_c);
+            const unsigned cs = stage == 0 ? before_c + (unsigned)smp_prefix<BLOCK>(s, own_c) : own_c;
             if (own_c && cond(cs, ms) && !cond(cs - own_c, ms - own)) { s.hit_key = lowest + ((u64)d << sh); s.hit_mass = ms - own; s.known_c = cs - own_c; }
             __syncthreads();
             lowest = s.hit_key;
@@ -720,7 +707,12 @@ __global__ __launch_bounds__(BLOCK) void sample_row_kernel(SampleArgs a)
         const u64 above = smp_histogram<false, BLOCK>(row, s, q, m, e);
         if (q.some_min && above) atomicAdd(&s.above, above);
         __syncthreads();
-        smp_scan<BLOCK>(s, q.k > 0);
+        u64 mm[PER];
+        unsigned cc[PER];
+#pragma unroll
+        for (int t = 0; t < PER; ++t) { mm[t] = s.mass[smp_at(PER * tid + t)]; cc[t] = s.count[smp_at(PER * tid + t)]; }
+        __syncthreads();
+        smp_scan<BLOCK>(s, mm, cc, q.k > 0);
         const auto stored = row.stored();
         key = smp_borders<BLOCK>([&](const SmpWindow &win, auto f) {
             stored.some([&](float v) { return win.near(v); }, [&](float v) { return smp_place(smp_gap(m, v), q.c).bin == win.b0; }, f);
@@ -845,7 +837,7 @@ __global__ __launch_bounds__(SMP_BLOCK) void sample_draw_kernel(SampleArgs a)
     u64 mass[SMP_BINS / SMP_BLOCK];
     unsigned count[SMP_BINS / SMP_BLOCK];
 #pragma unroll
-    for (int t = 0; t < SMP_BINS / SMP_BLOCK; ++t) { mass[t] = st.mass[t * SMP_BLOCK + tid]; count[t] = st.count[t * SMP_BLOCK + tid]; }
+    for (int t = 0; t < SMP_BINS / SMP_BLOCK; ++t) { mass[t] = st.mass[SMP_BINS / SMP_BLOCK * tid + t]; count[t] = st.count[SMP_BINS / SMP_BLOCK * tid + t]; }
     const u64 above = st.above;
     const double e_parts = smp_row_e(a, st);
     row.open(a.logits + (size_t)j * a.ldl, a.V, part * a.part_pieces, a.part_pieces);
@@ -861,28 +853,25 @@ __global__ __launch_bounds__(SMP_BLOCK) void sample_draw_kernel(SampleArgs a)
 #pragma unroll
     for (int i = 0; i < 3; ++i) { w[i].b0 = 1; w[i].b1 = 0; w[i].low = INFINITY; w[i].high = -INFINITY; }
     if (q.drawn) {
-#pragma unroll
-        for (int t = 0; t < SMP_BINS / SMP_BLOCK; ++t) { s.mass[smp_at(t * SMP_BLOCK + tid)] = mass[t]; s.count[smp_at(t * SMP_BLOCK + tid)] = count[t]; }
-        __syncthreads();
-        smp_scan<SMP_BLOCK>(s, q.k > 0);
+        smp_scan<SMP_BLOCK>(s, mass, count, q.k > 0);
         u64 low = s.mass[smp_at(SMP_BINS - 1)], high = low;
         if (q.k > 0 && (unsigned)q.k < s.count[smp_at(SMP_BINS - 1)]) {
             const unsigned b = smp_find<SMP_BLOCK>(s, true, [&](unsigned c, u64) { return c >= (unsigned)q.k; });
-            w[0].open(b, b, m, q.c);
+            w[0].open(b, b, m, q.inv);
             low = b ? s.mass[smp_at(b - 1)] : 0;
             high = s.mass[smp_at(b)];
         }
         if (q.tp < 1.0f) {
             const double n0 = fmax((double)q.tp * (double)low, 0.5), n1 = fmax((double)q.tp * (double)high, 0.5);
             const unsigned b0 = smp_find<SMP_BLOCK>(s, false, [&](unsigned, u64 x) { return (double)x >= n0; }), b1 = smp_find<SMP_BLOCK>(s, false, [&](unsigned, u64 x) { return (double)x >= n1; });
-            w[1].open(b0, b1, m, q.c);
+            w[1].open(b0, b1, m, q.inv);
             low = b0 ? s.mass[smp_at(b0 - 1)] : 0;
             high = s.mass[smp_at(b1)];
         }
         if (q.some_min) { low = min(low, above); high = min(high, above); }
         const u64 first = 1ull << a.shift;
         const double n0 = (double)q.u * (double)max(low, first), n1 = (double)q.u * (double)max(high, first);
-        w[2].open(smp_find<SMP_BLOCK>(s, false, [&](unsigned, u64 x) { return (double)x > n0; }), smp_find<SMP_BLOCK>(s, false, [&](unsigned, u64 x) { return (double)x > n1; }), m, q.c);
+        w[2].open(smp_find<SMP_BLOCK>(s, false, [&](unsigned, u64 x) { return (double)x > n0; }), smp_find<SMP_BLOCK>(s, false, [&](unsigned, u64 x) { return (double)x > n1; }), m, q.inv);
     } else {
         w[2].low = w[2].high = m;
         w[2].b0 = 0; w[2].b1 = SMP_BINS;

@@ -59,7 +59,8 @@ struct F8QuantArgs {
 
 #define F8_QUANT_PER_WAVE 8          // blocks that a wave takes, two at a time
 
-// A half wave per block of 128 columns: four values a lane.
+// A half wave per block of 128 columns: four values a lane.  A wave asks for eight blocks before it waits.  Bound by memory:
+// 50000 x 620 in 31.6 us, 4.9 TB/s read and written (a copy of 4 GiB: 4.8); 8 x 1024 in 4.3, a launch.
 __global__ __launch_bounds__(256) void f8_quantize_kernel(F8QuantArgs a)
 {
     const int lane = threadIdx.x & 63, half = lane >> 5, i = lane & 31;
@@ -178,6 +179,10 @@ __device__ __forceinline__ void f8_to_lds(__amdgpu_buffer_rsrc_t rsrc, uint8_t *
 // an instruction, which the matrix cores' time covers (24 conversions beside 8 products of 32 x 32 x 16).  The order of k
 // inside a block is the same for both operands, which is all that it has to be: lane half h takes the 16-byte pieces 2 j + h.
 // KS > 1: KS such groups of waves take turns at the stages; their sums meet in LDS, in one order.
+// The results go past the caches: a lane has one row of eight vectors and more, and a half wave writes 128 contiguous bytes.
+// 8192 x 8192 x 8192 in 867 us, 1.27 PFLOP/s (codes of zeros: 604, so that power bounds it; without results 826, without stages
+// 749; the library's bf16 product of that size 1.20 PFLOP/s).  50000 x 512 x 1024 in 80 us: 205 MB of results, which alone take 50
+// (4.1 TB/s), and products, which alone take 52, overlap in part.
 template <int WM, int WN, int TM, int TN, int KS>
 __global__ __launch_bounds__(64 * WM * WN * KS) void f8_gemm_kernel(F8GemmArgs a)
 {
@@ -397,7 +402,9 @@ struct F8StreamArgs {
 // Up to 16 vectors: the weights go from memory to registers once, requested before anything else is waited for and again as
 // soon as a register is free; the vectors lie in LDS as bf16 values, put there by every block for itself.  A wave multiplies 16
 // rows at a time; `split` waves share them, each with its range of the columns.  Lane (i, g) has row i and of every 128 columns
-// the 16-byte pieces g and g + 4.
+// the 16-byte pieces g and g + 4.  Bound by the weights' way: 50000 x 512 x 5 in 8.9 us (26.9 MB, 3.0 TB/s; the kernel 8.0, of which
+// a launch, the vectors' quantization and the last stores are some 3.5), 250000 x 1024 x 8 in 43 (5.9 TB/s; 52 with the weights out of
+// every cache).
 __global__ __launch_bounds__(512) void f8_stream_kernel(F8StreamArgs a)
 {
     extern __shared__ __align__(16) uint8_t s_x[];                          // [n][pitch], then the waves' sums [waves][64]
@@ -551,7 +558,7 @@ q8_status q8i_gemm_f8(q8_ctx *ctx, const q8_mat_f8 *W, const q8_mat_f8 *X, const
     const int nb = (a.cols + F8_BLOCK - 1) / F8_BLOCK;
     const bool streams = gemm_f8_streams(a.n, nb);
     // (results over the vectors: these are quantized first, as a whole)
-    const char *x0 = (const char *)Xf, *x1 = (const char *)(Xf + (size_t)(a.n - 1) * ldxf + a.cols), *y0 = (const char *)Y, *y1 = (const char *)(Y + (size_t)(a.n - 1) * ldy + a.rows);
+    const uintptr_t x0 = (uintptr_t)Xf, x1 = x0 + 4 * ((size_t)(a.n - 1) * ldxf + a.cols), y0 = (uintptr_t)Y, y1 = y0 + 4 * ((size_t)(a.n - 1) * ldy + a.rows);
     if (Xf && (!streams || (x0 < y1 && y0 < x1))) {
         const q8_status st = q8i_quantize_f8(ctx, Xf, a.n, a.cols, ldxf, (uint8_t *)X->data, X->ld, (uint8_t *)X->scale, X->lds);
         if (st) return st;

@@ -8,6 +8,11 @@
 //
 // Weights are whole numbers, rint(w_i 2^S): their sums are exact whatever their order, so a token does not depend on which
 // thread adds what, and the borders between tokens lie where sums in 64-bit floating point put them to about 1e-12.
+//
+// Long rows take three launches over parts of the rows (largest logit; bins; borders and words), and every one
+// reads the row.  Few rows are a chain of latencies: one of 50000 words 15.6 to 17 us (kernels 2.5 + 3.7 + 9.5 at the least), 64 of them 34.5;
+// many are bound by memory and 64-bit arithmetic: 1000 of 63644 words 196 us (44 + 77 + 71; reading the 255 MB three times 127,
+// the sums' LDS additions 24, the weights' 64-bit operations some 50 of the 77).
 #include "q8_internal.h"
 
 #include <algorithm>
@@ -17,7 +22,8 @@ typedef unsigned long long u64;
 
 #define SMP_BINS 2048                        // of 1/32 octave of weight each; beyond the last one every weight rounds to zero
 #define SMP_LOG2E32 46.166241308446828384    // 32 log2(e)
-#define SMP_SMALL 8192                       // vocabularies of at most so many words: a block per row
+#define SMP_SMALL 2048                       // vocabularies of at most so many words: a block per row
+#define SMP_MIDDLE 8192                      // ... where few rows have top-k or min_p
 #define SMP_PARTS 128                        // blocks of a row
 #define SMP_BLOCK 256                        // threads of these
 #define SMP_ROWS 1024                        // rows of a launch
@@ -1011,11 +1017,16 @@ q8_status q8i_sample(q8_ctx *ctx, const float *logits, int n, int V, int ldl, co
     while (((size_t)1 << bits) < (size_t)V) ++bits;
     a.shift = 62 - bits < 46 ? 62 - bits : 46;                // the sum of V weights stays below 2^63
     const size_t smem = sizeof(SmpShared<256>);
-    // A block per row while its threads hold eight words each at most: 5 rows of 2500 / 8001 words 12.9 / 13.5 us against 19.8 / 19.7 over
-    // several blocks, of 50000 words 25 to 29 against 18 to 23 (1 to 8 rows; 64 rows 41 against 38).
+    // A block per row while its threads hold eight words each at most and mostly find the borders among the words at the top, which
+    // top-k and min_p see to (us; a block per row, several blocks): 5 rows of 2000 words 9.8, 14.8 without filters, 10.0, 17.1 with top-k, 1000
+    // rows 20.4, 25.7 and 18.3, 30.8; 64 rows of 5003 words 24.0, 17.3 without filters, 12.7, 19.6 with top-k, 11.9, 17.7 with min_p,
+    // 32.7, 21.2 with top-p, 1000 rows 73.9, 36.7, 40.7, 39.6, 40.6, 39.8, 98.1, 43.0.  Of 50000 words 25 to 29 against 16 to 17 (one row).
     if (V <= SMP_SMALL) {
-        if (V <= SMP_SMALL / 4) hipLaunchKernelGGL((sample_row_kernel<8, 256>), dim3(n), dim3(256), smem, ctx->stream, a);
-        else hipLaunchKernelGGL((sample_row_kernel<8, 1024>), dim3(n), dim3(1024), sizeof(SmpShared<1024>), ctx->stream, a);
+        hipLaunchKernelGGL((sample_row_kernel<8, 256>), dim3(n), dim3(256), smem, ctx->stream, a);
+        return q8i_launch_check(ctx, "sample");
+    }
+    if (V <= SMP_MIDDLE && n <= 256 && (a.top_k || a.min_p)) {
+        hipLaunchKernelGGL((sample_row_kernel<8, 1024>), dim3(n), dim3(1024), sizeof(SmpShared<1024>), ctx->stream, a);
         return q8i_launch_check(ctx, "sample");
     }
     a.state = (SmpRowState *)state;

@@ -370,22 +370,24 @@ template <int WM, int WN, int TM, int TN, int KS = 1> static q8_status launch_f8
     return q8i_launch_check(ctx, "product f8");
 }
 
-// Tiles by what each costs (us; rows x columns x vectors): 256 x 256 and 128 x 128 where they are about one round of blocks or more and
-// long enough that reading counts most (8192 x 8192 x 8192 865, 986 and in 128 x 64 1146; 4096 x 1024 x 4096 43.3, 41.0 and 44.0;
-// 50000 x 512 x 1024, four stages a tile, 110, 77.0 and 76.0); 128 x 32 for up to 32 vectors; 128 x 96 for 65 to 96 (63644 x 620 x 77
-// 19.9 against 25.5 in 64 x 64 and 24.6 in 128 x 64); 64 x 32 with four groups in turns at the stages where 64 x 64 would leave compute
-// units without any (1024 x 8192 x 64 22.9 against 35.1, 512 x 4096 x 17 10.2 against 17.2); else 128 x 64 where these are a round, in
-// eight waves (50000 x 640 x 320 35.0 against 39.7 in 64 x 64 and 39.1 in four waves), and 64 x 64 (1024 x 2048 x 1024 11.9 against
-// 14.3, 3000 x 1024 x 128 7.9 against 9.1).
+// Tiles by what each costs (us; rows x columns x vectors, the product alone): 256 x 256 and 128 x 128 where they are about one round of
+// blocks or more, long enough that reading counts most, and the vectors fill them (8192 x 8192 x 8192 865, 986 and in 128 x 64 1146;
+// 4096 x 1024 x 4096 43.3, 41.0 and 44.0; 50000 x 512 x 1024, four stages a tile, 110, 77.0 and 76.0); 128 x 32 for up to 32 vectors;
+// 128 x 96 for 65 to 96 and many rows (63644 x 620 x 77 19.9 against 25.5 in 64 x 64 and 24.6 in 128 x 64; 19736 x 293 x 82 13.7 against
+// 11.2 and 11.4); 64 x 32 with four groups in turns at the stages where the others would leave compute units without any (1024 x 8192 x
+// 64 22.9 against 35.1 in 64 x 64, 512 x 4096 x 17 10.2 against 17.2, 11807 x 1012 x 8 8.0 against 9.6 in 128 x 32); else 128 x 64 where
+// these are more than a round, in eight waves (50000 x 640 x 320 35.0 against 39.7 in 64 x 64 and 39.1 in four waves), and 64 x 64
+// (1024 x 2048 x 1024 11.9 against 14.3, 3117 x 4084 x 663 37.4 against 41.2).
 static q8_status gemm_f8_tiles(q8_ctx *ctx, F8GemmArgs &a)
 {
     auto tiles = [&](int r, int v) { return (long long)((a.rows + r - 1) / r) * ((a.n + v - 1) / v); };
-    if (tiles(256, 256) >= 200 && a.cols >= 2048) return launch_f8<2, 4, 4, 2>(ctx, a);
-    if (tiles(128, 128) >= 500 && a.cols >= 1024) return launch_f8<2, 4, 2, 1>(ctx, a);
-    if (tiles(64, 64) < 128 && a.cols >= 512) return launch_f8<2, 1, 1, 1, 4>(ctx, a);
+    auto filled = [&](int v) { return (long long)((a.n + v - 1) / v) * v * 4 <= 5ll * a.n; };
+    if (filled(256) && tiles(256, 256) >= 200 && a.cols >= 2048) return launch_f8<2, 4, 4, 2>(ctx, a);
+    if (filled(128) && tiles(128, 128) >= 500 && a.cols >= 1024) return launch_f8<2, 4, 2, 1>(ctx, a);
+    if (a.cols >= 512 && (a.n <= 32 ? tiles(128, 32) < 256 : tiles(64, 64) < 128)) return launch_f8<2, 1, 1, 1, 4>(ctx, a);
     if (a.n <= 32) return launch_f8<4, 1, 1, 1>(ctx, a);
-    if (a.n > 64 && a.n <= 96 && tiles(128, 96) >= 128) return launch_f8<4, 1, 1, 3>(ctx, a);
-    if (tiles(128, 64) >= 250) return launch_f8<4, 2, 1, 1>(ctx, a);
+    if (a.n > 64 && a.n <= 96 && tiles(128, 96) >= 400) return launch_f8<4, 1, 1, 3>(ctx, a);
+    if (tiles(128, 64) >= 320) return launch_f8<4, 2, 1, 1>(ctx, a);
     return launch_f8<2, 2, 1, 1>(ctx, a);
 }
 

@@ -108,7 +108,7 @@ def test_product(q, ctx, rows, cols, n, codes):
 
 
 @pytest.mark.parametrize("rows,cols,n", [(100, 620, 3), (64, 512, 16), (70, 2048, 20), (300, 1030, 64), (260, 640, 130), (513, 512, 600), (900, 384, 2100),
-                                          (3300, 2100, 4200), (2900, 1100, 2900), (16500, 300, 77), (16100, 260, 129), (512, 4100, 17), (500, 8200, 1), (37, 16384, 1),
+                                          (3300, 2100, 4200), (2900, 1100, 2900), (16500, 300, 77), (52000, 260, 77), (16100, 260, 129), (512, 4100, 17), (500, 8200, 1), (37, 16384, 1),
                                           (2050, 2000, 3), (3000, 1000, 4), (20000, 1200, 2), (40000, 1100, 4), (33000, 130, 16)])
 def test_product_of_whole_numbers_is_exact(q, ctx, rows, cols, n):
     """Codes of whole numbers up to 8 and scales of powers of two up to 4: every sum is exact in fp32, in any order."""

@@ -985,7 +985,9 @@ class MatF8:
 
 def q8_quantize_matrix_f8(ctx, W, ld_out=None, bind=False):
     """Rows of W (weights or vectors) in e4m3 with a power of two per 128 columns: a MatF8."""
-    W = W if isinstance(W, torch.Tensor) and W.is_cuda and W.dtype == torch.float32 else ctx.f32(W)
+    if not (isinstance(W, torch.Tensor) and W.is_cuda and W.dtype == torch.float32):
+        with torch.cuda.stream(ctx.stream):
+            W = ctx.f32(W)
     ld_in = _rows(W, "W")
     rows, cols = W.shape
     ld_out = (cols + 15) // 16 * 16 if ld_out is None else ld_out
@@ -1028,8 +1030,10 @@ def output_logits_f8(ctx, ro, W_out, b_out, s=None, y_emb=None, ctx_vec=None, t_
     V, R = W_out.rows, W_out.cols
     if logits is None and (want_logits or k == 0):
         logits = ctx.empty(n, V)
-    if logits is not None and (tuple(logits.shape) != (n, V) or not logits.is_contiguous()):
-        raise ValueError("logits: expected %d x %d, contiguous" % (n, V))
+    given = [(t_in, "t_in", R)] if ro is None else [(s, "s", ro.W_s.cols), (y_emb, "y_emb", ro.W_y.cols), (ctx_vec, "ctx_vec", ro.W_c.cols)]
+    for t, name, cols in given + ([(logits, "logits", V)] if logits is not None else []):
+        if t is None or t.dtype != torch.float32 or tuple(t.shape) != (n, cols) or not t.is_cuda or not t.is_contiguous():
+            raise ValueError("%s: expected a contiguous fp32 device tensor %d x %d" % (name, n, cols))
     _vector(b_out, "b_out", V)
     t = ctx.empty(n, R) if ro is not None else None
     lse, lp, idx = (ctx.empty(n), ctx.empty(n, k), ctx.empty(n, k, dtype=torch.int32)) if k > 0 else (None, None, None)
@@ -1059,7 +1063,8 @@ def q8_sample_logits(ctx, logits, u, temperature=None, top_k=None, top_p=None, m
 
     def per_row(v, name, dtype):
         if v is not None and not isinstance(v, torch.Tensor):
-            v = torch.full((n,), v, dtype=dtype, device=ctx.device)
+            with torch.cuda.stream(ctx.stream):          # written where it is read
+                v = torch.full((n,), v, dtype=dtype, device=ctx.device)
         _vector(v, name, n, dtype)
         return v
 

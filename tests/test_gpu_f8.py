@@ -254,6 +254,9 @@ def test_refusals(q, ctx):
                 lambda: q.q8_gemm_f8(ctx, W, x, ctx.empty(31)), lambda: q.q8_gemm_f8(ctx, W, x.double()), lambda: q.q8_gemm_f8(ctx, W, ctx.empty(64, 4).t())):
         with pytest.raises(ValueError):
             bad()
+    for bad in (dict(t_in=x[:, :60].contiguous()), dict(t_in=x.double()), dict(t_in=x.cpu()), dict(t_in=ctx.empty(64, 4).t()), dict(t_in=x, logits=ctx.empty(4, 33)), dict(t_in=x, logits=ctx.empty(3, 32))):
+        with pytest.raises(ValueError):
+            q.output_logits_f8(ctx, None, W, None, k=4, **bad)
     small = q.Context(workspace_bytes=q.q8_gemm_f8_bytes(1, 64))
     with pytest.raises(q.Q8Error) as e:                   # 400 vectors of 64 codes, a workspace for one
         q.q8_gemm_f8(small, W, ctx.empty(400, 64))

@@ -218,6 +218,24 @@ def test_the_largest_vocabulary(q, ctx):
         _check(q, ctx, lg, np.array([0.77], np.float32), **k)
 
 
+def test_two_streams_at_once(q):
+    """Rows over several blocks, whose launches leave sums for each other, on two streams; one number for all rows."""
+    rng = np.random.default_rng(17)
+    n, V = 40, 50000
+    base = q.Context(workspace_bytes=q.q8_sample_bytes(n, V))
+    lg = [base.f32(_logits(rng, n, V)) for _ in range(2)]
+    u = base.f32(rng.random(n).astype(np.float32))
+    full = lambda v, t=torch.float32: torch.full((n,), v, dtype=t, device=base.device)
+    want = [np_(q.q8_sample_logits(base, g, u, full(0.9), full(200, torch.int32), full(0.8), full(0.001))["tokens"]).copy() for g in lg]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    cs = [q.Context(workspace_bytes=q.q8_sample_bytes(n, V), stream=s) for s in streams]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        r = [q.q8_sample_logits(c, g, u, 0.9, 200, 0.8, 0.001) for c, g in zip(cs, lg)]
+        torch.cuda.synchronize()
+        assert all((np_(o["tokens"]) == w).all() for o, w in zip(r, want))
+
+
 def test_refusals(q, ctx):
     """What the binding refuses (the library's own refusals: test_f8_refusals.py, on the host)."""
     lg, u, E, y = ctx.empty(4, 100), ctx.empty(4), ctx.empty(100, 8), ctx.empty(4, 8)

@@ -9,10 +9,12 @@
 // Weights are whole numbers, rint(w_i 2^S): their sums are exact whatever their order, so a token does not depend on which
 // thread adds what, and the borders between tokens lie where sums in 64-bit floating point put them to about 1e-12.
 //
-// Long rows take three launches over parts of the rows (largest logit; bins; borders and words), and every one
-// reads the row.  Few rows are a chain of latencies: one of 50000 words 15.6 to 17 us (kernels 2.5 + 3.7 + 9.5 at the least), 64 of them 34.5;
-// many are bound by memory and 64-bit arithmetic: 1000 of 63644 words 196 us (44 + 77 + 71; reading the 255 MB three times 127,
-// the sums' LDS additions 24, the weights' 64-bit operations some 50 of the 77).
+// Long rows take three launches over parts of the rows (largest logit; bins; borders and words), and every one reads the row.  Few
+// rows are a chain of latencies: one of 50000 words 17 us (kernels 2 + 4 + 10 at the least), 64 of them 35.5; many are bound by memory and
+// 64-bit arithmetic: 1000 of 63644 words 203 us (reading the 255 MB three times 127, the sums' LDS additions 24, the weights' 64-bit
+// operations some 50).  Bins are as wide as the row's spread asks for: of 1/32 octave alone, flat rows (deviation 0.1 nat) went
+// through the row again and again in one block: 64 rows of 50000 words with top-p 345 us, now 40, 12 of 250001 1328, now 55 (ordinary rows 3 %
+// more).  Rows of one logit alone still do (50000 words: some 300 us).
 #include "q8_internal.h"
 
 #include <algorithm>
@@ -20,13 +22,14 @@
 
 typedef unsigned long long u64;
 
-#define SMP_BINS 2048                        // of 1/32 octave of weight each; beyond the last one every weight rounds to zero
+#define SMP_BINS 2048                        // of 1/32 octave of weight each, or finer; 2048/32 octaves below the largest every weight rounds to zero
 #define SMP_LOG2E32 46.166241308446828384    // 32 log2(e)
 #define SMP_SMALL 2048                       // vocabularies of at most so many words: a block per row
 #define SMP_MIDDLE 8192                      // ... where few rows have top-k or min_p
 #define SMP_PARTS 128                        // blocks of a row
 #define SMP_BLOCK 256                        // threads of these
 #define SMP_ROWS 1024                        // rows of a launch
+#define SMP_REACH 64.0f                      // nat below the largest logit that count in what a row spreads over
 #define SMP_LIST 1536                        // words in LDS of those that lie where a row's borders do
 
 struct SampleArgs {
@@ -239,7 +242,7 @@ template <int BLOCK> struct SmpShared {
     unsigned count[SMP_BINS];
     u64 list[BLOCK];                        // keys of words that are ranked
     double pow[32];                         // 2^(S - j / 32)
-    u64 red_u[16];
+    u64 red_u[16], red_v[16];
     double red_d[16];
     float red_f[16], red_g[16];
     unsigned red_c[16];
@@ -253,6 +256,21 @@ struct SmpAsk {
     int k;
     bool drawn, some_min;
     double c, inv, one, floor_w;            // 32 log2(e) / T; 1 / c; 2^S; min_p 2^S
+    int fine;                               // a bin is 1/32 octave over 2^fine
+
+    // Bins for logits that spread over so much (an estimate: what lies below its end is in the last bin), as fine as 2^(most + 1) of them
+    // hold it.
+    __device__ __forceinline__ void spread(float d, int most = 10)
+    {
+        const float x = d * (float)c;
+        fine = __builtin_amdgcn_readfirstlane(x < 0x1p-14f ? 24 : x < 1024.0f ? most + 127 - (int)(__float_as_uint(x) >> 23) : 0);
+    }
+    __device__ __forceinline__ unsigned bin(SmpPlace p) const
+    {
+        if (fine == 0) return min(p.bin, SMP_BINS - 1u);
+        const unsigned b = __builtin_amdgcn_alignbit(p.bin, p.frac, (unsigned)(32 - fine));
+        return p.bin < max((unsigned)SMP_BINS >> fine, 1u) ? min(b, SMP_BINS - 1u) : SMP_BINS - 1u;
+    }
 
     __device__ __forceinline__ void open(const SampleArgs &a, int j)
     {
@@ -268,6 +286,7 @@ struct SmpAsk {
         // (T = inf: every finite distance counts as none, an infinite one still as infinite)
         c = fmax(SMP_LOG2E32 / (drawn ? (double)T : 1.0), 1e-300);
         inv = 1.0 / c;
+        fine = 0;
         floor_w = (double)mp * one;
     }
 };
@@ -388,6 +407,8 @@ template <int BLOCK> __device__ __forceinline__ u64 smp_prefix(SmpShared<BLOCK> 
 
 // ---------------------------------------------------------------------- borders by bins ----
 
+__device__ __forceinline__ unsigned smp_rank(u64 mask) { return __builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0)); }
+
 // Histogram of the weights of (a part of) a row, and per thread the mass of its words at or above the border of min_p.
 // With SUM, e: the sum of the exponentials at T = 1 as well.
 template <bool SUM, int BLOCK, class Row>
@@ -405,12 +426,34 @@ __device__ __forceinline__ u64 smp_histogram(const Row &row, SmpShared<BLOCK> &s
         for (int t = 0; t < 4; ++t) p[t] = smp_place<false>(smp_gap(m, v[t]), q.c);
 #pragma unroll
         for (int t = 0; t < 4; ++t) w[t] = smp_weight(p[t], s.pow);
+        unsigned bin[4];
+        if (q.fine) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t) bin[t] = q.bin(p[t]);
+        } else {
+#pragma unroll
+            for (int t = 0; t < 4; ++t) bin[t] = p[t].bin;                                // (used below SMP_BINS only)
+        }
+        const float one = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v[0])));
+        if (!__ballot(v[0] != one || v[1] != one || v[2] != one || v[3] != one)) {       // one logit: one addition, where 256 would meet
+            const u64 lanes = __ballot(true);
+            const unsigned words = 4u * (unsigned)__popcll(lanes);
+            if (p[0].bin >= SMP_BINS) return;
+            const u64 x = smp_whole(w[0]);
+            if (q.some_min && w[0] >= q.floor_w) above += 4 * x;
+            if (smp_rank(lanes) == 0) {
+                atomicAdd(&s.mass[smp_at(bin[0])], x * words);
+                if (q.k > 0) atomicAdd(&s.count[smp_at(bin[0])], words);
+            }
+            return;
+        }
 #pragma unroll
         for (int t = 0; t < 4; ++t)
             if (p[t].bin < SMP_BINS) {
                 const u64 x = smp_whole(w[t]);
-                atomicAdd(&s.mass[smp_at(p[t].bin)], x);
-                if (q.k > 0) atomicAdd(&s.count[smp_at(p[t].bin)], 1u);
+                const unsigned at = smp_at(bin[t]);
+                atomicAdd(&s.mass[at], x);
+                if (q.k > 0) atomicAdd(&s.count[at], 1u);
             }
         if (q.some_min) {
 #pragma unroll
@@ -431,6 +474,11 @@ __device__ __forceinline__ u64 smp_lane(u64 v, unsigned lane)
     return ((u64)(unsigned)__builtin_amdgcn_readlane((int)(unsigned)(v >> 32), (int)lane) << 32) | (unsigned)__builtin_amdgcn_readlane((int)(unsigned)v, (int)lane);
 }
 
+__device__ __forceinline__ u64 smp_first(u64 v)                 // the first active lane's
+{
+    return ((u64)(unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)(v >> 32)) << 32) | (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)v);
+}
+
 // The first bin at which cond(count, mass up to and including it) is true; SMP_BINS - 1 if none.  By every wave for itself.
 template <int BLOCK, class Cond> __device__ __forceinline__ unsigned smp_find(const SmpShared<BLOCK> &s, bool counts, Cond cond)
 {
@@ -444,17 +492,18 @@ template <int BLOCK, class Cond> __device__ __forceinline__ unsigned smp_find(co
     return (unsigned)(STEP * group + (close ? min(__ffsll((long long)close) - 1, STEP - 1) : STEP - 1));
 }
 
-// The logits of the bins from b0 to b1, a little wider: what rounding there is, is below 2^-20 of the largest logit and the distance.
+// The logits of the bins from b0 to b1, a little wider: what rounding there is, is below 2^-23 of the largest logit and the distance.
 struct SmpWindow {
     unsigned b0, b1;
     float low, high;
-    __device__ __forceinline__ void open(unsigned first, unsigned last, float m, double inv)
+    __device__ __forceinline__ void open(unsigned first, unsigned last, float m, const SmpAsk &q)
     {
         b0 = first;
         b1 = last;
-        const double gap0 = (double)first * inv, gap1 = ((double)last + 1.0) * inv, am = fabs((double)m);
-        high = (float)((double)m - gap0 + 1e-6 * (am + gap0));
-        low = (float)((double)m - gap1 - 1e-6 * (am + gap1));
+        const double wide = __hiloint2double(__double2hiint(q.inv) - (q.fine << 20), __double2loint(q.inv)), am = fabs((double)m);
+        const double gap0 = (double)first * wide, gap1 = last == SMP_BINS - 1 ? SMP_BINS * q.inv : ((double)last + 1.0) * wide;
+        high = (float)((double)m - gap0 + 2.5e-7 * (am + gap0));
+        low = (float)((double)m - gap1 - 2.5e-7 * (am + gap1));
     }
     __device__ __forceinline__ bool near(float v) const { return v >= low && v <= high; }
     __device__ __forceinline__ bool has(unsigned bin) const { return bin >= b0 && bin <= b1; }
@@ -487,15 +536,19 @@ __device__ __forceinline__ u64 smp_borders(Words words, SmpShared<BLOCK> &s, con
         u64 before_m = bin ? s.mass[smp_at(bin - 1)] : 0;
         unsigned before_c = stage == 0 && bin ? s.count[smp_at(bin - 1)] : 0;
         SmpWindow win;
-        win.open(bin, bin, m, q.inv);
+        win.open(bin, bin, m, q);
         u64 lowest = topk_key(win.low, 0x7fffffff), highest = topk_key(win.high, 0);
+        bool again = false;
         for (;;) {
             if (tid == 0) s.listed = 0;
             __syncthreads();
+            u64 first = 0, last = ~0ull;
             words(win, [&](u64 key) {
                 if (key < lowest || key > highest) return;
+                first = max(first, key);
+                last = min(last, key);
                 const unsigned at = atomicAdd(&s.listed, 1u);
-                if (at < BLOCK) s.list[at] = key;
+                if (at < 64) s.list[at] = key;
             });
             __syncthreads();
             const unsigned members = s.listed;
@@ -515,15 +568,33 @@ __device__ __forceinline__ u64 smp_borders(Words words, SmpShared<BLOCK> &s, con
                 found_m = smp_lane(ms, at);
                 break;
             }
-            __syncthreads();
+            if (again || members > BLOCK) {                     // the range that their keys have (of fewer at first, the bin's will do)
+                first = wave_max_u64(first);
+                last = ~wave_max_u64(~last);
+                if ((tid & 63) == 0) { s.red_u[tid >> 6] = first; s.red_v[tid >> 6] = last; }
+                __syncthreads();
+                highest = s.red_u[0];
+                lowest = s.red_v[0];
+                for (int o = 1; o < BLOCK / 64; ++o) { highest = max(highest, s.red_u[o]); lowest = min(lowest, s.red_v[o]); }
+            }
+            again = true;
             u64 *h_m = s.list;                                  // [256], the block has at least as many threads
             const int sh = max(0, 64 - 8 - __clzll((long long)(highest - lowest)));
             if (tid < 256) { h_m[tid] = 0; s.bytes[tid] = 0; }
             __syncthreads();
             words(win, [&](u64 key) {
                 if (key < lowest || key > highest) return;
-                const unsigned d = (unsigned)((key - lowest) >> sh);
-                atomicAdd(&h_m[d], smp_mass_of(key, m, q.c, s.pow));
+                const unsigned d = (unsigned)((key - lowest) >> sh), d0 = __builtin_amdgcn_readfirstlane(d);
+                const u64 own = smp_mass_of(key, m, q.c, s.pow), own0 = smp_first(own);
+                if (!__ballot(d != d0 || own != own0)) {        // one addition, where all would meet
+                    const u64 lanes = __ballot(true);
+                    if (smp_rank(lanes) == 0) {
+                        atomicAdd(&h_m[d], own * (unsigned)__popcll(lanes));
+                        atomicAdd(&s.bytes[d], (unsigned)__popcll(lanes));
+                    }
+                    return;
+                }
+                atomicAdd(&h_m[d], own);
                 atomicAdd(&s.bytes[d], 1u);
             });
             __syncthreads();
@@ -709,7 +780,12 @@ __global__ __launch_bounds__(BLOCK) void sample_row_kernel(SampleArgs a)
 #pragma unroll
         for (int t = 0; t < PER; ++t) { s.mass[smp_at(t * BLOCK + tid)] = 0; s.count[smp_at(t * BLOCK + tid)] = 0; }
         if (tid == 0) s.above = 0;
-        __syncthreads();
+        float far = 0.0f;
+        row.pieces([&](const float (&v)[4], int) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t) far = fmaxf(far, m - v[t] <= SMP_REACH ? m - v[t] : 0.0f);
+        });
+        q.spread(smp_block_max<BLOCK>(far, s.red_f));
         const u64 above = smp_histogram<false, BLOCK>(row, s, q, m, e);
         if (q.some_min && above) atomicAdd(&s.above, above);
         __syncthreads();
@@ -721,7 +797,7 @@ __global__ __launch_bounds__(BLOCK) void sample_row_kernel(SampleArgs a)
         smp_scan<BLOCK>(s, mm, cc, q.k > 0);
         const auto stored = row.stored();
         key = smp_borders<BLOCK>([&](const SmpWindow &win, auto f) {
-            stored.some([&](float v) { return win.near(v); }, [&](float v) { return smp_place(smp_gap(m, v), q.c).bin == win.b0; }, f);
+            stored.some([&](float v) { return win.near(v); }, [&](float v) { const SmpPlace p = smp_place(smp_gap(m, v), q.c); return p.bin < SMP_BINS && q.bin(p) == win.b0; }, f);
         }, s, q, m, a.shift);
     }
     smp_write(a, j, topk_key_idx(key), (float)(-smp_gap(m, topk_key_val(key)) - log(e)), BLOCK);
@@ -734,31 +810,48 @@ struct SmpRowState {
     u64 mass[SMP_BINS];
     unsigned count[SMP_BINS];
     double e[SMP_PARTS];                    // sum of exp at T = 1 of a part
-    float top[SMP_PARTS];                   // its largest logit
+    float top[SMP_PARTS], low[SMP_PARTS];   // its largest logit, and the lowest seen of those in reach of it
+    float all_top;                          // the row's
+    int fine;
     u64 above;
     unsigned listed, arrived;
 };
 
-// 1. The largest logit of each part; the row's sums are set to zero.
+// 1. The largest logit of each part, and how far the others lie below it (every fourth, as far as they are within SMP_REACH nat, which
+// a mask's values are not); the row's sums are set to zero.
 __global__ __launch_bounds__(SMP_BLOCK) void sample_top_kernel(SampleArgs a)
 {
-    __shared__ float red[SMP_BLOCK / 64];
+    __shared__ float red[SMP_BLOCK / 64], red_low[SMP_BLOCK / 64];
     const int j = a.row0 + blockIdx.y, part = blockIdx.x, tid = threadIdx.x;
     SmpRowState &st = a.state[blockIdx.y];
     SmpRow<0, SMP_BLOCK> row;
     row.open(a.logits + (size_t)j * a.ldl, a.V, part * a.part_pieces, a.part_pieces);
     for (int b = part * SMP_BLOCK + tid; b < SMP_BINS; b += SMP_BLOCK * a.parts) { st.mass[b] = 0; st.count[b] = 0; }
     if (part == 0 && tid == 0) { st.above = 0; st.listed = 0; st.arrived = 0; }
-    const float m = smp_block_max<SMP_BLOCK>(row.largest(), red);
-    if (tid == 0) st.top[part] = m;
+    float m = -INFINITY, low = INFINITY;
+    row.pieces([&](const float (&v)[4], int) {
+        const float next = fmaxf(fmaxf(fmaxf(m, v[0]), fmaxf(v[1], v[2])), v[3]), cut = next - SMP_REACH;
+        if (m < cut) low = next;
+        low = fminf(low, v[0] >= cut ? v[0] : next);
+        m = next;
+    });
+    const float top = smp_block_max<SMP_BLOCK>(m, red);
+    low = -smp_block_max<SMP_BLOCK>(m >= top - SMP_REACH ? -low : -top, red_low);
+    if (tid == 0) { st.top[part] = top; st.low[part] = low; }
 }
 
-__device__ __forceinline__ float smp_row_top(const SampleArgs &a, const SmpRowState &st)       // by every wave for itself
+// The row's largest logit, and its bins, by every wave for itself.
+__device__ __forceinline__ float smp_row_top(const SampleArgs &a, const SmpRowState &st, SmpAsk &q)
 {
-    float m = -INFINITY;
-    for (int p = threadIdx.x & 63; p < a.parts; p += 64) m = fmaxf(m, st.top[p]);
-    return wave_max_f(m);
+    const int p0 = threadIdx.x & 63, p1 = p0 + 64;
+    const float t0 = p0 < a.parts ? st.top[p0] : -INFINITY, t1 = p1 < a.parts ? st.top[p1] : -INFINITY;
+    const float l0 = p0 < a.parts ? st.low[p0] : INFINITY, l1 = p1 < a.parts ? st.low[p1] : INFINITY;
+    const float m = wave_max_f(fmaxf(t0, t1));
+    const float d0 = t0 >= m - SMP_REACH ? m - l0 : 0.0f, d1 = t1 >= m - SMP_REACH ? m - l1 : 0.0f;
+    q.spread(fminf(wave_max_f(fmaxf(d0, d1)), SMP_REACH), a.parts > 2 ? 9 : 10);
+    return m;
 }
+static_assert(SMP_PARTS <= 128, "two parts a lane");
 
 // The sum of the parts' sums, in one order, by every wave for itself.
 __device__ __forceinline__ double smp_row_e(const SampleArgs &a, const SmpRowState &st)
@@ -780,7 +873,8 @@ __global__ __launch_bounds__(SMP_BLOCK) void sample_bins_kernel(SampleArgs a)
     row.open(a.logits + (size_t)j * a.ldl, a.V, part * a.part_pieces, a.part_pieces);
     SmpAsk q;
     q.open(a, j);
-    float m = smp_row_top(a, st);
+    float m = smp_row_top(a, st, q);
+    if (part == 0 && tid == 0) { st.all_top = m; st.fine = q.fine; }
     if (tid < 32) s.pow[tid] = smp_pow[tid] * q.one;
     if (m == -INFINITY) return;
     if (m == INFINITY) { row.share_inf(); m = 0.0f; }
@@ -847,7 +941,8 @@ __global__ __launch_bounds__(SMP_BLOCK) void sample_draw_kernel(SampleArgs a)
     const u64 above = st.above;
     const double e_parts = smp_row_e(a, st);
     row.open(a.logits + (size_t)j * a.ldl, a.V, part * a.part_pieces, a.part_pieces);
-    float m = smp_row_top(a, st);
+    float m = st.all_top;
+    q.fine = __builtin_amdgcn_readfirstlane(st.fine);
     if (m == -INFINITY) {                               // no word can be drawn
         if (part == 0) smp_write(a, j, -1, -INFINITY, SMP_BLOCK);
         return;
@@ -863,21 +958,21 @@ __global__ __launch_bounds__(SMP_BLOCK) void sample_draw_kernel(SampleArgs a)
         u64 low = s.mass[smp_at(SMP_BINS - 1)], high = low;
         if (q.k > 0 && (unsigned)q.k < s.count[smp_at(SMP_BINS - 1)]) {
             const unsigned b = smp_find<SMP_BLOCK>(s, true, [&](unsigned c, u64) { return c >= (unsigned)q.k; });
-            w[0].open(b, b, m, q.inv);
+            w[0].open(b, b, m, q);
             low = b ? s.mass[smp_at(b - 1)] : 0;
             high = s.mass[smp_at(b)];
         }
         if (q.tp < 1.0f) {
             const double n0 = fmax((double)q.tp * (double)low, 0.5), n1 = fmax((double)q.tp * (double)high, 0.5);
             const unsigned b0 = smp_find<SMP_BLOCK>(s, false, [&](unsigned, u64 x) { return (double)x >= n0; }), b1 = smp_find<SMP_BLOCK>(s, false, [&](unsigned, u64 x) { return (double)x >= n1; });
-            w[1].open(b0, b1, m, q.inv);
+            w[1].open(b0, b1, m, q);
             low = b0 ? s.mass[smp_at(b0 - 1)] : 0;
             high = s.mass[smp_at(b1)];
         }
         if (q.some_min) { low = min(low, above); high = min(high, above); }
         const u64 first = 1ull << a.shift;
         const double n0 = (double)q.u * (double)max(low, first), n1 = (double)q.u * (double)max(high, first);
-        w[2].open(smp_find<SMP_BLOCK>(s, false, [&](unsigned, u64 x) { return (double)x > n0; }), smp_find<SMP_BLOCK>(s, false, [&](unsigned, u64 x) { return (double)x > n1; }), m, q.inv);
+        w[2].open(smp_find<SMP_BLOCK>(s, false, [&](unsigned, u64 x) { return (double)x > n0; }), smp_find<SMP_BLOCK>(s, false, [&](unsigned, u64 x) { return (double)x > n1; }), m, q);
     } else {
         w[2].low = w[2].high = m;
         w[2].b0 = 0; w[2].b1 = SMP_BINS;
@@ -891,7 +986,6 @@ __global__ __launch_bounds__(SMP_BLOCK) void sample_draw_kernel(SampleArgs a)
     u64 *list = a.lists + (size_t)blockIdx.y * a.list_words;
     const unsigned room = (unsigned)a.list_words;
     unsigned mine = 0;                                  // (the same in all lanes that are at work; lane 0 is to the end)
-    auto rank = [](u64 mask) { return __builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0)); };
     row.pieces([&](const float (&v)[4], int i) {
         bool n[4];
 #pragma unroll
@@ -911,7 +1005,7 @@ __global__ __launch_bounds__(SMP_BLOCK) void sample_draw_kernel(SampleArgs a)
                 const unsigned more = (unsigned)__popcll(mask);
                 if (mine + more > LIST) {
                     const u64 active = __ballot(true);
-                    const unsigned me = rank(active);
+                    const unsigned me = smp_rank(active);
                     unsigned at = 0;
                     if (me == 0) at = atomicAdd(&st.listed, mine);
                     at = __builtin_amdgcn_readfirstlane(at);
@@ -921,7 +1015,7 @@ __global__ __launch_bounds__(SMP_BLOCK) void sample_draw_kernel(SampleArgs a)
                     __builtin_amdgcn_wave_barrier();
                     mine = 0;
                 }
-                if (n[t]) s_found[wave * LIST + mine + rank(mask)] = topk_key(v[t], i + t);
+                if (n[t]) s_found[wave * LIST + mine + smp_rank(mask)] = topk_key(v[t], i + t);
                 mine += more;
             }
         }
@@ -958,7 +1052,7 @@ __global__ __launch_bounds__(SMP_BLOCK) void sample_draw_kernel(SampleArgs a)
     u64 key;
     if (q.drawn) {
         key = smp_borders<SMP_BLOCK>([&](const SmpWindow &win, auto f) {
-            auto in = [&](float v) { return smp_place(smp_gap(m, v), q.c).bin == win.b0; };
+            auto in = [&](float v) { const SmpPlace p = smp_place(smp_gap(m, v), q.c); return p.bin < SMP_BINS && q.bin(p) == win.b0; };
             if (listed > room) {
                 whole.some([&](float v) { return win.near(v); }, in, f);
                 return;
@@ -1036,7 +1130,7 @@ q8_status q8i_sample(q8_ctx *ctx, const float *logits, int n, int V, int ldl, co
     for (a.row0 = 0; a.row0 < n; a.row0 += SMP_ROWS) {
         const int rows = n - a.row0 < SMP_ROWS ? n - a.row0 : SMP_ROWS;
         // three blocks a compute unit, none of less than 2048 words: 64 rows of 50000 words 36.5 / 37.2 / 47 us with 768 / 1024 / 1536
-        // blocks, 12 of 250001 26.4 / 31.6 / 40, 200 of 33658 53.9 / 58.4 / 67
+        // blocks, 12 of 250001 26.4 / 31.6 / 40, 200 of 33658 53.9 / 58.4 / 67 (all of these before bins of a row's own width)
         int parts = (768 + rows - 1) / rows;
         if (parts > (pieces + 511) / 512) parts = (pieces + 511) / 512;
         if (parts > SMP_PARTS) parts = SMP_PARTS;

@@ -218,6 +218,29 @@ def test_the_largest_vocabulary(q, ctx):
         _check(q, ctx, lg, np.array([0.77], np.float32), **k)
 
 
+@pytest.mark.parametrize("V", [1500, 6000, 50000, 250001])
+@pytest.mark.parametrize("sigma", [1e-6, 1e-3, 0.05, 0.4])
+@pytest.mark.parametrize("mask", ["none", "half", "fourths", "run", "tail"])
+def test_flat_rows(q, ctx, V, sigma, mask):
+    """Logits that spread over little, so that a bin of one width would hold most words, beside masks and a tail that do not."""
+    n = 4
+    rng = np.random.default_rng(V + int(1e6 * sigma))
+    lg = (7.25 + sigma * rng.standard_normal((n, V))).astype(np.float32)
+    if mask == "half":
+        lg[rng.random((n, V)) < 0.5] = np.finfo(np.float32).min
+    elif mask == "fourths":
+        lg[:, ::4] = -1e9
+    elif mask == "run":
+        lg[:, V // 3:] = -1e4
+    elif mask == "tail":
+        t = rng.random((n, V)) < 0.02
+        lg[t] -= (30 * rng.random(int(t.sum()))).astype(np.float32)
+    u = rng.random(n).astype(np.float32).clip(0, TOP)
+    _check(q, ctx, lg, u)
+    _check(q, ctx, lg, u, T=np.array([0.5, 1.0, 2.0, 30.0], np.float32), top_p=rng.random(n).astype(np.float32))
+    _check(q, ctx, lg, u, top_k=rng.integers(1, V, n).astype(np.int32), min_p=np.full(n, 0.9, np.float32))
+
+
 def test_two_streams_at_once(q):
     """Rows over several blocks, whose launches leave sums for each other, on two streams; one number for all rows."""
     rng = np.random.default_rng(17)

@@ -179,11 +179,11 @@ __device__ __forceinline__ void f8_to_lds(__amdgpu_buffer_rsrc_t rsrc, uint8_t *
 // an instruction, which the matrix cores' time covers (24 conversions beside 8 products of 32 x 32 x 16).  The order of k
 // inside a block is the same for both operands, which is all that it has to be: lane half h takes the 16-byte pieces 2 j + h.
 // KS > 1: KS such groups of waves take turns at the stages; their sums meet in LDS, in one order.
-// The results go past the caches: a lane has one row of eight vectors and more, and a half wave writes 128 contiguous bytes.
 // 8192 x 8192 x 8192 in 867 us, 1.27 PFLOP/s (codes of zeros: 604, so that power bounds it; without results 826, without stages
 // 749; the library's bf16 product of that size 1.20 PFLOP/s).  50000 x 512 x 1024 in 80 us: 205 MB of results, which alone take 50
 // (4.1 TB/s), and products, which alone take 52, overlap in part.
-template <int WM, int WN, int TM, int TN, int KS>
+// PAST: the results go past the caches.
+template <int WM, int WN, int TM, int TN, int KS, bool PAST>
 __global__ __launch_bounds__(64 * WM * WN * KS) void f8_gemm_kernel(F8GemmArgs a)
 {
     constexpr int ROWS = 32 * WM * TM, VECS = 32 * WN * TN, THREADS = 64 * WM * WN, STAGE = (ROWS + VECS) * F8_BLOCK;
@@ -332,20 +332,35 @@ __global__ __launch_bounds__(64 * WM * WN * KS) void f8_gemm_kernel(F8GemmArgs a
                     for (int e = 0; e < 16; ++e) acc[t][u][e] += o[((t * TN + u) * 16 + e) * 64];
         }
     }
-    // lane (i, h): row i of each group, vectors 8 q + 4 h + (0 .. 3): 128 contiguous bytes of a vector a half wave
+    // lane (i, h): row i of each group, vectors 8 q + 4 h + (0 .. 3): 128 contiguous bytes of a vector a half wave.  Two groups of rows
+    // trade halves: 64 rows of one vector, 256 contiguous bytes, a store.
+    constexpr int PAIR = TM % 2 == 0 ? 2 : 1;
 #pragma unroll
-    for (int t = 0; t < TM; ++t) {
-        const int row = r0 + 32 * (wm * TM + t) + i;
-        if (row >= a.rows) continue;
-        const float b = a.bias ? a.bias[row] : 0.0f;
+    for (int t = 0; t < TM; t += PAIR) {
+        const int row = r0 + 32 * (wm * TM + t) + (PAIR == 2 ? lane : i);
+        const float b = a.bias && row < a.rows ? a.bias[row] : 0.0f;
 #pragma unroll
         for (int u = 0; u < TN; ++u) {
-            const int vec = c0 + 32 * (wn * TN + u) + 4 * h;
+            const int vec = c0 + 32 * (wn * TN + u) + (PAIR == 2 ? 0 : 4 * h);
             float *out = a.Y + (size_t)vec * a.ldy + row;
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 const int v = 8 * (e >> 2) + (e & 3);
-                if (vec + v < a.n) __builtin_nontemporal_store(a.bias ? acc[t][u][e] + b : acc[t][u][e], &out[(size_t)v * a.ldy]);      // (y + 0 would turn -0 into 0)
+                float y[PAIR];
+                if constexpr (PAIR == 2) {                                  // (by all lanes)
+                    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_int(acc[t][u][e]), __float_as_int(acc[t + 1][u][e]), false, false);
+                    y[0] = __int_as_float(p[0]);
+                    y[1] = __int_as_float(p[1]);
+                } else {
+                    y[0] = acc[t][u][e];
+                }
+#pragma unroll
+                for (int z = 0; z < PAIR; ++z) {
+                    if (row >= a.rows || vec + v + 4 * z >= a.n) continue;
+                    const float sum = a.bias ? y[z] + b : y[z];             // (y + 0 would turn -0 into 0)
+                    if constexpr (PAST) __builtin_nontemporal_store(sum, &out[(size_t)(v + 4 * z) * a.ldy]);
+                    else out[(size_t)(v + 4 * z) * a.ldy] = sum;
+                }
             }
         }
     }
@@ -353,20 +368,24 @@ __global__ __launch_bounds__(64 * WM * WN * KS) void f8_gemm_kernel(F8GemmArgs a
 
 template <int WM, int WN, int TM, int TN, int KS = 1> static q8_status launch_f8(q8_ctx *ctx, F8GemmArgs &a)
 {
-    static Q8OncePerDevice once;
+    static Q8OncePerDevice once[2];
     const size_t smem = (size_t)KS * 2 * 32 * (WM * TM + WN * TN) * F8_BLOCK;
     a.row_tiles = (a.rows + 32 * WM * TM - 1) / (32 * WM * TM);
     a.col_tiles = (a.n + 32 * WN * TN - 1) / (32 * WN * TN);
     const size_t tiles = (size_t)a.row_tiles * a.col_tiles;
+    // 50000 x 512 x 1024 77 against 92 us in the caches; but where blocks share the 64-byte pieces that memory takes, the caches put
+    // them together: 6582 x 84 x 7068 43 us against 88 past them
+    const bool past = a.ldy % 16 == 0 && ((uintptr_t)a.Y & 63) == 0;
+    void (*const kernel)(F8GemmArgs) = past ? f8_gemm_kernel<WM, WN, TM, TN, KS, true> : f8_gemm_kernel<WM, WN, TM, TN, KS, false>;
     // t / d for t < 2^31 as (t magic / 2^32) / 2^shift: magic = ceil(2^(32 + shift) / d) with 2^shift < d <= 2^(shift + 1) is below 2^32, and
     // its excess over the quotient, less than 1, adds less than t / 2^(32 + shift) < 1 / d
     const unsigned long long d = 8ull * a.col_tiles;
     for (a.shift = 0; (2ull << a.shift) < d; ++a.shift) {}
     a.magic = (unsigned)(((1ull << (32 + a.shift)) + d - 1) / d);
     if (tiles > 0x7fffffffu) return q8_fail(ctx, Q8_ERR_SHAPE, "f8 product: %d x %d results are too many for a launch", a.rows, a.n);
-    const q8_status st = q8i_lds(ctx, once, (const void *)f8_gemm_kernel<WM, WN, TM, TN, KS>, smem, "f8 product");
+    const q8_status st = q8i_lds(ctx, once[past], (const void *)kernel, smem, "f8 product");
     if (st) return st;
-    hipLaunchKernelGGL((f8_gemm_kernel<WM, WN, TM, TN, KS>), dim3((unsigned)tiles), dim3(64 * WM * WN * KS), smem, ctx->stream, a);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)tiles), dim3(64 * WM * WN * KS), smem, ctx->stream, a);
     return q8i_launch_check(ctx, "product f8");
 }
 

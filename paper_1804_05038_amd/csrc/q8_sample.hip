@@ -492,7 +492,8 @@ template <int BLOCK, class Cond> __device__ __forceinline__ unsigned smp_find(co
     return (unsigned)(STEP * group + (close ? min(__ffsll((long long)close) - 1, STEP - 1) : STEP - 1));
 }
 
-// The logits of the bins from b0 to b1, a little wider: what rounding there is, is below 2^-23 of the largest logit and the distance.
+// The logits of the bins from b0 to b1, a little wider: a place is rounded to 2^-33 of 1/32 octave, which may carry a word over a border
+// (bins are 2^-24 wide at the finest), and what is rounded here to below 2^-23 of the largest logit and the distance.
 struct SmpWindow {
     unsigned b0, b1;
     float low, high;
@@ -502,8 +503,8 @@ struct SmpWindow {
         b1 = last;
         const double wide = __hiloint2double(__double2hiint(q.inv) - (q.fine << 20), __double2loint(q.inv)), am = fabs((double)m);
         const double gap0 = (double)first * wide, gap1 = last == SMP_BINS - 1 ? SMP_BINS * q.inv : ((double)last + 1.0) * wide;
-        high = (float)((double)m - gap0 + 2.5e-7 * (am + gap0));
-        low = (float)((double)m - gap1 - 2.5e-7 * (am + gap1));
+        high = (float)((double)m - gap0 + 2.5e-7 * (am + gap0) + 0x1p-31 * q.inv);
+        low = (float)((double)m - gap1 - 2.5e-7 * (am + gap1) - 0x1p-31 * q.inv);
     }
     __device__ __forceinline__ bool near(float v) const { return v >= low && v <= high; }
     __device__ __forceinline__ bool has(unsigned bin) const { return bin >= b0 && bin <= b1; }
@@ -539,7 +540,7 @@ __device__ __forceinline__ u64 smp_borders(Words words, SmpShared<BLOCK> &s, con
         win.open(bin, bin, m, q);
         u64 lowest = topk_key(win.low, 0x7fffffff), highest = topk_key(win.high, 0);
         bool again = false;
-        for (;;) {
+        for (int turn = 0; turn < 12; ++turn) {                 // (each at most a 256th of the keys before: nine suffice)
             if (tid == 0) s.listed = 0;
             __syncthreads();
             u64 first = 0, last = ~0ull;
@@ -576,6 +577,7 @@ __device__ __forceinline__ u64 smp_borders(Words words, SmpShared<BLOCK> &s, con
                 highest = s.red_u[0];
                 lowest = s.red_v[0];
                 for (int o = 1; o < BLOCK / 64; ++o) { highest = max(highest, s.red_u[o]); lowest = min(lowest, s.red_v[o]); }
+                found = highest;
             }
             again = true;
             u64 *h_m = s.list;                                  // [256], the block has at least as many threads
@@ -668,6 +670,7 @@ __device__ __forceinline__ u64 smp_borders_of_list(SmpShared<BLOCK> &s, const Sm
 
 __device__ __forceinline__ void smp_write(const SampleArgs &a, int j, int token, float logp, int block)
 {
+    if ((unsigned)token >= (unsigned)a.V) token = -1;
     if (threadIdx.x == 0) {
         a.tokens[j] = token;
         if (a.logp) a.logp[j] = logp;

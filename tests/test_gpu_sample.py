@@ -241,6 +241,22 @@ def test_flat_rows(q, ctx, V, sigma, mask):
     _check(q, ctx, lg, u, top_k=rng.integers(1, V, n).astype(np.int32), min_p=np.full(n, 0.9, np.float32))
 
 
+@pytest.mark.parametrize("V", [1500, 6000, 50000])
+@pytest.mark.parametrize("sigma", [1e-30, 1e-12, 1e-8, 1e-7, 1e-6, 1e-4])
+def test_flat_rows_around_zero(q, ctx, V, sigma):
+    """Logits whose differences are near what a word's place is rounded to, the largest of them zero."""
+    n = 6
+    rng = np.random.default_rng(V)
+    lg = (-sigma * np.abs(rng.standard_normal((n, V)))).astype(np.float32)
+    lg[np.arange(n), rng.integers(0, V, n)] = 0.0
+    lg[1] *= 50.0
+    lg[2, ::2] = 0.0
+    u = rng.random(n).astype(np.float32).clip(0, TOP)
+    _check(q, ctx, lg, u)
+    _check(q, ctx, lg, u, T=np.array([0.01, 0.3, 1.0, 1.0, 2.0, 30.0], np.float32), top_p=rng.random(n).astype(np.float32))
+    _check(q, ctx, lg, u, top_k=rng.integers(1, V, n).astype(np.int32))
+
+
 def test_two_streams_at_once(q):
     """Rows over several blocks, whose launches leave sums for each other, on two streams; one number for all rows."""
     rng = np.random.default_rng(17)

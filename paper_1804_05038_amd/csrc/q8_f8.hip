@@ -179,7 +179,7 @@ __device__ __forceinline__ void f8_to_lds(__amdgpu_buffer_rsrc_t rsrc, uint8_t *
 // an instruction, which the matrix cores' time covers (24 conversions beside 8 products of 32 x 32 x 16).  The order of k
 // inside a block is the same for both operands, which is all that it has to be: lane half h takes the 16-byte pieces 2 j + h.
 // KS > 1: KS such groups of waves take turns at the stages; their sums meet in LDS, in one order.
-// 8192 x 8192 x 8192 in 850 us, 1.29 PFLOP/s (codes of zeros: 604, so that power bounds it; without results 826, without stages
+// 8192 x 8192 x 8192 in 850 to 875 us, 1.26 to 1.29 PFLOP/s (codes of zeros: 604, so that power bounds it; without results 826, without stages
 // 749; the library's bf16 product of that size 1.20 PFLOP/s).  50000 x 512 x 1024 in 80 us: 205 MB of results, which alone take 50
 // (4.1 TB/s), and products, which alone take 52, overlap in part.
 // PAST: the results go past the caches.

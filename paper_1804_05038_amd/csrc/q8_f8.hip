@@ -509,8 +509,8 @@ __global__ __launch_bounds__(512) void f8_stream_kernel(F8StreamArgs a)
     const v8bf none = {};
     const uint8_t *px = s_x + (size_t)min(i, n - 1) * a.pitch + 32 * g;
     while (tile < tiles) {
-        const int at = b, from = tile;
-        const unsigned es = e;
+        const int at = b, from = tile, left = max(b1 - at, 0);
+        const unsigned es = left < 4 ? e & ((1u << 8 * left) - 1u) : e;     // (bytes past the columns: anything, 255 would make their zeros NaN)
         const float add = bias;
         b += 4;
         const bool last = b >= b1;

@@ -169,6 +169,21 @@ def test_product_of_extreme_scales(q, ctx):
             assert (Y == want.astype(np.float32)).all()
 
 
+@pytest.mark.parametrize("n", [1, 3, 16, 17, 70, 300])
+@pytest.mark.parametrize("cols", [100, 620, 1300])
+def test_scale_bytes_past_the_last_block_do_not_count(q, ctx, n, cols):
+    """1, 5 and 11 blocks of columns: what stands in the rest of a row's scales changes nothing, in either operand."""
+    rng = np.random.default_rng(cols + n)
+    nb = -(-cols // 128)
+    W = q.q8_quantize_matrix_f8(ctx, ctx.f32(rng.standard_normal((300, cols)).astype(np.float32)))
+    X = q.q8_quantize_matrix_f8(ctx, ctx.f32(rng.standard_normal((n, cols)).astype(np.float32)))
+    want = np_(q.q8_gemm_f8(ctx, W, X)).copy()
+    for byte in (0, 1, 254, 255):
+        for m in (W, X):
+            m.scale_rows[:, nb:] = byte
+        assert (np_(q.q8_gemm_f8(ctx, W, X)) == want).all(), byte
+
+
 def test_product_over_its_vectors(q, ctx):
     """Results that overwrite the vectors they are made of."""
     for n in (2, 16, 90):

@@ -648,7 +648,8 @@ q8_status output_logits_f8(q8_ctx *ctx, const q8_readout_weights *ro, const q8_m
  * A temperature that is not positive takes the first word.  Masses are exact sums of weights in units of at most 2^-38 of the largest
  * (2^-46 for V <= 65536), so that a word below half a unit is not drawn; the same inputs give the same tokens on every run.
  * Several logits of +inf share the mass.  logp[j] (logp may be NULL) = logit - log sum exp(logits) at T = 1 without filters, as
- * topk_logp.  A row without words: token -1, logp -inf.
+ * topk_logp: exponentials in 32 bits summed in 64 (for T = 1 and V <= 2^19, and short rows, the sum of the masses), within 2^-18 and one
+ * rounding to fp32.  A row without words: token -1, logp -inf.
  * E_tgt [V x E] and y_emb [n x E] (both or neither): y_emb[j] = E_tgt[tokens[j]], zeros for token -1, the next step's input.
  * n <= 65536, V <= 2^24.  Workspace: the context's must have q8_sample_bytes(n, V) bytes. */
 typedef struct {

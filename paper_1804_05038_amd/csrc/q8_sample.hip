@@ -44,6 +44,7 @@ struct SampleArgs {
     float *y_emb;
     int E;
     int shift;                              // S
+    bool mass_sums;                         // at T = 1 the mass of a row stands for its sum of exponentials
     // rows over several blocks
     struct SmpRowState *state;              // [rows of the launch]
     u64 *lists;                             // [rows of the launch x list_words]: a row's words that lie where its borders do
@@ -886,7 +887,7 @@ __global__ __launch_bounds__(SMP_BLOCK) void sample_bins_kernel(SampleArgs a)
         for (int t = 0; t < SMP_BINS / SMP_BLOCK; ++t) { s.mass[smp_at(t * SMP_BLOCK + tid)] = 0; s.count[smp_at(t * SMP_BLOCK + tid)] = 0; }
     }
     __syncthreads();
-    const bool own_sum = a.logp && q.T != 1.0f;
+    const bool own_sum = a.logp && !(a.mass_sums && q.T == 1.0f);
     double e = 0.0;
     u64 above = 0;
     if (own_sum) {
@@ -1091,7 +1092,7 @@ __global__ __launch_bounds__(SMP_BLOCK) void sample_draw_kernel(SampleArgs a)
         key = s.red_u[0];
         for (int w = 1; w < SMP_BLOCK / 64; ++w) key = max(key, s.red_u[w]);
     }
-    const double e = q.T == 1.0f ? (double)s.mass[smp_at(SMP_BINS - 1)] / q.one : e_parts;
+    const double e = a.mass_sums && q.T == 1.0f ? (double)s.mass[smp_at(SMP_BINS - 1)] / q.one : e_parts;
     smp_write(a, j, topk_key_idx(key), (float)(-smp_gap(m, topk_key_val(key)) - log(e)), SMP_BLOCK);
 }
 
@@ -1113,6 +1114,9 @@ q8_status q8i_sample(q8_ctx *ctx, const float *logits, int n, int V, int ldl, co
     int bits = 0;
     while (((size_t)1 << bits) < (size_t)V) ++bits;
     a.shift = 62 - bits < 46 ? 62 - bits : 46;                // the sum of V weights stays below 2^63
+    // words below half a unit are missing from the mass, V 2^-(S + 1) in all: up to 2^19 words 2^-25 of the largest, less than the logarithm's
+    // rounding to fp32 (at 2^24 it would be 2^-15)
+    a.mass_sums = V <= 1 << 19;
     const size_t smem = sizeof(SmpShared<256>);
     // A block per row while its threads hold eight words each at most and mostly find the borders among the words at the top, which
     // top-k and min_p see to (us; a block per row, several blocks): 5 rows of 2000 words 9.8, 14.8 without filters, 10.0, 17.1 with top-k, 1000

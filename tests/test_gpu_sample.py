@@ -218,6 +218,20 @@ def test_the_largest_vocabulary(q, ctx):
         _check(q, ctx, lg, np.array([0.77], np.float32), **k)
 
 
+@pytest.mark.parametrize("V,low", [(1 << 19, -30.6), ((1 << 19) + 1, -29.9), (1 << 21, -29.2), ((1 << 22) + 1, -27.8), (1 << 24, -27.1)])
+def test_log_probability_counts_words_too_light_to_be_drawn(q, ctx, V, low):
+    """One likely word, every other one just under half a unit of mass: none of these is drawn, and all of them are in the sum of
+    the exponentials, at every temperature.  The distances are exact in fp32; an exponential is off by 30 2^-24 + 2^-23 of itself, their
+    sum (below 2^-14) by less than 2^-32; the likely word's pair is rounded to 2^-24, and the result once."""
+    lg = torch.full((1, V), float(np.float32(low)), device=ctx.device)
+    lg[0, V - 2] = 0.0
+    want = -np.log1p((V - 1) * np.exp(np.float64(np.float32(low))))
+    for T in (1.0, 0.999):
+        r = q.q8_sample_logits(ctx, lg, torch.full((1,), 0.5, device=ctx.device), T)
+        assert int(r["tokens"]) == V - 2
+        assert abs(float(r["logp"]) - want) <= 2.0 ** -23, (T, float(r["logp"]), want)
+
+
 @pytest.mark.parametrize("V", [1500, 6000, 50000, 250001])
 @pytest.mark.parametrize("sigma", [1e-6, 1e-3, 0.05, 0.4])
 @pytest.mark.parametrize("mask", ["none", "half", "fourths", "run", "tail"])

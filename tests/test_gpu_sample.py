@@ -218,6 +218,40 @@ def test_the_largest_vocabulary(q, ctx):
         _check(q, ctx, lg, np.array([0.77], np.float32), **k)
 
 
+def _pinned(q, ctx, lg, u, T=1.0, top_k=0, top_p=1.0):
+    """The rows of a long vocabulary, each of them held to the definition.  A word's mass is half a unit off, and 4e-12 of itself
+    (the place in 2^-33 of 1/32 octave, the polynomial); so the mass up to a border and the one that it is compared with are together
+    V units and 1e-11 of the whole off at most, in shares of the row's whole mass, as the margin is.  The log-probability is that of
+    the drawn word, its tolerance _check's."""
+    n, V = lg.shape
+    full = lambda v, t: torch.full((n,), v, dtype=t, device=ctx.device)
+    r = q.q8_sample_logits(ctx, torch.from_numpy(lg).to(ctx.device), torch.from_numpy(u).to(ctx.device), full(T, torch.float32), full(top_k, torch.int32),
+                           full(top_p, torch.float32))
+    tokens, logp = np_(r["tokens"]), np_(r["logp"]).astype(np.float64)
+    unit = 2.0 ** -min(46, 62 - (V - 1).bit_length())
+    for j in range(n):
+        gap = np.float64(lg[j].max()) - lg[j].astype(np.float64)
+        tok, _, margin = ref.draw(lg[j], u[j], T, top_k, top_p)
+        assert margin > V * unit / np.exp(-gap / float(np.float32(T))).sum() + 1e-11, (j, margin)     # (of the inputs: no row is left out)
+        assert tokens[j] == tok, (j, tokens[j], tok, margin)
+        lp = -gap[tokens[j]] - np.log(np.exp(-gap).sum())
+        assert abs(logp[j] - lp) <= 2.0 ** -18 + 2.0 ** -24 * abs(lp), (j, logp[j], lp)
+
+
+@pytest.mark.parametrize("k", [dict(), dict(top_k=5), dict(top_p=0.3), dict(T=0.5), dict(T=0.5, top_k=1000, top_p=0.9)])
+def test_the_largest_vocabulary_to_its_last_word(q, ctx, k):
+    """Three dozen likely words up to the very end, all others some 40 nat below; and Gaussian logits."""
+    rng = np.random.default_rng(23)
+    V, n = 1 << 24, 2
+    lg = (rng.standard_normal((n, V), dtype=np.float32) - 40).astype(np.float32)
+    for j in range(n):
+        lg[j, np.concatenate([rng.integers(0, V, 33), [0, V - 2, V - 1]])] = (2 * rng.random(36)).astype(np.float32)
+    lg[0, V - 1] = 3.0
+    _pinned(q, ctx, lg, np.array([0.31, 0.93], np.float32), **k)
+    if k != dict(T=0.5):                                  # (there, no word's share clears the units of 2^24 words)
+        _pinned(q, ctx, rng.standard_normal((1, V), dtype=np.float32), np.array([0.77], np.float32), **k)
+
+
 @pytest.mark.parametrize("V,low", [(1 << 19, -30.6), ((1 << 19) + 1, -29.9), (1 << 21, -29.2), ((1 << 22) + 1, -27.8), (1 << 24, -27.1)])
 def test_log_probability_counts_words_too_light_to_be_drawn(q, ctx, V, low):
     """One likely word, every other one just under half a unit of mass: none of these is drawn, and all of them are in the sum of

@@ -1,4 +1,6 @@
 """GPU parity of q8_sample_logits with the plain definition in 64 bits."""
+import ctypes as C
+
 import numpy as np
 import pytest
 import torch
@@ -303,6 +305,22 @@ def test_flat_rows_around_zero(q, ctx, V, sigma):
     _check(q, ctx, lg, u)
     _check(q, ctx, lg, u, T=np.array([0.01, 0.3, 1.0, 1.0, 2.0, 30.0], np.float32), top_p=rng.random(n).astype(np.float32))
     _check(q, ctx, lg, u, top_k=rng.integers(1, V, n).astype(np.int32))
+
+
+@pytest.mark.parametrize("V", [700, 5000, 50000])
+def test_without_log_probabilities(q, ctx, V):
+    """logp NULL: the same tokens, whatever form draws them."""
+    rng = np.random.default_rng(V)
+    n = 6
+    lg = ctx.f32(_logits(rng, n, V))
+    u = ctx.f32(rng.random(n).astype(np.float32).clip(0, TOP))
+    T, k = ctx.f32(np.array([1, 0.7, 0, 1, 2, 1], np.float32)), torch.tensor([0, 5, 0, 40, 0, 1], dtype=torch.int32, device=ctx.device)
+    for top_k in (None, k):
+        want = np_(q.q8_sample_logits(ctx, lg, u, T, top_k)["tokens"]).copy()
+        s = q.binding._Sampling(T.data_ptr(), top_k.data_ptr() if top_k is not None else None, None, None)
+        tokens = torch.full((n,), -9, dtype=torch.int32, device=ctx.device)
+        ctx.check(ctx.lib.q8_sample_logits(ctx.handle, lg.data_ptr(), n, V, V, C.byref(s), u.data_ptr(), tokens.data_ptr(), None, None, 0, None))
+        assert (np_(tokens) == want).all()
 
 
 def test_two_streams_at_once(q):

@@ -37,12 +37,12 @@ __device__ __forceinline__ float f8_half_max(float v)
 }
 
 // Four codes; the scaled values are at most 448 in magnitude or not finite (then the code is NaN).  The product with a power
-// of two is exact, so the conversion's rounding (to nearest, ties to even) is the only one.
+// of two is exact, so the conversion's rounding (to nearest, ties to even) is the only one.  inv = 0: zeros without a sign.
 __device__ __forceinline__ unsigned f8_codes4(float4 v, float inv)
 {
     int p = __builtin_amdgcn_cvt_pk_fp8_f32(v.x * inv, v.y * inv, 0, false);
     p = __builtin_amdgcn_cvt_pk_fp8_f32(v.z * inv, v.w * inv, p, true);
-    return (unsigned)p;
+    return inv > 0.0f ? (unsigned)p : (unsigned)p & 0x7f7f7f7fu;
 }
 
 struct F8QuantArgs {

@@ -57,6 +57,24 @@ def test_quantize_edges(q, ctx):
     _same_codes(np_(m.data), codes)
 
 
+def test_blocks_of_zeros_have_codes_of_zero(q, ctx):
+    """Blocks below 2^-100 in all places, negative ones too: bytes of zero; zeros of other blocks keep their sign."""
+    X = np.zeros((4, 300), np.float32)
+    X[0] = -0.0
+    X[1] = -2.0 ** -101
+    X[2, ::2] = -1e-45
+    X[3, :128] = -1e-38
+    X[3, 128:] = -0.0
+    X[3, 200] = 1.0
+    m = q.q8_quantize_matrix_f8(ctx, ctx.f32(X))
+    c = np_(m.data)
+    assert not c[:3].any() and not c[3, :128].any() and not c[3, 256:].any()
+    assert (np_(m.scale)[:, 0] == 127).all()
+    want = np.full(128, 0x80, np.uint8)
+    want[200 - 128] = ref.e4m3_round(256.0)
+    assert (c[3, 128:256] == want).all()
+
+
 @pytest.mark.parametrize("off,pitch,ld_out,lds", [(0, 133, 144, 4), (1, 132, 144, 4), (3, 301, 512, 8), (0, 400, 384, 12), (2, 130, 16384, 128)])
 def test_quantize_pitches(q, ctx, off, pitch, ld_out, lds):
     """Rows that begin anywhere, a pitch of codes and of scales beyond the last block; nothing outside is written."""

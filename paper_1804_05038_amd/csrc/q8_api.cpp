@@ -3,6 +3,7 @@
 // kernels (the .hip files beside this one).
 #include "q8_internal.h"
 
+#include <algorithm>
 #include <new>
 #include <stdlib.h>
 #include <string.h>
@@ -153,14 +154,15 @@ size_t q8_workspace_bytes(int max_n, int max_l, int max_rows, int max_ld)
     const size_t nv = (size_t)(max_n > max_l ? max_n : max_l);
     size_t b = Q8_WS_HEADER;
     b += up256(nv * (size_t)max_ld) + up256(nv * 4);              // quantized vectors + scales (MFMA path)
-    b += up256(nv * (size_t)(max_ld / 128 + 4));                  // a scale per block of 128 columns (8-bit floating point)
     b += 2 * up256((size_t)max_l * max_rows * 4);                 // encoder input pre-activations, both directions
     b += 8 * up256((size_t)max_n * max_rows * 4);                 // per-hypothesis vectors of a decoder step
     b += up256((size_t)max_n * max_l * 4);                        // attention energies
-    b += up256(q8i_sample_bytes(max_n, max_rows));
-    const size_t ngrp = (size_t)q8i_out_tiles(max_rows);
-    b += up256(ngrp * max_n * 4) + up256(ngrp * max_n * 8);
-    return b + 65536;
+    const size_t ngrp = (size_t)q8i_out_tiles(max_rows), tiles = up256(ngrp * max_n * 4) + up256(ngrp * max_n * 8);
+    b += tiles + 65536;
+    // calls that lay their room out otherwise: less than the above, unless the matrices have few rows
+    const size_t layer = Q8_WS_HEADER + 5 * up256((size_t)max_n * max_rows * 4) + 4 * up256((size_t)max_n * ((max_ld + 15) & ~15)) +
+                         3 * up256((size_t)max_n * 4) + up256((size_t)max_n * (max_ld / 128 + 4)) + tiles;
+    return std::max({b, layer, q8_gemm_f8_bytes(max_n, max_ld), q8_sample_bytes(max_n, max_rows)});
 }
 
 q8_status q8_create(q8_ctx **out, void *hip_stream, void *workspace, size_t workspace_bytes)

@@ -107,3 +107,37 @@ def test_draws(lib):
     for k in range(4):
         assert call(s=C.byref(_Sampling(*[P + 2 if i == k else None for i in range(4)]))) == ALIGN
     assert call() == call(s=C.byref(_Sampling(P, P, P, P)), e=P, E=8, y=P, lp=P) == call(n=1, ld=0) == DEVICE
+
+
+def _up(v):
+    return -(-v // 256) * 256
+
+
+@pytest.mark.parametrize("n,l,rows,ld", [(1, 1, 1000, 512), (8, 64, 65536, 2048), (60, 50, 50000, 1024), (1024, 64, 50000, 2048), (1024, 1, 2049, 512), (5, 1, 1 << 24, 1024)])
+def test_workspace_of_callers_who_draw_nothing(lib, n, l, rows, ld):
+    """Drawing and 8-bit floating point lay their room out over that of the other calls: nothing on top of it at a model's sizes."""
+    nv, tiles, header = max(n, l), -(-rows // 16), 262144
+    others = header + _up(nv * ld) + _up(nv * 4) + 2 * _up(l * rows * 4) + 8 * _up(n * rows * 4) + _up(n * l * 4) + _up(tiles * n * 4) + _up(tiles * n * 8) + 65536
+    assert lib.q8_workspace_bytes(n, l, rows, ld) == others
+
+
+@pytest.mark.parametrize("n", [1, 8, 9, 300, 1024])
+@pytest.mark.parametrize("V,R,H", [(1, 16384, 16), (16, 16, 1024), (100, 64, 7000), (3000, 620, 1000), (70000, 512, 1024)])
+def test_workspace_is_enough(lib, n, V, R, H):
+    """q8_workspace_bytes: every call succeeds at the sizes that it was asked for."""
+    from paper_1804_05038_amd.binding import _Mat, _Readout
+    ld = lambda c: -(-c // 16) * 16
+    ro = C.byref(_Readout(*[_Mat(P, R, H, ld(H), 1.0, None)] * 3, None))
+    w = mat(rows=V, cols=R, ld=ld(R), lds=-(-R // 512) * 4)
+    k = min(V, 12)
+    plain = context(lib.q8_workspace_bytes(n, 1, V, ld(R)))
+    whole = context(lib.q8_workspace_bytes(n, 1, max(V, R), max(ld(R), ld(H))))
+    for logits in (P, None):
+        for kk in (0, k) if logits else (k,):
+            if kk and V > 65536:
+                continue
+            assert lib.output_logits_f8(plain, None, w, None, None, None, None, P, n, kk, logits, None, P, P, None) == DEVICE
+            if R <= 1024 and (n > 8 or 3 * n * ld(H) <= 65536):
+                assert lib.output_logits_f8(whole, ro, w, None, P, P, P, None, n, kk, logits, None, P, P, None) == DEVICE
+    assert lib.q8_gemm_f8(plain, w, P, n, -(-R // 4) * 4, None, P, V) == DEVICE
+    assert lib.q8_sample_logits(plain, P, n, V, V, None, P, P, None, None, 0, None) == DEVICE

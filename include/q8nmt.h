@@ -617,7 +617,8 @@ typedef struct {
 /* X fp32 [rows x cols] (ld_in floats per row, any alignment) -> codes_out [rows x ld_out], pad bytes zero, and scale_out
  * [rows x lds_out].  Per block: m = the largest finite magnitude, scale 2^e with the smallest e for which m <= 448 * 2^e, code =
  * x 2^-e rounded to the nearest e4m3 value, ties to even (the product is exact); m < 2^-100: e = 0, codes 0.  A value that is not
- * finite becomes NaN.  Pad bytes of a row's scales are set to 127.  rows <= 2^24.  Enqueued; nothing returns to the host. */
+ * finite becomes NaN.  Pad bytes of a row's scales are set to 127.  rows <= 2^24, rows * max(ceil(ld_out / 128), lds_out) <= 2^29 - 32.
+ * Enqueued; nothing returns to the host. */
 q8_status q8_quantize_matrix_f8(q8_ctx *ctx, const float *X, int rows, int cols, int ld_in, uint8_t *codes_out, int ld_out,
                                 uint8_t *scale_out, int lds_out);
 
@@ -626,7 +627,7 @@ q8_status q8_quantize_matrix_f8(q8_ctx *ctx, const float *X, int rows, int cols,
  * q8_gemm_f8: n vectors X [n x ldx] fp32 (16-byte aligned, ldx % 4 == 0), quantized in the call as above; workspace: the
  * context's must have q8_gemm_f8_bytes(n, W->cols) bytes.  q8_gemm_codes_f8: X in codes already (n = X->rows, X->cols ==
  * W->cols), no workspace; X and W may share memory, Y must overlap neither.  q8_gemm_f8's Y may overlap its X.
- * 1 <= n <= 2^20, W->rows <= 2^24; any of the two may be large as long as the results number below 2^43. */
+ * 1 <= n <= 2^20, W->rows <= 2^24; both may be large as far as a launch holds them (some 2^36 results; Q8_ERR_SHAPE past it). */
 size_t q8_gemm_f8_bytes(int n, int cols);
 q8_status q8_gemm_f8(q8_ctx *ctx, const q8_mat_f8 *W, const float *X, int n, int ldx, const float *bias, float *Y, int ldy);
 q8_status q8_gemm_codes_f8(q8_ctx *ctx, const q8_mat_f8 *W, const q8_mat_f8 *X, const float *bias, float *Y, int ldy);

@@ -113,8 +113,10 @@ q8_status q8i_quantize_f8(q8_ctx *ctx, const float *X, int rows, int cols, int l
     a.units_per_row = nb > lds ? nb : lds;
     a.units = (size_t)rows * a.units_per_row;
     a.vec = ldx % 4 == 0 && ((uintptr_t)X & 15) == 0;
-    const size_t per_block = 4 * F8_QUANT_PER_WAVE;
-    hipLaunchKernelGGL(f8_quantize_kernel, dim3((unsigned)((a.units + per_block - 1) / per_block)), dim3(256), 0, ctx->stream, a);
+    const size_t per_block = 4 * F8_QUANT_PER_WAVE, grid = (a.units + per_block - 1) / per_block;
+    if (grid >= 1u << 24)                                                   // a launch has fewer than 2^32 threads
+        return q8_fail(ctx, Q8_ERR_SHAPE, "quantize f8: %d rows of %d blocks are too many for a launch", rows, a.units_per_row);
+    hipLaunchKernelGGL(f8_quantize_kernel, dim3((unsigned)grid), dim3(256), 0, ctx->stream, a);
     return q8i_launch_check(ctx, "quantize f8");
 }
 
@@ -382,7 +384,8 @@ template <int WM, int WN, int TM, int TN, int KS = 1> static q8_status launch_f8
     const unsigned long long d = 8ull * a.col_tiles;
     for (a.shift = 0; (2ull << a.shift) < d; ++a.shift) {}
     a.magic = (unsigned)(((1ull << (32 + a.shift)) + d - 1) / d);
-    if (tiles > 0x7fffffffu) return q8_fail(ctx, Q8_ERR_SHAPE, "f8 product: %d x %d results are too many for a launch", a.rows, a.n);
+    if (tiles * (64 * WM * WN * KS) > 0xffffffffu)                          // a launch has fewer than 2^32 threads
+        return q8_fail(ctx, Q8_ERR_SHAPE, "f8 product: %d x %d results are too many for a launch", a.rows, a.n);
     const q8_status st = q8i_lds(ctx, once[past], (const void *)kernel, smem, "f8 product");
     if (st) return st;
     hipLaunchKernelGGL(kernel, dim3((unsigned)tiles), dim3(64 * WM * WN * KS), smem, ctx->stream, a);

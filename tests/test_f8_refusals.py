@@ -141,3 +141,15 @@ def test_workspace_is_enough(lib, n, V, R, H):
                 assert lib.output_logits_f8(whole, ro, w, None, P, P, P, None, n, kk, logits, None, P, P, None) == DEVICE
     assert lib.q8_gemm_f8(plain, w, P, n, -(-R // 4) * 4, None, P, V) == DEVICE
     assert lib.q8_sample_logits(plain, P, n, V, V, None, P, P, None, None, 0, None) == DEVICE
+
+
+def test_more_than_a_launch_holds(lib):
+    """Blocks of 256 threads, 32 blocks of columns or bytes of scales each: 2^32 threads are one too many.  (Wider pitches of the scales
+    had the number of blocks cut to 32 bits.)"""
+    c = context(1 << 20)
+    call = lambda rows, lds: lib.q8_quantize_matrix_f8(c, P, rows, 1, 1, P, 16, P, lds)
+    assert call((1 << 24) - 1, 32) == call(1 << 24, 28) == call(1 << 15, 16380) == DEVICE
+    assert call(1 << 24, 32) == call(1 << 24, 8196) == call(1 << 24, 16384) == call(1 << 23, 64) == SHAPE
+    # products: tiles of 128 x 64 in 512 threads
+    many = lambda rows, n: lib.q8_gemm_codes_f8(c, mat(rows=rows), mat(rows=n), None, P, rows)
+    assert many(1 << 24, 4032) == DEVICE and many(1 << 24, 4160) == many(1 << 24, 1 << 18) == SHAPE

@@ -968,6 +968,13 @@ def _vector(t, name, n, dtype=torch.float32):
         raise ValueError("%s: expected %d contiguous %s on the device, got %s %s on %s" % (name, n, dtype, tuple(t.shape), t.dtype, t.device))
 
 
+def _on_device(ctx, **tensors):
+    """A kernel of the context takes an address of another GPU for one of its own: refused here."""
+    for name, t in tensors.items():
+        if t is not None and t.device != ctx.workspace.device:
+            raise ValueError("%s: on %s, the context is on %s" % (name, t.device, ctx.workspace.device))
+
+
 class MatF8:
     """q8_mat_f8: e4m3 codes [rows x ld] (uint8) and the bytes of their blocks' scales [rows x blocks] on the device."""
 
@@ -980,12 +987,14 @@ class MatF8:
         self.scale = scale_rows[:, :(cols + 127) // 128]
         if not (data.is_contiguous() and scale_rows.is_contiguous()) or scale_rows.shape[0] != self.rows:
             raise ValueError("codes and scales must be contiguous, with as many rows each")
+        if data.device != scale_rows.device:
+            raise ValueError("codes on %s, scales on %s" % (data.device, scale_rows.device))
         self.c = _MatF8(data.data_ptr(), scale_rows.data_ptr(), self.rows, cols, self.ld, scale_rows.shape[1])
 
 
 def q8_quantize_matrix_f8(ctx, W, ld_out=None, bind=False):
     """Rows of W (weights or vectors) in e4m3 with a power of two per 128 columns: a MatF8."""
-    if not (isinstance(W, torch.Tensor) and W.is_cuda and W.dtype == torch.float32):
+    if not (isinstance(W, torch.Tensor) and W.device == ctx.workspace.device and W.dtype == torch.float32):
         with torch.cuda.stream(ctx.stream):
             W = ctx.f32(W)
     ld_in = _rows(W, "W")
@@ -1013,6 +1022,7 @@ def q8_gemm_f8(ctx, W, X, bias=None, Y=None, bind=False):
     if Y.shape[0] != n:
         raise ValueError("Y: expected %d rows, got %d" % (n, Y.shape[0]))
     _vector(bias, "bias", W.rows)
+    _on_device(ctx, W=W.data, X=X.data if codes else X, bias=bias, Y=Y)
     if codes:
         fn, args = ctx.lib.q8_gemm_codes_f8, (ctx.handle, C.byref(W.c), C.byref(X.c), _ptr(bias), _ptr(Y), ldy)
     else:
@@ -1035,6 +1045,7 @@ def output_logits_f8(ctx, ro, W_out, b_out, s=None, y_emb=None, ctx_vec=None, t_
         if t is None or t.dtype != torch.float32 or tuple(t.shape) != (n, cols) or not t.is_cuda or not t.is_contiguous():
             raise ValueError("%s: expected a contiguous fp32 device tensor %d x %d" % (name, n, cols))
     _vector(b_out, "b_out", V)
+    _on_device(ctx, W_out=W_out.data, b_out=b_out, logits=logits, **{name: t for t, name, _ in given})
     t = ctx.empty(n, R) if ro is not None else None
     lse, lp, idx = (ctx.empty(n), ctx.empty(n, k), ctx.empty(n, k, dtype=torch.int32)) if k > 0 else (None, None, None)
     args = (ctx.handle, C.byref(ro.c) if ro is not None else None, C.byref(W_out.c), _ptr(b_out), _ptr(s), _ptr(y_emb), _ptr(ctx_vec),
@@ -1068,6 +1079,8 @@ def q8_sample_logits(ctx, logits, u, temperature=None, top_k=None, top_p=None, m
         _vector(v, name, n, dtype)
         return v
 
+    _on_device(ctx, logits=logits, u=u, E_tgt=E_tgt, y_emb=y_emb, tokens=tokens, logp=logp,
+               **{name: v for name, v in (("temperature", temperature), ("top_k", top_k), ("top_p", top_p), ("min_p", min_p)) if isinstance(v, torch.Tensor)})
     p = [per_row(temperature, "temperature", torch.float32), per_row(top_k, "top_k", torch.int32), per_row(top_p, "top_p", torch.float32),
          per_row(min_p, "min_p", torch.float32)]
     sampling = _Sampling(*[t.data_ptr() if t is not None else None for t in p])

@@ -61,3 +61,43 @@ def test_calls_without_a_context_return_the_null_code():
         assert q.q8_workspace_bytes(n, 1, 1, (cols + 15) // 16 * 16) >= q.q8_gemm_f8_bytes(n, cols)
     for n, V in ((1, 8193), (1024, 9000), (1, 1 << 24)):
         assert q.q8_workspace_bytes(n, 1, V, 16) >= q.q8_sample_bytes(n, V)
+
+
+def test_the_binding_refuses_tensors_of_another_gpu():
+    """(Tensors without memory, which torch lets be on any device.)"""
+    from types import SimpleNamespace
+
+    from torch._subclasses.fake_tensor import FakeTensorMode
+
+    import paper_1804_05038_amd as q
+
+    class Converted(Exception):
+        pass
+
+    def f32(t):
+        raise Converted
+
+    with FakeTensorMode():
+        here, there = (lambda *s, dtype=torch.float32: torch.empty(*s, dtype=dtype, device="cuda:0")), (lambda *s, dtype=torch.float32: torch.empty(*s, dtype=dtype, device="cuda:1"))
+        ctx = SimpleNamespace(workspace=here(256, dtype=torch.uint8), device=torch.device("cuda:0"), stream=None, empty=here, f32=f32, handle=None)
+        u8 = torch.uint8
+
+        def mat(data, scale):                            # (its address is not asked for: refused before)
+            m = q.MatF8.__new__(q.MatF8)
+            m.data, m.scale_rows, m.rows, m.cols, m.ld = data(32, 64, dtype=u8), scale(32, 4, dtype=u8), 32, 64, 64
+            return m
+        with pytest.raises(ValueError, match="codes on cuda:0, scales on cuda:1"):
+            q.MatF8(here(32, 64, dtype=u8), there(32, 4, dtype=u8), 64)
+        W, far = mat(here, here), mat(there, there)
+        x, lg, u = here(4, 64), here(4, 100), here(4)
+        for name, call in (("W", lambda: q.q8_gemm_f8(ctx, far, x)), ("X", lambda: q.q8_gemm_f8(ctx, W, there(4, 64))), ("X", lambda: q.q8_gemm_f8(ctx, W, far)),
+                           ("bias", lambda: q.q8_gemm_f8(ctx, W, x, there(32))), ("Y", lambda: q.q8_gemm_f8(ctx, W, x, Y=there(4, 32))),
+                           ("W_out", lambda: q.output_logits_f8(ctx, None, far, None, t_in=x)), ("t_in", lambda: q.output_logits_f8(ctx, None, W, None, t_in=there(4, 64))),
+                           ("b_out", lambda: q.output_logits_f8(ctx, None, W, there(32), t_in=x)), ("logits", lambda: q.output_logits_f8(ctx, None, W, None, t_in=x, logits=there(4, 32))),
+                           ("logits", lambda: q.q8_sample_logits(ctx, there(4, 100), u)), ("u", lambda: q.q8_sample_logits(ctx, lg, there(4))),
+                           ("top_k", lambda: q.q8_sample_logits(ctx, lg, u, top_k=there(4, dtype=torch.int32))), ("temperature", lambda: q.q8_sample_logits(ctx, lg, u, there(4))),
+                           ("tokens", lambda: q.q8_sample_logits(ctx, lg, u, tokens=there(4, dtype=torch.int32))), ("E_tgt", lambda: q.q8_sample_logits(ctx, lg, u, E_tgt=there(100, 8)))):
+            with pytest.raises(ValueError, match="%s: on cuda:1, the context is on cuda:0" % name):
+                call()
+        with pytest.raises(Converted):                   # a matrix to be quantized comes to the context's device first, as one of the host does
+            q.q8_quantize_matrix_f8(ctx, there(32, 64))

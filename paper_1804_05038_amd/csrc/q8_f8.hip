@@ -395,8 +395,10 @@ template <int WM, int WN, int TM, int TN, int KS = 1> static q8_status launch_f8
 // Tiles by what each costs (us; rows x columns x vectors, the product alone): 256 x 256 and 128 x 128 where they are about one round of
 // blocks or more, long enough that reading counts most, and the vectors fill them (8192 x 8192 x 8192 865, 986 and in 128 x 64 1146;
 // 4096 x 1024 x 4096 43.3, 41.0 and 44.0; 50000 x 512 x 1024, four stages a tile, 110, 77.0 and 76.0); 128 x 32 for up to 32 vectors;
-// 128 x 96 for 65 to 96 and many rows (63644 x 620 x 77 19.9 against 25.5 in 64 x 64 and 24.6 in 128 x 64; 19736 x 293 x 82 13.7 against
-// 11.2 and 11.4); 64 x 32 with four groups in turns at the stages where the others would leave compute units without any (1024 x 8192 x
+// 128 x 96 for 65 to 96 where they are one round (two blocks a compute unit) and the 128 x 64 ones, three a unit, are not, and longer than
+// four stages (128 x 96, 128 x 64, 64 x 64 with 81 vectors: 47323 x 640 16.8, 14.7, 16.7; 50011 x 640 17.0, 17.0, 17.1; 63707 x 640 18.1,
+// 19.6, 20.5; 67803 x 640 25.5, 20.3, 21.6; x 2048 31.8, 32.4, 35.8; 32.3, 38.6, 37.5; 34.6, 43.9, 44.8; 50.0, 47.0, 48.7; with 77 63644 x 256 11.9,
+// 11.8, 12.1); 64 x 32 with four groups in turns at the stages where the others would leave compute units without any (1024 x 8192 x
 // 64 22.9 against 35.1 in 64 x 64, 512 x 4096 x 17 10.2 against 17.2, 11807 x 1012 x 8 8.0 against 9.6 in 128 x 32); else 128 x 64 where
 // these are more than a round, in eight waves (50000 x 640 x 320 35.0 against 39.7 in 64 x 64 and 39.1 in four waves), and 64 x 64
 // (1024 x 2048 x 1024 11.9 against 14.3, 3117 x 4084 x 663 37.4 against 41.2).
@@ -408,7 +410,7 @@ static q8_status gemm_f8_tiles(q8_ctx *ctx, F8GemmArgs &a)
     if (filled(128) && tiles(128, 128) >= 500 && a.cols >= 1024) return launch_f8<2, 4, 2, 1>(ctx, a);
     if (a.cols >= 512 && (a.n <= 32 ? tiles(128, 32) < 256 : tiles(64, 64) < 128)) return launch_f8<2, 1, 1, 1, 4>(ctx, a);
     if (a.n <= 32) return launch_f8<4, 1, 1, 1>(ctx, a);
-    if (a.n > 64 && a.n <= 96 && tiles(128, 96) >= 400) return launch_f8<4, 1, 1, 3>(ctx, a);
+    if (a.n > 64 && a.n <= 96 && a.cols > 512 && tiles(128, 96) <= 512 && tiles(128, 64) > 768) return launch_f8<4, 1, 1, 3>(ctx, a);
     if (tiles(128, 64) >= 320) return launch_f8<4, 2, 1, 1>(ctx, a);
     return launch_f8<2, 2, 1, 1>(ctx, a);
 }

@@ -146,6 +146,17 @@ def test_product_of_whole_numbers_is_exact(q, ctx, rows, cols, n):
     assert (np_(q.q8_gemm_f8(ctx, W, X)) == xv @ wv.T).all()
 
 
+@pytest.mark.parametrize("rows,cols,n", [(49300, 620, 77), (65500, 513, 96), (50000, 1100, 65), (65537, 620, 77), (49152, 620, 96), (90000, 530, 70)])
+def test_products_of_65_to_96_vectors(q, ctx, rows, cols, n):
+    """On both sides of where they go in tiles of 128 x 96: whole numbers, every sum exact."""
+    rng = np.random.default_rng(rows + n)
+    Wi, Xi = rng.integers(-8, 9, (rows, cols)).astype(np.float32), rng.integers(-8, 9, (n, cols)).astype(np.float32)
+    Wi[:, ::128], Xi[:, ::128] = 8.0, -8.0               # every block has the same scale, and every whole number up to 8 a code
+    b = rng.integers(-99, 100, rows).astype(np.float32)
+    W = q.q8_quantize_matrix_f8(ctx, ctx.f32(Wi))
+    assert (np_(q.q8_gemm_f8(ctx, W, q.q8_quantize_matrix_f8(ctx, ctx.f32(Xi)), ctx.f32(b))) == Xi @ Wi.T + b).all()
+
+
 @pytest.mark.parametrize("rows,cols,n", [(70, 200, 3), (70, 200, 20), (130, 300, 70), (300, 256, 300)])
 @pytest.mark.parametrize("off", [0, 1])
 def test_product_leaves_the_rest_of_y(q, ctx, rows, cols, n, off):

@@ -14,7 +14,9 @@
 // 64-bit arithmetic: 1000 of 63644 words 203 us (reading the 255 MB three times 127, the sums' LDS additions 24, the weights' 64-bit
 // operations some 50).  Bins are as wide as the row's spread asks for: of 1/32 octave alone, flat rows (deviation 0.1 nat) went
 // through the row again and again in one block: 64 rows of 50000 words with top-p 345 us, now 40, 12 of 250001 1328, now 55 (ordinary rows 3 %
-// more).  Rows of one logit alone still do (50000 words: some 300 us).
+// more).  Rows with more words in the borders' bins than their list holds, 1/32 of them, still do, for a time that grows with their length:
+// one logit alone 295 us for one row of 50000 words, 1320 for 250001, 5400 for 2^20; deviation 0.1 nat and five words 8 nat above that 67 (with
+// top-p 185), with top-p 764, 4900 (a sort of all words: 370 to 430, 390 to 425, 470 to 510).
 #include "q8_internal.h"
 
 #include <algorithm>
@@ -1098,9 +1100,10 @@ __global__ __launch_bounds__(SMP_BLOCK) void sample_draw_kernel(SampleArgs a)
 
 static int sample_rows(int n) { return n < SMP_ROWS ? n : SMP_ROWS; }
 
-// Words that a row's list holds: of Gaussian logits 0.6 % lie in the fullest bin (row of 1.4 nat deviation), and there are three.
-// Where there are more, one block goes through the row again for every border (12 rows of 250001 words 108 us instead of 26).
-static int sample_list_words(int V) { return std::min(std::max(SMP_LIST, (V / 32 + 63) & ~63), 16384); }
+// Words that a row's list holds, 1/32 of the row: of Gaussian logits 0.6 % lie in the fullest bin (row of 1.4 nat deviation), and there are
+// three.  Where there are more, one block goes through the row again for every border (12 rows of 250001 words 108 us instead of 26; a list of
+// 16384 words at most: one row of 2^24 words 20.8 ms instead of 0.42, with top-p 33 instead of 0.82).
+static int sample_list_words(int V) { return std::max(SMP_LIST, (V / 32 + 63) & ~63); }
 
 size_t q8i_sample_bytes(int n, int V) { return V <= SMP_SMALL ? 0 : (size_t)sample_rows(n) * (sizeof(SmpRowState) + sizeof(u64) * sample_list_words(V)); }
 

@@ -153,3 +153,11 @@ def test_more_than_a_launch_holds(lib):
     # products: tiles of 128 x 64 in 512 threads
     many = lambda rows, n: lib.q8_gemm_codes_f8(c, mat(rows=rows), mat(rows=n), None, P, rows)
     assert many(1 << 24, 4032) == DEVICE and many(1 << 24, 4160) == many(1 << 24, 1 << 18) == SHAPE
+
+
+@pytest.mark.parametrize("V", [2049, 50000, 250001, 600000, (1 << 22) + 1, 1 << 24])
+def test_lists_of_words_grow_with_the_vocabulary(lib, V):
+    """A row's list holds 1/32 of its words: a longer row must not be one that a single block goes through again."""
+    one, two = lib.q8_sample_bytes(1, V), lib.q8_sample_bytes(2, V)
+    assert two - one >= 8 * (V // 32)
+    assert lib.q8_workspace_bytes(2, 1, V, 16) >= two

@@ -652,7 +652,9 @@ q8_status output_logits_f8(q8_ctx *ctx, const q8_readout_weights *ro, const q8_m
  * topk_logp: exponentials in 32 bits summed in 64 (for T = 1 and V <= 2^19, and short rows, the sum of the masses), within 2^-18 and one
  * rounding to fp32.  A row without words: token -1, logp -inf.
  * E_tgt [V x E] and y_emb [n x E] (both or neither): y_emb[j] = E_tgt[tokens[j]], zeros for token -1, the next step's input.
- * n <= 65536, V <= 2^24.  Workspace: the context's must have q8_sample_bytes(n, V) bytes. */
+ * n <= 65536, V <= 2^24.  Workspace: the context's must have q8_sample_bytes(n, V) bytes.
+ * Time depends on the logits: rows of one or few values, or nearly flat ones below a few words far above, are gone through by one block (one
+ * value: 0.3 ms for 50000 words, 1.3 for 250000, 113 for 2^24, twice that with top-p, against 18 us, 23 us and 0.4 ms). */
 typedef struct {
     const float *temperature;
     const int32_t *top_k;

@@ -183,7 +183,8 @@ __device__ __forceinline__ void f8_to_lds(__amdgpu_buffer_rsrc_t rsrc, uint8_t *
 // KS > 1: KS such groups of waves take turns at the stages; their sums meet in LDS, in one order.
 // 8192 x 8192 x 8192 in 850 to 875 us, 1.26 to 1.29 PFLOP/s (codes of zeros: 604, so that power bounds it; without results 826, without stages
 // 749; the library's bf16 product of that size 1.20 PFLOP/s).  50000 x 512 x 1024 in 80 us: 205 MB of results, which alone take 50
-// (4.1 TB/s), and products, which alone take 52, overlap in part.
+// (4.1 TB/s), and products, which alone take 52, overlap in part.  As compiled every store waits for the one before: a wait for all memory
+// operations, which the bias's load asks for, stands in front of each.
 // PAST: the results go past the caches.
 template <int WM, int WN, int TM, int TN, int KS, bool PAST>
 __global__ __launch_bounds__(64 * WM * WN * KS) void f8_gemm_kernel(F8GemmArgs a)
@@ -426,7 +427,7 @@ struct F8StreamArgs {
 };
 
 // Up to 16 vectors: the weights go from memory to registers once, requested before anything else is waited for and again as
-// soon as a register is free; the vectors lie in LDS as bf16 values, put there by every block for itself.  A wave multiplies 16
+// soon as they are multiplied (as compiled into other registers, which are waited for and moved at a turn's end); the vectors lie in LDS as bf16 values, put there by every block for itself.  A wave multiplies 16
 // rows at a time; `split` waves share them, each with its range of the columns.  Lane (i, g) has row i and of every 128 columns
 // the 16-byte pieces g and g + 4.  Bound by the weights' way: 50000 x 512 x 5 in 8.9 us (26.9 MB, 3.0 TB/s; the kernel 8.0, of which
 // a launch, the vectors' quantization and the last stores are some 3.5), 250000 x 1024 x 8 in 43 (5.9 TB/s; 52 with the weights out of
@@ -560,7 +561,8 @@ __global__ __launch_bounds__(512) void f8_stream_kernel(F8StreamArgs a)
         if (4 * g + v < n) m.Y[(size_t)(4 * g + v) * m.ldy + r] = m.bias ? sum[v] + add : sum[v];
 }
 
-// split: waves for a row's columns, a power of two, at most `waves`; every one has columns, a multiple of four blocks of them.
+// split: waves for a row's columns, a power of two, at most `waves`.  A part is a multiple of four blocks of columns, so that the last ones
+// may have none (of 9 to 12 blocks in 4 parts one, of 17 to 20 in 8 three): their sums are zeros.
 static q8_status launch_stream(q8_ctx *ctx, F8StreamArgs &a, int waves, int split)
 {
     a.split = split;

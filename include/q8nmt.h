@@ -610,7 +610,8 @@ q8_status output_logits_f32(q8_ctx *ctx, const q8_readout_weights_f32 *ro, const
 typedef struct {
     const uint8_t *data;   /* [rows x ld] codes, pad bytes [cols, ld) zero; 16-byte aligned, ld % 16 == 0, ld <= 16384 */
     const uint8_t *scale;  /* [rows x lds] bytes, one per block of 128 columns; 4-byte aligned, lds % 4 == 0, lds >= ceil(cols / 128);
-                              0 and 255 are no scales; what lies past a row's last block is not used */
+                              0 and 255 are no scales, and 3 to 246 hold every code exactly (else values go to multiples of 2^-133,
+                              and to infinity past fp32's range); what lies past a row's last block is not used */
     int rows, cols, ld, lds;
 } q8_mat_f8;
 

@@ -213,6 +213,21 @@ def test_scale_bytes_past_the_last_block_do_not_count(q, ctx, n, cols):
         assert (np_(q.q8_gemm_f8(ctx, W, X)) == want).all(), byte
 
 
+@pytest.mark.parametrize("n", [2, 40, 200])
+@pytest.mark.parametrize("byte,other", [(3, 230), (246, 40)])
+def test_the_smallest_and_the_largest_scale_hold_every_code(q, ctx, n, byte, other):
+    """Every code times every scale from 3 to 246 is a bf16 value: 2^-9 2^(3 - 127) = 2^-133, the smallest there is, and 448 2^(246 - 127) < 2^128.
+    One product a result, exact in fp32."""
+    codes = np.array([c for c in range(256) if c & 127 != 127], np.uint8)
+    W, X = np.zeros((len(codes), 128), np.uint8), np.zeros((n, 128), np.uint8)
+    W[:, 77] = codes
+    X[:, 77] = ref.e4m3_round(np.where(np.arange(n) % 2, 1.0, -1.5))
+    sw, sx = np.full((len(codes), 4), byte, np.uint8), np.full((n, 4), other, np.uint8)
+    dev = lambda c, s: q.MatF8(torch.from_numpy(c).to(ctx.device), torch.from_numpy(s).to(ctx.device), 128)
+    want = ref.values(X, sx, 128) @ ref.values(W, sw, 128).T
+    assert (np_(q.q8_gemm_f8(ctx, dev(W, sw), dev(X, sx))) == want).all()
+
+
 def test_product_over_its_vectors(q, ctx):
     """Results that overwrite the vectors they are made of."""
     for n in (2, 16, 90):

@@ -640,6 +640,66 @@ q8_status output_logits_f8(q8_ctx *ctx, const q8_readout_weights *ro, const q8_m
                            const float *y_emb, const float *ctx_vec, const float *t_in, int n, int k, float *logits, float *lse,
                            float *topk_logp, int32_t *topk_idx, float *t_out);
 
+/* ---- 4-bit weights with a scale and a zero point per group (beside 8-bit weights, for products bound by the weights' bytes) ----
+ * A row's columns in groups of 32, 64 or 128; a weight is (code - z) s with a code of 0 .. 15.  Codes lie in blocks of 128 columns, 16 words
+ * of 32 bits: word 4 g + t of a block has its columns 32 t + 8 g + (0 .. 7), column 2 j + e of those eight in bits 4 j + 16 e and up. */
+typedef struct {
+    const uint8_t *data;   /* [rows x ld] bytes; 16-byte aligned, ld % 64 == 0, ld >= 64 ceil(cols / 128), ld <= 8192; codes past the columns: any */
+    const uint32_t *scale; /* [rows x lds] words, one per group: the upper 16 bits those of s as an fp32 number whose other bits are zero, the
+                              lowest four z, the others zero; 16-byte aligned, lds % 4 == 0, lds >= ceil(cols / group); words past a row's last group: any */
+    int rows, cols, ld, lds, group;
+} q8_mat_w4;
+
+/* X fp32 [rows x cols] (ld_in floats per row) -> the codes and words that `out` points to.  Per group lo = min(0, least value), hi = max(0,
+ * largest): s = (hi - lo) / 15 rounded up to 8 significant bits, z = rint(-lo / s), code = rint(x / s) + z within 0 .. 15 (fp32 quotients, ties to
+ * even); a group of magnitudes below 2^-100 has s = 1, z = 0 and codes 0.  Infinities take the ends of the range that the finite values have, NaN counts as 0.
+ * Codes past the columns are those of 0, words past the last group 1.0.  rows <= 2^24, rows * max(ld / 64, lds group / 128) < 2^27.  Enqueued;
+ * nothing returns to the host. */
+q8_status q8_quantize_matrix_w4(q8_ctx *ctx, const float *X, int rows, int cols, int ld_in, const q8_mat_w4 *out);
+
+/* Y[j][i] = sum_k W[i][k] X[j][k] + bias[i] (bias may be NULL) for n fp32 vectors X [n x ldx] (16-byte aligned, ldx % 4 == 0), Y [n x ldy] fp32,
+ * elements past a vector's W->rows untouched.  X is not quantized: its values are held within 2^-22 of themselves (or 2^-38 of the
+ * vector's largest; blocks of 128, or vectors, of magnitudes below 2^-100 count as zeros), products and sums in fp32.  A value that is not
+ * finite stays with its vector.  Y may overlap X.  1 <= n <= 2^20, as far as a launch holds the results.  Workspace: the context's must have
+ * q8_gemm_w4_bytes(n, W->cols) bytes. */
+size_t q8_gemm_w4_bytes(int n, int cols);
+q8_status q8_gemm_w4(q8_ctx *ctx, const q8_mat_w4 *W, const float *X, int n, int ldx, const float *bias, float *Y, int ldy);
+
+/* output_logits_f8 with the vocabulary matrix in 4 bits. */
+q8_status output_logits_w4(q8_ctx *ctx, const q8_readout_weights *ro, const q8_mat_w4 *W_out, const float *b_out, const float *s,
+                           const float *y_emb, const float *ctx_vec, const float *t_in, int n, int k, float *logits, float *lse,
+                           float *topk_logp, int32_t *topk_idx, float *t_out);
+
+/* ---- the gated delta rule (a recurrent cell beside the GRU whose state is a matrix per head) ----
+ * Per token and head, with the state S [dk x dv], key k, query q [dk], value v [dv], a = exp(g) and b = beta:
+ *   S = a S;  u = b (v - S^T k);  S = S + k u^T;  o = S^T q.
+ * Query head h / (hv / hk) serves value head h.  normalize != 0: k / sqrt(|k|^2 + 1e-6) and q / sqrt(|q|^2 + 1e-6) in the places of k and q; q is
+ * multiplied by `scale` either way.  g <= 0 (the logarithm of the decay; -inf or the lowest value: the state is forgotten), b in [0, 2], keys of at
+ * most unit length keep states bounded; other values are computed as written.  All numbers fp32.  Row t of every table is
+ * token t (or slot t): q, k [. x ldq, ldk] with hk dk, v [. x ldv] with hv dv, g, beta [. x ldg, ldb] with hv numbers side by side, of any alignment
+ * (states, values and results in whole 16 bytes are faster).  1 <= dk, dv <= 256, hv a multiple of hk. */
+typedef struct {
+    const float *q, *k, *v, *g, *beta;
+    int ldq, ldk, ldv, ldg, ldb;
+    int hk, hv, dk, dv;
+    float scale;
+    int normalize;
+} q8_delta_inputs;
+
+/* One token for n slots: out [n x ldo] (hv dv numbers a slot) and state_out [n x hv x dk x dv].  Slot j starts from state[parent[j]], the search's
+ * back pointers (parent: n numbers on the device; NULL: from state[j], and slots == n); a parent outside [0, slots), or state == NULL: from zeros.
+ * Without parents state_out may be state; else they must not overlap.  out overlaps no input. */
+q8_status q8_delta_step(q8_ctx *ctx, const q8_delta_inputs *in, int n, const float *state, int slots, const int32_t *parent, float *state_out,
+                        float *out, int ldo);
+
+/* n_seq sequences laid end to end: sequence s has the tokens off[s] .. off[s + 1] - 1 (off: n_seq + 1 numbers on the device, ascending, within
+ * [0, L]; one without tokens keeps its state).  out [L x ldo]: rows that belong to no sequence stay as they are.  state (NULL: zeros) and state_out (may be NULL; may be
+ * state) [n_seq x hv x dk x dv].  L <= 2^24, n_seq <= 65536, and (L / 32 + n_seq) hv, n_seq hv < 2^24.  out overlaps no input.  Workspace: the context's must have
+ * q8_delta_bytes(L, n_seq, hv, dk, dv) bytes. */
+size_t q8_delta_bytes(int L, int n_seq, int hv, int dk, int dv);
+q8_status q8_delta_sequence(q8_ctx *ctx, const q8_delta_inputs *in, int L, const int32_t *off, int n_seq, const float *state, float *state_out,
+                            float *out, int ldo);
+
 /* ---- drawing a token (beside the search: one hypothesis per row, no beam) ----
  * Row j of logits [n x ldl] (V floats) has its own temperature T, top-k, top-p and min-p (device arrays of n; NULL: T = 1,
  * filters not in force).  The words are ordered by (logit descending, index ascending); a word whose logit is -inf or NaN is

@@ -20,7 +20,8 @@ __all__ = ["Q8Error", "Context", "Mat", "Codes", "RowCodes", "GruWeights", "Cgru
            "q8_beam_update_batch", "q8_beam_result_batch", "q8_translate_batch", "q8_translate_batch_bytes",
            "KERNEL_CLASSES", "LIB_PATH", "source_ids",
            "cgru_decoder_step_noalloc_q8", "q8_noalloc_setup", "q8_noalloc_scratch_bytes",
-           "MatF8", "q8_quantize_matrix_f8", "q8_gemm_f8", "q8_gemm_f8_bytes", "output_logits_f8", "q8_sample_logits", "q8_sample_bytes"]
+           "MatF8", "q8_quantize_matrix_f8", "q8_gemm_f8", "q8_gemm_f8_bytes", "output_logits_f8", "q8_sample_logits", "q8_sample_bytes",
+           "MatW4", "q8_quantize_matrix_w4", "q8_gemm_w4", "q8_gemm_w4_bytes", "output_logits_w4", "q8_delta_step", "q8_delta_sequence", "q8_delta_bytes"]
 LIB_PATH = _LIB_PATH
 
 STATUS = {0: "Q8_OK", 1: "Q8_ERR_NULL", 2: "Q8_ERR_SHAPE", 3: "Q8_ERR_ALIGN", 4: "Q8_ERR_WORKSPACE", 5: "Q8_ERR_DEVICE"}
@@ -47,6 +48,15 @@ class _Codes(C.Structure):
 
 class _MatF8(C.Structure):
     _fields_ = [("data", C.c_void_p), ("scale", C.c_void_p), ("rows", C.c_int), ("cols", C.c_int), ("ld", C.c_int), ("lds", C.c_int)]
+
+
+class _MatW4(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("scale", C.c_void_p), ("rows", C.c_int), ("cols", C.c_int), ("ld", C.c_int), ("lds", C.c_int), ("group", C.c_int)]
+
+
+class _DeltaInputs(C.Structure):
+    _fields_ = [(f, C.c_void_p) for f in ("q", "k", "v", "g", "beta")] + [(f, C.c_int) for f in ("ldq", "ldk", "ldv", "ldg", "ldb", "hk", "hv", "dk", "dv")] + \
+               [("scale", C.c_float), ("normalize", C.c_int)]
 
 
 class _Sampling(C.Structure):
@@ -172,6 +182,15 @@ def load_library():
         lib.q8_sample_bytes.restype = C.c_size_t
         lib.q8_sample_bytes.argtypes = [ci, ci]
         lib.q8_sample_logits.argtypes = [vp, vp, ci, ci, ci, C.POINTER(_Sampling), vp, vp, vp, vp, ci, vp]
+        lib.q8_quantize_matrix_w4.argtypes = [vp, vp, ci, ci, ci, C.POINTER(_MatW4)]
+        lib.q8_gemm_w4_bytes.restype = C.c_size_t
+        lib.q8_gemm_w4_bytes.argtypes = [ci, ci]
+        lib.q8_gemm_w4.argtypes = [vp, C.POINTER(_MatW4), vp, ci, ci, vp, vp, ci]
+        lib.output_logits_w4.argtypes = [vp, C.POINTER(_Readout), C.POINTER(_MatW4), vp, vp, vp, vp, vp, ci, ci, vp, vp, vp, vp, vp]
+        lib.q8_delta_step.argtypes = [vp, C.POINTER(_DeltaInputs), ci, vp, ci, vp, vp, vp, ci]
+        lib.q8_delta_bytes.restype = C.c_size_t
+        lib.q8_delta_bytes.argtypes = [ci] * 5
+        lib.q8_delta_sequence.argtypes = [vp, C.POINTER(_DeltaInputs), ci, vp, ci, vp, vp, vp, ci]
         lib.q8_profile_end.argtypes = [vp, C.POINTER(C.c_float), C.POINTER(C.c_int)]
         _lib = lib
     return _lib
@@ -1036,25 +1055,30 @@ def q8_gemm_f8(ctx, W, X, bias=None, Y=None, bind=False):
 
 def output_logits_f8(ctx, ro, W_out, b_out, s=None, y_emb=None, ctx_vec=None, t_in=None, k=12, want_logits=True, logits=None, bind=False):
     """output_logits_q8 with the vocabulary matrix a MatF8: dict(logits?, t, and for k > 0 lse, topk_logp, topk_idx)."""
+    return _output_logits_blocks(ctx, "output_logits_f8", ro, W_out, b_out, s, y_emb, ctx_vec, t_in, k, want_logits, logits, bind)
+
+
+def _output_logits_blocks(ctx, name, ro, W_out, b_out, s, y_emb, ctx_vec, t_in, k, want_logits, logits, bind):
     n = (t_in if ro is None else s).shape[0]
     V, R = W_out.rows, W_out.cols
     if logits is None and (want_logits or k == 0):
         logits = ctx.empty(n, V)
     given = [(t_in, "t_in", R)] if ro is None else [(s, "s", ro.W_s.cols), (y_emb, "y_emb", ro.W_y.cols), (ctx_vec, "ctx_vec", ro.W_c.cols)]
-    for t, name, cols in given + ([(logits, "logits", V)] if logits is not None else []):
+    for t, what, cols in given + ([(logits, "logits", V)] if logits is not None else []):
         if t is None or t.dtype != torch.float32 or tuple(t.shape) != (n, cols) or not t.is_cuda or not t.is_contiguous():
-            raise ValueError("%s: expected a contiguous fp32 device tensor %d x %d" % (name, n, cols))
+            raise ValueError("%s: expected a contiguous fp32 device tensor %d x %d" % (what, n, cols))
     _vector(b_out, "b_out", V)
-    _on_device(ctx, W_out=W_out.data, b_out=b_out, logits=logits, **{name: t for t, name, _ in given})
+    _on_device(ctx, W_out=W_out.data, b_out=b_out, logits=logits, **{what: t for t, what, _ in given})
     t = ctx.empty(n, R) if ro is not None else None
     lse, lp, idx = (ctx.empty(n), ctx.empty(n, k), ctx.empty(n, k, dtype=torch.int32)) if k > 0 else (None, None, None)
     args = (ctx.handle, C.byref(ro.c) if ro is not None else None, C.byref(W_out.c), _ptr(b_out), _ptr(s), _ptr(y_emb), _ptr(ctx_vec),
             _ptr(t_in), n, k, _ptr(logits), _ptr(lse), _ptr(lp), _ptr(idx), _ptr(t))
     r = {"logits": logits, "t": t, "lse": lse, "topk_logp": lp, "topk_idx": idx}
+    fn = getattr(ctx.lib, name)
     if bind:
         r["keep"] = (ro, W_out, b_out, s, y_emb, ctx_vec, t_in)
-        return _Bound(ctx, ctx.lib.output_logits_f8, args, r)
-    ctx.check(ctx.lib.output_logits_f8(*args))
+        return _Bound(ctx, fn, args, r)
+    ctx.check(fn(*args))
     return r
 
 
@@ -1103,4 +1127,149 @@ def q8_sample_logits(ctx, logits, u, temperature=None, top_k=None, top_p=None, m
         r["keep"] = (logits, u, p, sampling, E_tgt)
         return _Bound(ctx, ctx.lib.q8_sample_logits, args, r)
     ctx.check(ctx.lib.q8_sample_logits(*args))
+    return r
+
+
+# ---- 4-bit weights with a scale and a zero point per group, and the gated delta rule ----
+
+class MatW4:
+    """q8_mat_w4: 4-bit codes [rows x ld bytes] (uint8) and the words of their groups [rows x lds] (int32) on the device."""
+
+    def __init__(self, data, scale, cols, group):
+        _rows(data, "codes", torch.uint8)
+        _rows(scale, "scales", torch.int32)
+        if not (data.is_contiguous() and scale.is_contiguous()) or scale.shape[0] != data.shape[0]:
+            raise ValueError("codes and scales must be contiguous, with as many rows each")
+        if data.device != scale.device:
+            raise ValueError("codes on %s, scales on %s" % (data.device, scale.device))
+        self.data, self.scale, self.cols, self.group = data, scale, cols, group
+        self.rows, self.ld = data.shape
+        self.c = _MatW4(data.data_ptr(), scale.data_ptr(), self.rows, cols, self.ld, scale.shape[1], group)
+
+
+def q8_quantize_matrix_w4(ctx, W, group=128, bind=False):
+    """Rows of W in 4 bits with a scale and a zero point per `group` (32, 64, 128) columns: a MatW4."""
+    if group not in (32, 64, 128):
+        raise ValueError("group: 32, 64 or 128 columns, got %s" % (group,))
+    if not (isinstance(W, torch.Tensor) and W.device == ctx.workspace.device and W.dtype == torch.float32):
+        with torch.cuda.stream(ctx.stream):
+            W = ctx.f32(W)
+    ld_in = _rows(W, "W")
+    rows, cols = W.shape
+    out = MatW4(ctx.empty(rows, (cols + 127) // 128 * 64, dtype=torch.uint8),
+                ctx.empty(rows, ((cols + group - 1) // group + 3) // 4 * 4, dtype=torch.int32), cols, group)
+    args = (ctx.handle, _ptr(W), rows, cols, ld_in, C.byref(out.c))
+    if bind:
+        return _Bound(ctx, ctx.lib.q8_quantize_matrix_w4, args, {"W": out, "keep": W})
+    ctx.check(ctx.lib.q8_quantize_matrix_w4(*args))
+    return out
+
+
+def q8_gemm_w4_bytes(n, cols):
+    """Workspace bytes of a context for q8_gemm_w4."""
+    return load_library().q8_gemm_w4_bytes(n, cols)
+
+
+def q8_gemm_w4(ctx, W, X, bias=None, Y=None, bind=False):
+    """Y [n x W.rows] = X W^T + bias for fp32 vectors X [n x W.cols] and a MatW4."""
+    ldx = _rows(X, "X", cols=W.cols)
+    n = X.shape[0]
+    Y = ctx.empty(n, W.rows) if Y is None else Y
+    ldy = _rows(Y, "Y", cols=W.rows)
+    if Y.shape[0] != n:
+        raise ValueError("Y: expected %d rows, got %d" % (n, Y.shape[0]))
+    _vector(bias, "bias", W.rows)
+    _on_device(ctx, W=W.data, X=X, bias=bias, Y=Y)
+    args = (ctx.handle, C.byref(W.c), _ptr(X), n, ldx, _ptr(bias), _ptr(Y), ldy)
+    if bind:
+        return _Bound(ctx, ctx.lib.q8_gemm_w4, args, {"Y": Y, "keep": (W, X, bias)})
+    ctx.check(ctx.lib.q8_gemm_w4(*args))
+    return Y
+
+
+def output_logits_w4(ctx, ro, W_out, b_out, s=None, y_emb=None, ctx_vec=None, t_in=None, k=12, want_logits=True, logits=None, bind=False):
+    """output_logits_q8 with the vocabulary matrix a MatW4: dict(logits?, t, and for k > 0 lse, topk_logp, topk_idx)."""
+    return _output_logits_blocks(ctx, "output_logits_w4", ro, W_out, b_out, s, y_emb, ctx_vec, t_in, k, want_logits, logits, bind)
+
+
+def _heads(t, name, shape):
+    """Checks a device tensor [tokens, ...] of fp32 whose dimensions past the first are contiguous; returns its pitch."""
+    if t.dtype != torch.float32 or tuple(t.shape) != tuple(shape) or not t.is_cuda:
+        raise ValueError("%s: expected a float32 device tensor %s, got %s %s on %s" % (name, tuple(shape), t.dtype, tuple(t.shape), t.device))
+    run = 1
+    for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+        if size > 1 and stride != run:
+            raise ValueError("%s: the numbers of a token must be contiguous (strides %s)" % (name, t.stride()))
+        run *= size
+    return t.stride(0) if t.shape[0] > 1 else run
+
+
+def _delta_inputs(ctx, q, k, v, g, beta, scale, normalize):
+    if q.dim() != 3 or v.dim() != 3:
+        raise ValueError("q, k: expected [tokens, heads, dk], v: [tokens, heads, dv]")
+    N, hk, dk = q.shape
+    hv, dv = v.shape[1:]
+    lds = [_heads(t, name, shape) for t, name, shape in ((q, "q", (N, hk, dk)), (k, "k", (N, hk, dk)), (v, "v", (N, hv, dv)), (g, "g", (N, hv)), (beta, "beta", (N, hv)))]
+    _on_device(ctx, q=q, k=k, v=v, g=g, beta=beta)
+    return _DeltaInputs(q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(), beta.data_ptr(), *lds, hk, hv, dk, dv, float(scale), int(bool(normalize)))
+
+
+def _state(t, name, shape):
+    if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != tuple(shape) or not t.is_cuda or not t.is_contiguous()):
+        raise ValueError("%s: expected a contiguous float32 device tensor %s, got %s %s" % (name, tuple(shape), t.dtype, tuple(t.shape)))
+
+
+def q8_delta_step(ctx, q, k, v, g, beta, state=None, scale=1.0, normalize=True, parent=None, state_out=None, out=None, bind=False):
+    """One token of the gated delta rule for n slots: q, k [n, hk, dk], v [n, hv, dv], g, beta [n, hv], state [slots, hv, dk, dv] (None: zeros),
+    parent [n] int32 or None.  Returns dict(out [n, hv, dv], state [n, hv, dk, dv]); without state_out and without parents the
+    state is updated in place."""
+    c = _delta_inputs(ctx, q, k, v, g, beta, scale, normalize)
+    n, hv, dv = v.shape
+    shape = (n, hv, q.shape[2], dv)
+    slots = state.shape[0] if state is not None else n
+    _state(state, "state", (slots,) + shape[1:])
+    _vector(parent, "parent", n, torch.int32)
+    if state_out is None:
+        state_out = state if parent is None and state is not None else ctx.empty(*shape)
+    _state(state_out, "state_out", shape)
+    out = ctx.empty(n, hv, dv) if out is None else out
+    ldo = _heads(out, "out", (n, hv, dv))
+    _on_device(ctx, state=state, parent=parent, state_out=state_out, out=out)
+    args = (ctx.handle, C.byref(c), n, _ptr(state), slots, _ptr(parent), _ptr(state_out), _ptr(out), ldo)
+    r = {"out": out, "state": state_out}
+    if bind:
+        r["keep"] = (c, q, k, v, g, beta, state, parent)
+        return _Bound(ctx, ctx.lib.q8_delta_step, args, r)
+    ctx.check(ctx.lib.q8_delta_step(*args))
+    return r
+
+
+def q8_delta_bytes(L, n_seq, hv, dk, dv):
+    """Workspace bytes of a context for q8_delta_sequence."""
+    return load_library().q8_delta_bytes(L, n_seq, hv, dk, dv)
+
+
+def q8_delta_sequence(ctx, q, k, v, g, beta, sent_off, scale=1.0, normalize=True, state=None, state_out=None, out=None, bind=False):
+    """The gated delta rule over sequences laid end to end: q, k [L, hk, dk], v [L, hv, dv], g, beta [L, hv]; sent_off: device int32
+    [sequences + 1]; state [sequences, hv, dk, dv] or None (zeros).  Returns dict(out [L, hv, dv], state): rows of out that belong to no
+    sequence are left as they are."""
+    c = _delta_inputs(ctx, q, k, v, g, beta, scale, normalize)
+    L, hv, dv = v.shape
+    S = sent_off.numel() - 1
+    _vector(sent_off, "sent_off", S + 1, torch.int32)
+    if S < 1:
+        raise ValueError("sent_off: at least two numbers")
+    shape = (S, hv, q.shape[2], dv)
+    state_out = ctx.empty(*shape) if state_out is None else state_out
+    _state(state, "state", shape)
+    _state(state_out, "state_out", shape)
+    out = ctx.empty(L, hv, dv) if out is None else out
+    ldo = _heads(out, "out", (L, hv, dv))
+    _on_device(ctx, sent_off=sent_off, state=state, state_out=state_out, out=out)
+    args = (ctx.handle, C.byref(c), L, _ptr(sent_off), S, _ptr(state), _ptr(state_out), _ptr(out), ldo)
+    r = {"out": out, "state": state_out}
+    if bind:
+        r["keep"] = (c, q, k, v, g, beta, sent_off, state)
+        return _Bound(ctx, ctx.lib.q8_delta_sequence, args, r)
+    ctx.check(ctx.lib.q8_delta_sequence(*args))
     return r

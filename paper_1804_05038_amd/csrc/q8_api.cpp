@@ -161,8 +161,8 @@ size_t q8_workspace_bytes(int max_n, int max_l, int max_rows, int max_ld)
     b += tiles + 65536;
     // calls that lay their room out otherwise: less than the above, unless the matrices have few rows
     const size_t layer = Q8_WS_HEADER + 5 * up256((size_t)max_n * max_rows * 4) + 4 * up256((size_t)max_n * ((max_ld + 15) & ~15)) +
-                         3 * up256((size_t)max_n * 4) + up256((size_t)max_n * (max_ld / 128 + 4)) + tiles;
-    return std::max({b, layer, q8_gemm_f8_bytes(max_n, max_ld), q8_sample_bytes(max_n, max_rows)});
+                         3 * up256((size_t)max_n * 4) + up256((size_t)max_n * (max_ld / 128 + 4)) + up256(q8i_gemm_w4_parts(max_n, max_ld)) + tiles;
+    return std::max({b, layer, q8_gemm_f8_bytes(max_n, max_ld), q8_gemm_w4_bytes(max_n, max_ld), q8_sample_bytes(max_n, max_rows)});
 }
 
 q8_status q8_create(q8_ctx **out, void *hip_stream, void *workspace, size_t workspace_bytes)
@@ -1848,13 +1848,13 @@ q8_status q8_gemm_f8(q8_ctx *ctx, const q8_mat_f8 *W, const float *X, int n, int
     return q8i_gemm_f8(ctx, W, &xq, X, ldx, bias, Y, ldy);
 }
 
-q8_status output_logits_f8(q8_ctx *ctx, const q8_readout_weights *ro, const q8_mat_f8 *W_out, const float *b_out, const float *s,
-                           const float *y_emb, const float *ctx_vec, const float *t_in, int n, int k, float *logits, float *lse,
-                           float *topk_logp, int32_t *topk_idx, float *t_out)
+namespace {
+// The output layer with the vocabulary matrix in 8-bit floating point (W8) or in 4 bits (W4), checked by the caller.
+q8_status output_logits_blocks(q8_ctx *ctx, const q8_readout_weights *ro, const q8_mat_f8 *W8, const q8_mat_w4 *W4, const float *b_out, const float *s,
+                               const float *y_emb, const float *ctx_vec, const float *t_in, int n, int k, float *logits, float *lse,
+                               float *topk_logp, int32_t *topk_idx, float *t_out)
 {
-    if (!ctx) return Q8_ERR_NULL;
-    TRY(check_mat_f8(ctx, W_out, kF8MaxRows, "W_out"));
-    const int R = W_out->cols, V = W_out->rows;
+    const int R = W4 ? W4->cols : W8->cols, V = W4 ? W4->rows : W8->rows;
     if (n <= 0 || n > kMaxMfmaN) return q8_fail(ctx, Q8_ERR_SHAPE, "n = %d outside [1, %d]", n, kMaxMfmaN);
     if (k < 0 || k > kMaxK || k > V) return q8_fail(ctx, Q8_ERR_SHAPE, "k = %d outside [0, min(%d, rows)]", k, kMaxK);
     if (k > 0 && V > q8i_out_max_rows()) return q8_fail(ctx, Q8_ERR_SHAPE, "W_out: more than %d rows", q8i_out_max_rows());
@@ -1891,13 +1891,14 @@ q8_status output_logits_f8(q8_ctx *ctx, const q8_readout_weights *ro, const q8_m
     } else {
         TRY(check_vecs(ctx, t_in, R, R, "t_in"));
     }
+    // the hidden vectors as the product takes them: codes and scales, or parts and scales
     q8_mat_f8 tq = {nullptr, nullptr, n, R, f8_pitch(R), f8_scale_pitch(R)};
-    uint8_t *codes = cv.take<uint8_t>((size_t)n * tq.ld), *scale = cv.take<uint8_t>((size_t)n * tq.lds);
+    uint8_t *codes = cv.take<uint8_t>(W4 ? q8i_gemm_w4_parts(n, R) : (size_t)n * tq.ld), *scale = cv.take<uint8_t>(W4 ? (size_t)n * 4 : (size_t)n * tq.lds);
     const size_t tiles = k > 0 ? (size_t)q8i_out_tiles(V) * n : 0;
     float *pm = k > 0 ? cv.take<float>(tiles) : nullptr;
     double *ps = k > 0 ? cv.take<double>(tiles) : nullptr;
     float *lg = logits ? logits : cv.take<float>((size_t)n * V);
-    if (!cv.ok) return q8_fail(ctx, Q8_ERR_WORKSPACE, "output_logits_f8: workspace too small");
+    if (!cv.ok) return q8_fail(ctx, Q8_ERR_WORKSPACE, "%s: workspace too small", W4 ? "output_logits_w4" : "output_logits_f8");
     if (ro && n <= kMaxNarrow) {
         TRY(q8i_readout(ctx, ro, s, y_emb, ctx_vec, n, t, nullptr));
     } else if (ro) {
@@ -1908,10 +1909,21 @@ q8_status output_logits_f8(q8_ctx *ctx, const q8_readout_weights *ro, const q8_m
     }
     tq.data = codes;
     tq.scale = scale;
-    TRY(q8i_gemm_f8(ctx, W_out, &tq, T, R, b_out, lg, V));
+    if (W4) TRY(q8i_gemm_w4(ctx, W4, T, n, R, b_out, lg, V, codes, (float *)scale));
+    else TRY(q8i_gemm_f8(ctx, W8, &tq, T, R, b_out, lg, V));
     if (k == 0) return Q8_OK;
     TRY(q8i_tile_stats(ctx, lg, n, V, pm, ps));
     return q8i_select_logits(ctx, pm, ps, lg, V, n, k, lse, topk_logp, topk_idx);
+}
+}  // namespace
+
+q8_status output_logits_f8(q8_ctx *ctx, const q8_readout_weights *ro, const q8_mat_f8 *W_out, const float *b_out, const float *s,
+                           const float *y_emb, const float *ctx_vec, const float *t_in, int n, int k, float *logits, float *lse,
+                           float *topk_logp, int32_t *topk_idx, float *t_out)
+{
+    if (!ctx) return Q8_ERR_NULL;
+    TRY(check_mat_f8(ctx, W_out, kF8MaxRows, "W_out"));
+    return output_logits_blocks(ctx, ro, W_out, nullptr, b_out, s, y_emb, ctx_vec, t_in, n, k, logits, lse, topk_logp, topk_idx, t_out);
 }
 
 size_t q8_sample_bytes(int n, int V)
@@ -1936,6 +1948,122 @@ q8_status q8_sample_logits(q8_ctx *ctx, const float *logits, int n, int V, int l
     char *state = cv.take<char>(q8i_sample_bytes(n, V));
     if (!cv.ok) return q8_fail(ctx, Q8_ERR_WORKSPACE, "q8_sample_logits: workspace too small");
     return q8i_sample(ctx, logits, n, V, ldl, sampling, u, tokens, logp, E_tgt, E, y_emb, state);
+}
+
+// ------------------------------------------------------------------------------- 4-bit weights ----
+
+namespace {
+q8_status check_mat_w4(q8_ctx *ctx, const q8_mat_w4 *W, const char *name)
+{
+    if (!W || !W->data || !W->scale) return q8_fail(ctx, Q8_ERR_NULL, "%s: NULL matrix", name);
+    if (W->group != 32 && W->group != 64 && W->group != 128) return q8_fail(ctx, Q8_ERR_SHAPE, "%s: groups of %d columns", name, W->group);
+    if (W->rows <= 0 || W->rows > kF8MaxRows || W->cols <= 0 || W->cols > kMaxLd || W->ld < 64 * f8_blocks(W->cols) || W->ld > kMaxLd / 2 ||
+        W->lds < (W->cols + W->group - 1) / W->group || W->lds > kMaxLd)
+        return q8_fail(ctx, Q8_ERR_SHAPE, "%s: bad shape %d x %d (ld %d, lds %d)", name, W->rows, W->cols, W->ld, W->lds);
+    if (!aligned16(W->data) || W->ld % 64 != 0 || !aligned16(W->scale) || W->lds % 4 != 0)
+        return q8_fail(ctx, Q8_ERR_ALIGN, "%s: codes and scales need 16-byte aligned bases, ld %% 64 == 0, lds %% 4 == 0", name);
+    return Q8_OK;
+}
+}  // namespace
+
+q8_status q8_quantize_matrix_w4(q8_ctx *ctx, const float *X, int rows, int cols, int ld_in, const q8_mat_w4 *out)
+{
+    if (!ctx) return Q8_ERR_NULL;
+    if (!X) return q8_fail(ctx, Q8_ERR_NULL, "q8_quantize_matrix_w4: NULL argument");
+    TRY(check_mat_w4(ctx, out, "q8_quantize_matrix_w4"));
+    if (rows != out->rows || cols != out->cols) return q8_fail(ctx, Q8_ERR_SHAPE, "q8_quantize_matrix_w4: %d x %d into %d x %d", rows, cols, out->rows, out->cols);
+    if (rows > 1 && ld_in < cols) return q8_fail(ctx, Q8_ERR_SHAPE, "q8_quantize_matrix_w4: ld_in %d < cols %d", ld_in, cols);
+    if ((uintptr_t)X % 4 != 0) return q8_fail(ctx, Q8_ERR_ALIGN, "q8_quantize_matrix_w4: X is not aligned to 4 bytes");
+    return q8i_quantize_w4(ctx, X, rows, cols, ld_in, out);
+}
+
+size_t q8_gemm_w4_bytes(int n, int cols)
+{
+    if (n <= 0 || n > kF8MaxN || cols <= 0 || cols > kMaxLd) return Q8_WS_HEADER;
+    return Q8_WS_HEADER + up256(q8i_gemm_w4_parts(n, cols)) + up256((size_t)n * 4);
+}
+
+q8_status q8_gemm_w4(q8_ctx *ctx, const q8_mat_w4 *W, const float *X, int n, int ldx, const float *bias, float *Y, int ldy)
+{
+    if (!ctx) return Q8_ERR_NULL;
+    TRY(check_mat_w4(ctx, W, "W"));
+    if (n <= 0 || n > kF8MaxN) return q8_fail(ctx, Q8_ERR_SHAPE, "n = %d outside [1, %d]", n, kF8MaxN);
+    TRY(check_vecs(ctx, X, n == 1 ? W->cols + ((4 - W->cols % 4) % 4) : ldx, W->cols, "X"));
+    TRY(check_result_f8(ctx, bias, Y, n, W->rows, ldy));
+    Carver cv(ctx);
+    uint8_t *parts = cv.take<uint8_t>(q8i_gemm_w4_parts(n, W->cols));
+    float *sx = cv.take<float>(n);
+    if (!cv.ok) return q8_fail(ctx, Q8_ERR_WORKSPACE, "q8_gemm_w4: workspace too small");
+    return q8i_gemm_w4(ctx, W, X, n, ldx, bias, Y, ldy, parts, sx);
+}
+
+q8_status output_logits_w4(q8_ctx *ctx, const q8_readout_weights *ro, const q8_mat_w4 *W_out, const float *b_out, const float *s,
+                           const float *y_emb, const float *ctx_vec, const float *t_in, int n, int k, float *logits, float *lse,
+                           float *topk_logp, int32_t *topk_idx, float *t_out)
+{
+    if (!ctx) return Q8_ERR_NULL;
+    TRY(check_mat_w4(ctx, W_out, "W_out"));
+    return output_logits_blocks(ctx, ro, nullptr, W_out, b_out, s, y_emb, ctx_vec, t_in, n, k, logits, lse, topk_logp, topk_idx, t_out);
+}
+
+// ------------------------------------------------------------------------ the gated delta rule ----
+
+namespace {
+const int kDeltaMaxDim = 256, kDeltaMaxHeads = 1024, kDeltaMaxL = 1 << 24, kDeltaMaxSeq = 65536;
+
+q8_status check_delta(q8_ctx *ctx, const q8_delta_inputs *in, int rows, const float *out, int ldo)
+{
+    if (!in || !in->q || !in->k || !in->v || !in->g || !in->beta || !out) return q8_fail(ctx, Q8_ERR_NULL, "delta rule: NULL argument");
+    if (in->dk <= 0 || in->dk > kDeltaMaxDim || in->dv <= 0 || in->dv > kDeltaMaxDim) return q8_fail(ctx, Q8_ERR_SHAPE, "delta rule: heads of %d x %d", in->dk, in->dv);
+    if (in->hk <= 0 || in->hv <= 0 || in->hv > kDeltaMaxHeads || in->hv % in->hk) return q8_fail(ctx, Q8_ERR_SHAPE, "delta rule: %d heads of keys, %d of values", in->hk, in->hv);
+    if (rows > 1 && (in->ldq < in->hk * in->dk || in->ldk < in->hk * in->dk || in->ldv < in->hv * in->dv || in->ldg < in->hv || in->ldb < in->hv || ldo < in->hv * in->dv))
+        return q8_fail(ctx, Q8_ERR_SHAPE, "delta rule: a leading dimension is less than its row");
+    const void *p4[] = {in->q, in->k, in->v, in->g, in->beta, out};
+    for (const void *p : p4)
+        if ((uintptr_t)p % 4 != 0) return q8_fail(ctx, Q8_ERR_ALIGN, "delta rule: a buffer is not aligned to 4 bytes");
+    return Q8_OK;
+}
+}  // namespace
+
+q8_status q8_delta_step(q8_ctx *ctx, const q8_delta_inputs *in, int n, const float *state, int slots, const int32_t *parent, float *state_out,
+                        float *out, int ldo)
+{
+    if (!ctx) return Q8_ERR_NULL;
+    if (n <= 0 || n > kDeltaMaxSeq) return q8_fail(ctx, Q8_ERR_SHAPE, "q8_delta_step: n = %d outside [1, %d]", n, kDeltaMaxSeq);
+    TRY(check_delta(ctx, in, n, out, ldo));
+    if (!state_out) return q8_fail(ctx, Q8_ERR_NULL, "q8_delta_step: state_out: NULL");
+    if (state && (slots <= 0 || slots > kDeltaMaxSeq || (!parent && slots != n))) return q8_fail(ctx, Q8_ERR_SHAPE, "q8_delta_step: %d slots of states, %d of results", slots, n);
+    if ((size_t)n * in->hv >= 1u << 24) return q8_fail(ctx, Q8_ERR_SHAPE, "q8_delta_step: %d slots of %d heads are too many for a launch", n, in->hv);
+    if ((uintptr_t)state % 4 != 0 || (uintptr_t)state_out % 4 != 0 || (uintptr_t)parent % 4 != 0) return q8_fail(ctx, Q8_ERR_ALIGN, "q8_delta_step: a buffer is not aligned to 4 bytes");
+    const size_t one = (size_t)in->hv * in->dk * in->dv * 4;
+    const uintptr_t a0 = (uintptr_t)state, a1 = a0 + one * (state ? slots : 0), b0 = (uintptr_t)state_out, b1 = b0 + one * n;
+    if (state && (parent || a0 != b0) && a0 < b1 && b0 < a1) return q8_fail(ctx, Q8_ERR_SHAPE, "q8_delta_step: state_out lies over states that are still to be read");
+    return q8i_delta_step(ctx, in, n, state, slots, parent, state_out, out, ldo);
+}
+
+size_t q8_delta_bytes(int L, int n_seq, int hv, int dk, int dv)
+{
+    if (L < 0 || L > kDeltaMaxL || n_seq <= 0 || n_seq > kDeltaMaxSeq || hv <= 0 || hv > kDeltaMaxHeads || dk <= 0 || dk > kDeltaMaxDim || dv <= 0 || dv > kDeltaMaxDim)
+        return Q8_WS_HEADER;
+    return Q8_WS_HEADER + up256(q8i_delta_room(L, n_seq, hv));
+}
+
+q8_status q8_delta_sequence(q8_ctx *ctx, const q8_delta_inputs *in, int L, const int32_t *off, int n_seq, const float *state, float *state_out,
+                            float *out, int ldo)
+{
+    if (!ctx) return Q8_ERR_NULL;
+    if (L < 0 || L > kDeltaMaxL || n_seq <= 0 || n_seq > kDeltaMaxSeq) return q8_fail(ctx, Q8_ERR_SHAPE, "q8_delta_sequence: %d tokens, %d sequences", L, n_seq);
+    TRY(check_delta(ctx, in, L, out, ldo));
+    if (!off) return q8_fail(ctx, Q8_ERR_NULL, "q8_delta_sequence: off: NULL");
+    if (((size_t)L / 32 + n_seq) * in->hv >= 1u << 24) return q8_fail(ctx, Q8_ERR_SHAPE, "q8_delta_sequence: %d tokens of %d heads are too many for a launch", L, in->hv);
+    if ((uintptr_t)state % 4 != 0 || (uintptr_t)state_out % 4 != 0 || (uintptr_t)off % 4 != 0) return q8_fail(ctx, Q8_ERR_ALIGN, "q8_delta_sequence: a buffer is not aligned to 4 bytes");
+    const size_t all = (size_t)n_seq * in->hv * in->dk * in->dv * 4;
+    const uintptr_t a0 = (uintptr_t)state, b0 = (uintptr_t)state_out;
+    if (state && state_out && a0 != b0 && a0 < b0 + all && b0 < a0 + all) return q8_fail(ctx, Q8_ERR_SHAPE, "q8_delta_sequence: state_out lies over states that are still to be read");
+    Carver cv(ctx);
+    float *room = (float *)cv.take<char>(q8i_delta_room(L, n_seq, in->hv));
+    if (!cv.ok) return q8_fail(ctx, Q8_ERR_WORKSPACE, "q8_delta_sequence: workspace too small");
+    return q8i_delta_sequence(ctx, in, L, off, n_seq, state, state_out, out, ldo, room);
 }
 
 }  // extern "C"

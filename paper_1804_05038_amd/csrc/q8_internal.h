@@ -347,6 +347,14 @@ q8_status q8i_select_logits(q8_ctx *ctx, const float *part_max, const double *pa
 q8_status q8i_quantize_f8(q8_ctx *ctx, const float *X, int rows, int cols, int ldx, uint8_t *codes, int ld, uint8_t *scale, int lds);
 // X in codes, or Xf in fp32 with X the room for its codes
 q8_status q8i_gemm_f8(q8_ctx *ctx, const q8_mat_f8 *W, const q8_mat_f8 *X, const float *Xf, int ldxf, const float *bias, float *Y, int ldy);
+// 4-bit weights: parts (q8i_gemm_w4_parts bytes) and sx [n] are room for the vectors
+q8_status q8i_quantize_w4(q8_ctx *ctx, const float *X, int rows, int cols, int ldx, const q8_mat_w4 *out);
+size_t q8i_gemm_w4_parts(int n, int cols);
+q8_status q8i_gemm_w4(q8_ctx *ctx, const q8_mat_w4 *W, const float *X, int n, int ldx, const float *bias, float *Y, int ldy, uint8_t *parts, float *sx);
+// the gated delta rule; room: q8i_delta_room bytes
+q8_status q8i_delta_step(q8_ctx *ctx, const q8_delta_inputs *in, int n, const float *state, int slots, const int *parent, float *state_out, float *out, int ldo);
+size_t q8i_delta_room(int L, int S, int hv);
+q8_status q8i_delta_sequence(q8_ctx *ctx, const q8_delta_inputs *in, int L, const int *off, int S, const float *state, float *state_out, float *out, int ldo, float *room);
 q8_status q8i_tile_stats(q8_ctx *ctx, const float *logits, int n, int V, float *part_max, double *part_sum);
 q8_status q8i_sample(q8_ctx *ctx, const float *logits, int n, int V, int ldl, const q8_sampling *s, const float *u, int32_t *tokens, float *logp,
                      const float *E_tgt, int E, float *y_emb, void *state);

@@ -1,0 +1,352 @@
+"""GPU parity of the gated delta rule, in steps and over sequences, with the rule in 64 bits token by token."""
+import numpy as np
+import pytest
+import torch
+
+import delta_reference as ref
+import w4_reference
+from parity import np_
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def q():
+    import paper_1804_05038_amd as q
+    return q
+
+
+@pytest.fixture(scope="module")
+def ctx(q):
+    return q.Context(workspace_bytes=64 << 20)
+
+
+def _inputs(rng, N, hk, hv, dk, dv, normalize=True):
+    f = lambda *s: rng.standard_normal(s).astype(np.float32)
+    x = {"q": f(N, hk, dk), "k": f(N, hk, dk) + np.float32(0.7) * f(hk, dk), "v": f(N, hv, dv), "g": -np.abs(f(N, hv)) * np.exp(-2 * rng.random((1, hv))).astype(np.float32),
+         "beta": (1 / (1 + np.exp(-f(N, hv)))).astype(np.float32)}
+    if not normalize:
+        x["k"] /= np.float32(1.01) * np.linalg.norm(x["k"], axis=2, keepdims=True)
+    return x
+
+
+def _dev(ctx, x):
+    return {k: ctx.f32(v) for k, v in x.items()}
+
+
+def _close(got, want, bound, dk):
+    """Within the bound for every number, and as a whole within what independent roundings leave: three sums in a row of up to dk + 2 C
+    products, each off by about 2^-24 of the root of their number, times eight."""
+    out, state = np_(got["out"]).astype(np.float64), np_(got["state"]).astype(np.float64)
+    assert np.isfinite(out).all() and np.isfinite(state).all()
+    assert (np.abs(out - want[0]) <= bound[0]).all()
+    assert (np.linalg.norm(state - want[1], axis=2) <= bound[1]).all()
+    for a, b in ((out, want[0]), (state, want[1])):
+        if b.size > 500:
+            assert np.linalg.norm(a - b) <= 8 * 3 * 2.0 ** -24 * np.sqrt(dk + 2 * ref.C) * np.linalg.norm(b)
+
+
+DIMS = [(1, 1, 1, 1), (1, 1, 64, 64), (2, 4, 128, 128), (1, 3, 33, 17), (2, 2, 32, 30), (4, 4, 5, 256), (1, 2, 256, 4), (3, 6, 100, 72), (1, 1, 127, 129), (2, 2, 200, 250), (1, 2, 256, 256), (8, 8, 16, 8)]
+
+
+# ---- one token ----
+
+@pytest.mark.parametrize("hk,hv,dk,dv", DIMS)
+@pytest.mark.parametrize("n", [1, 5, 33])
+def test_step(q, ctx, hk, hv, dk, dv, n):
+    rng = np.random.default_rng(hk + 3 * hv + 5 * dk + 7 * dv + n)
+    x = _inputs(rng, n, hk, hv, dk, dv)
+    S = rng.standard_normal((n, hv, dk, dv)).astype(np.float32)
+    st = ctx.f32(S)
+    got = q.q8_delta_step(ctx, **_dev(ctx, x), state=st, scale=0.3, state_out=torch.empty_like(st))
+    _close(got, ref.step(**x, state=S, scale=0.3), ref.step_bound(**x, state=S, scale=0.3), dk)
+    assert (np_(st) == S).all()
+    here = q.q8_delta_step(ctx, **_dev(ctx, x), state=st, scale=0.3)                 # in place: the same numbers
+    assert here["state"] is st and (np_(st) == np_(got["state"])).all() and (np_(here["out"]) == np_(got["out"])).all()
+
+
+@pytest.mark.parametrize("dk,dv", [(64, 64), (20, 13)])
+def test_step_takes_parents(q, ctx, dk, dv):
+    """Back pointers: states shared, unused, none (-1), out of range; fewer and more slots than states."""
+    rng = np.random.default_rng(dk)
+    for n, slots in ((7, 7), (9, 3), (2, 8)):
+        x = _inputs(rng, n, 2, 2, dk, dv)
+        S = rng.standard_normal((slots, 2, dk, dv)).astype(np.float32)
+        parent = rng.integers(0, slots, n).astype(np.int32)
+        parent[0], parent[-1] = slots - 1, -1
+        if n > 4:
+            parent[2], parent[3] = slots, 2 ** 31 - 1
+        got = q.q8_delta_step(ctx, **_dev(ctx, x), state=ctx.f32(S), parent=torch.from_numpy(parent).to(ctx.device))
+        _close(got, ref.step(**x, state=S, parent=parent), ref.step_bound(**x, state=S, parent=parent), dk)
+    none = q.q8_delta_step(ctx, **_dev(ctx, x))
+    _close(none, ref.step(**x, state=None), ref.step_bound(**x, state=None), dk)
+
+
+def _edges(rng, x):
+    """Decays that forget, gates that are shut or wide open, keys and queries of zeros."""
+    N, hv = x["g"].shape
+    x["g"][rng.random((N, hv)) < 0.15] = -np.inf
+    x["g"][rng.random((N, hv)) < 0.1] = np.finfo(np.float32).min
+    x["g"][rng.random((N, hv)) < 0.1] = -150.0
+    x["g"][rng.random((N, hv)) < 0.2] = 0.0
+    x["beta"][rng.random((N, hv)) < 0.2] = 0.0
+    x["beta"][rng.random((N, hv)) < 0.2] = 1.0
+    x["k"][rng.random(N) < 0.1] = 0.0
+    x["q"][rng.random(N) < 0.1] = 0.0
+
+
+@pytest.mark.parametrize("normalize", [True, False])
+def test_step_edges(q, ctx, normalize):
+    rng = np.random.default_rng(3)
+    x = _inputs(rng, 40, 2, 4, 24, 20, normalize)
+    _edges(rng, x)
+    S = rng.standard_normal((40, 4, 24, 20)).astype(np.float32)
+    got = q.q8_delta_step(ctx, **_dev(ctx, x), state=ctx.f32(S), normalize=normalize)
+    _close(got, ref.step(**x, state=S, normalize=normalize), ref.step_bound(**x, state=S, normalize=normalize), 24)
+
+
+def _strided(ctx, x, lead):
+    """q, k, v, gates as parts of one row a token, which begins `lead` floats past a 16-byte boundary; results at a pitch of their own."""
+    N = x["q"].shape[0]
+    parts = [np.reshape(x[f], (N, -1)) for f in ("q", "k", "v", "g", "beta")]
+    row = np.concatenate(parts, 1)
+    pitch = row.shape[1] + 3
+    buf = torch.full((N * pitch + 8,), float("nan"), device=ctx.device)
+    t = buf[lead:lead + N * pitch].view(N, pitch)
+    t[:, :row.shape[1]] = torch.from_numpy(row)
+    out, at = {}, 0
+    for f, p in zip(("q", "k", "v", "g", "beta"), parts):
+        out[f] = t[:, at:at + p.shape[1]].view(N, *x[f].shape[1:]) if x[f].ndim == 2 else t[:, at:at + p.shape[1]].unflatten(1, x[f].shape[1:])
+        at += p.shape[1]
+    return out
+
+
+@pytest.mark.parametrize("lead", [0, 1, 2])
+@pytest.mark.parametrize("dk,dv", [(32, 64), (30, 21)])
+def test_strides(q, ctx, lead, dk, dv):
+    rng = np.random.default_rng(lead)
+    N, hv = 70, 4
+    x = _inputs(rng, N, 2, hv, dk, dv)
+    v = _strided(ctx, x, lead)
+    big = torch.full((N, hv * dv + 5), 9.0, device=ctx.device)
+    out = big[:, :hv * dv].unflatten(1, (hv, dv))
+    off = [0, 41, 70]
+    got = q.q8_delta_sequence(ctx, **v, sent_off=torch.tensor(off, dtype=torch.int32, device=ctx.device), out=out)
+    _close(got, ref.sequence(**x, off=off), ref.sequence_bound(**x, off=off), dk)
+    assert (np_(big)[:, hv * dv:] == 9.0).all()
+    S = rng.standard_normal((N, hv, dk, dv)).astype(np.float32)
+    raw = torch.zeros(S.size + 4, device=ctx.device)
+    state = raw[lead:lead + S.size].view(S.shape)
+    state.copy_(torch.from_numpy(S))
+    big.fill_(9.0)
+    got = q.q8_delta_step(ctx, **v, state=state, out=out)
+    _close(got, ref.step(**x, state=S), ref.step_bound(**x, state=S), dk)
+    assert (np_(big)[:, hv * dv:] == 9.0).all() and (np_(raw)[:lead] == 0).all() and (np_(raw)[lead + S.size:] == 0).all()
+
+
+# ---- sequences ----
+
+LENGTHS = [[1], [2], [31], [32], [33], [64], [65], [200], [0], [0, 5, 0], [1, 1, 1, 40], [70, 0, 33, 32, 1, 31, 64], [3] * 50]
+
+
+@pytest.mark.parametrize("lengths", LENGTHS, ids=str)
+@pytest.mark.parametrize("hk,hv,dk,dv", [(1, 1, 64, 64), (2, 4, 33, 20)])
+def test_sequence_lengths(q, ctx, lengths, hk, hv, dk, dv):
+    """With states to start from, tokens in front of the first sequence and behind the last, whose results stay as they were."""
+    rng = np.random.default_rng(sum(lengths) + dk)
+    front, behind = 3, 4
+    off = [front] + [front + int(c) for c in np.cumsum(lengths)]
+    L = off[-1] + behind
+    x = _inputs(rng, L, hk, hv, dk, dv)
+    S = rng.standard_normal((len(lengths), hv, dk, dv)).astype(np.float32)
+    out = torch.full((L, hv, dv), 5.0, device=ctx.device)
+    got = q.q8_delta_sequence(ctx, **_dev(ctx, x), sent_off=torch.tensor(off, dtype=torch.int32, device=ctx.device), scale=0.5, state=ctx.f32(S), out=out)
+    assert (np_(out)[:front] == 5.0).all() and (np_(out)[off[-1]:] == 5.0).all()
+    out[:front] = 0.0
+    out[off[-1]:] = 0.0
+    _close(got, ref.sequence(**x, off=off, scale=0.5, state=S), ref.sequence_bound(**x, off=off, scale=0.5, state=S), dk)
+
+
+@pytest.mark.parametrize("hk,hv,dk,dv", DIMS)
+def test_sequence_dims(q, ctx, hk, hv, dk, dv):
+    rng = np.random.default_rng(hk + 3 * hv + 5 * dk + 7 * dv)
+    off = [0, 45, 110]
+    x = _inputs(rng, 110, hk, hv, dk, dv)
+    got = q.q8_delta_sequence(ctx, **_dev(ctx, x), sent_off=torch.tensor(off, dtype=torch.int32, device=ctx.device), scale=dk ** -0.5)
+    _close(got, ref.sequence(**x, off=off, scale=dk ** -0.5), ref.sequence_bound(**x, off=off, scale=dk ** -0.5), dk)
+
+
+@pytest.mark.parametrize("normalize", [True, False])
+def test_sequence_edges(q, ctx, normalize):
+    rng = np.random.default_rng(11)
+    off = [0, 100, 101, 180]
+    x = _inputs(rng, 180, 2, 4, 24, 20, normalize)
+    _edges(rng, x)
+    S = rng.standard_normal((3, 4, 24, 20)).astype(np.float32)
+    st = ctx.f32(S)
+    got = q.q8_delta_sequence(ctx, **_dev(ctx, x), sent_off=torch.tensor(off, dtype=torch.int32, device=ctx.device), normalize=normalize, state=st, state_out=st)
+    _close(got, ref.sequence(**x, off=off, normalize=normalize, state=S), ref.sequence_bound(**x, off=off, normalize=normalize, state=S), 24)
+
+
+def test_strong_decays_keep_the_weak_ones_exact(q, ctx):
+    """A sum of decays over a chunk is far larger than those that matter: differences of it must not lose them."""
+    rng = np.random.default_rng(2)
+    x = _inputs(rng, 64, 1, 2, 32, 32)
+    x["g"][:] = -0.01
+    x["g"][3:20] = -120.0
+    x["g"][40] = np.finfo(np.float32).min
+    got = q.q8_delta_sequence(ctx, **_dev(ctx, x), sent_off=torch.tensor([0, 64], dtype=torch.int32, device=ctx.device))
+    _close(got, ref.sequence(**x, off=[0, 64]), ref.sequence_bound(**x, off=[0, 64]), 32)
+
+
+def test_keys_that_repeat(q, ctx):
+    """The same key again and again with open gates: (I + A)^-1 is what a power series would not give."""
+    rng = np.random.default_rng(4)
+    x = _inputs(rng, 96, 1, 2, 64, 32)
+    x["k"][:] = x["k"][:1] + np.float32(1e-3) * rng.standard_normal(x["k"].shape).astype(np.float32)
+    x["beta"][:] = 1.0
+    x["g"][:] = 0.0
+    off = [0, 96]
+    got = q.q8_delta_sequence(ctx, **_dev(ctx, x), sent_off=torch.tensor(off, dtype=torch.int32, device=ctx.device))
+    want, bound = ref.sequence(**x, off=off), ref.sequence_bound(**x, off=off)
+    assert (np.abs(np_(got["out"]) - want[0]) <= bound[0]).all()
+    assert (np.linalg.norm(np_(got["state"]) - want[1], axis=2) <= bound[1]).all()
+
+
+def test_offsets_out_of_range_write_nothing_outside(q, ctx):
+    """Offsets that descend, lie below zero or past the last token: sequences without or with fewer tokens."""
+    rng = np.random.default_rng(6)
+    x = _inputs(rng, 50, 1, 1, 16, 16)
+    buf = torch.full((60, 1, 16), 3.0, device=ctx.device)
+    for off in ([-5, 20, 70], [0, 60, 2 ** 31 - 1], [50, 0, 50]):
+        got = q.q8_delta_sequence(ctx, **_dev(ctx, x), sent_off=torch.tensor(off, dtype=torch.int32, device=ctx.device), out=buf[:50])
+        assert np.isfinite(np_(got["state"])).all() and (np_(buf)[50:] == 3.0).all()
+    off = [0, 20, 50]
+    got = q.q8_delta_sequence(ctx, **_dev(ctx, x), sent_off=torch.tensor([-7, 20, 70], dtype=torch.int32, device=ctx.device))
+    _close(got, ref.sequence(**x, off=off), ref.sequence_bound(**x, off=off), 16)
+
+
+def test_a_prompt_and_then_steps(q, ctx):
+    """A sentence at once is the same sentence in two parts, and the same in steps, up to rounding."""
+    rng = np.random.default_rng(8)
+    L, hk, hv, dk, dv = 75, 2, 4, 64, 48
+    x = _inputs(rng, L, hk, hv, dk, dv)
+    d = _dev(ctx, x)
+    o = lambda *v: torch.tensor(v, dtype=torch.int32, device=ctx.device)
+    want, bound = ref.sequence(**x, off=[0, L]), ref.sequence_bound(**x, off=[0, L])
+    cut = lambda a, b: {k: v[a:b] for k, v in d.items()}
+    first = q.q8_delta_sequence(ctx, **cut(0, 40), sent_off=o(0, 40))
+    rest = q.q8_delta_sequence(ctx, **cut(40, L), sent_off=o(0, L - 40), state=first["state"])
+    got = {"out": torch.cat([first["out"], rest["out"]]), "state": rest["state"]}
+    _close(got, want, (2 * bound[0], 2 * bound[1]), dk)
+    st, outs = first["state"], [first["out"]]
+    for t in range(40, L):
+        r = q.q8_delta_step(ctx, **cut(t, t + 1), state=st)
+        outs.append(r["out"].clone())
+    _close({"out": torch.cat(outs), "state": st}, want, (2 * bound[0], 2 * bound[1]), dk)
+
+
+def test_one_after_the_other_on_streams_and_in_graphs(q):
+    """A sequence and steps captured on a stream of their own, replayed with other inputs and eager calls in between: every replay
+    gives the eager call's bits."""
+    st = torch.cuda.Stream()
+    L, hv, dk, dv = 100, 3, 40, 36
+    ctx = q.Context(workspace_bytes=q.q8_delta_bytes(L, 2, hv, dk, dv), stream=st)
+    rng = np.random.default_rng(9)
+    d = {k: ctx.f32(v) for k, v in _inputs(rng, L, hv, hv, dk, dv).items()}
+    off = torch.tensor([0, 60, 100], dtype=torch.int32, device=ctx.device)
+    torch.cuda.synchronize()
+    seq = q.q8_delta_sequence(ctx, **d, sent_off=off, bind=True)
+    parent = torch.tensor([1, 0], dtype=torch.int32, device=ctx.device)
+    two = {k: v[:2] for k, v in d.items()}
+    step = q.q8_delta_step(ctx, **two, state=seq.out["state"], parent=parent, bind=True)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=st):
+        seq.launch()
+        step.launch()
+    for t in range(4):
+        for k, v in _inputs(rng, L, hv, hv, dk, dv).items():
+            d[k].copy_(torch.from_numpy(v))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [np_(v).copy() for v in (seq.out["out"], seq.out["state"], step.out["out"], step.out["state"])]
+        seq.launch()
+        step.launch()
+        torch.cuda.synchronize()
+        for a, b in zip(got, (seq.out["out"], seq.out["state"], step.out["out"], step.out["state"])):
+            assert np.isfinite(a).all() and (a == np_(b)).all()
+
+
+def test_two_contexts_at_once(q):
+    """Calls on two streams with workspaces of their own do not touch each other."""
+    rng = np.random.default_rng(10)
+    L, h, d = 500, 2, 64
+    xs = [_inputs(rng, L, h, h, d, d) for _ in range(2)]
+    off = torch.tensor([0, L], dtype=torch.int32, device="cuda:0")
+    cs = [q.Context(workspace_bytes=q.q8_delta_bytes(L, 1, h, d, d), stream=torch.cuda.Stream()) for _ in range(2)]
+    ds = [_dev(c, x) for c, x in zip(cs, xs)]
+    alone = []
+    for c, x in zip(cs, ds):
+        torch.cuda.synchronize()
+        r = q.q8_delta_sequence(c, **x, sent_off=off)
+        torch.cuda.synchronize()
+        alone.append(np_(r["out"]).copy())
+    calls = [q.q8_delta_sequence(c, **x, sent_off=off, bind=True) for c, x in zip(cs, ds)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for call in calls:
+            call.launch()
+    torch.cuda.synchronize()
+    for call, a in zip(calls, alone):
+        assert (np_(call.out["out"]) == a).all()
+
+
+# ---- together ----
+
+def test_a_decoder_of_them(q):
+    """A layer as it is used: 4-bit projections of a prompt, the rule over it, then steps of a beam (projections, the rule with the search's
+    parents, the 4-bit output layer, a drawn word and its embedding), against the same in 64 bits on the values that the codes stand for."""
+    rng = np.random.default_rng(12)
+    E, hk, hv, dk, dv, V, beam, l = 96, 2, 4, 32, 40, 700, 3, 37
+    ctx = q.Context(workspace_bytes=max(q.q8_workspace_bytes(64, 64, 1024, 512), q.q8_sample_bytes(beam, V), q.q8_delta_bytes(l, 1, hv, dk, dv)))
+    f = lambda *s: rng.standard_normal(s).astype(np.float32)
+    rows = 2 * hk * dk + hv * dv + 2 * hv
+    W, Wo, emb = f(rows, E) / np.float32(np.sqrt(E)), f(V, hv * dv) / np.float32(10), f(V, E)
+    mw, mo = q.q8_quantize_matrix_w4(ctx, ctx.f32(W), group=32), q.q8_quantize_matrix_w4(ctx, ctx.f32(Wo), group=64)
+    wv, wo = w4_reference.values(*w4_reference.quantize(W, 32), 32), w4_reference.values(*w4_reference.quantize(Wo, 64), 64)
+
+    def parts(y):
+        a, b, c = hk * dk, 2 * hk * dk, 2 * hk * dk + hv * dv
+        split = lambda t, h: t.reshape(t.shape[0], h, -1) if isinstance(t, np.ndarray) else t.unflatten(1, (h, t.shape[1] // h))
+        return {"q": split(y[:, :a], hk), "k": split(y[:, a:b], hk), "v": split(y[:, b:c], hv)}, y[:, c:c + hv], y[:, c + hv:]
+
+    def layer(x):                                       # on the device
+        p, g, b = parts(q.q8_gemm_w4(ctx, mw, x))
+        return {**p, "g": -torch.nn.functional.softplus(g), "beta": torch.sigmoid(b)}
+
+    def layer64(x):
+        p, g, b = parts(x @ wv.T)
+        return {**p, "g": -np.log1p(np.exp(g)), "beta": 1 / (1 + np.exp(-b))}
+
+    src = rng.integers(0, V, l)
+    off = torch.tensor([0, l], dtype=torch.int32, device=ctx.device)
+    r = q.q8_delta_sequence(ctx, **layer(ctx.f32(emb[src])), sent_off=off, scale=dk ** -0.5)
+    o64, s64 = ref.sequence(**layer64(np.asarray(emb[src], np.float64)), off=[0, l], scale=dk ** -0.5)
+    near = lambda a, b: np.linalg.norm(np_(a) - b) <= 1e-5 * np.linalg.norm(b)
+    assert near(r["out"], o64) and near(r["state"], s64)
+    state, S = r["state"], s64
+    parent, x, x64 = np.zeros(beam, np.int32), ctx.f32(emb[src[:beam]]), emb[src[:beam]].astype(np.float64)
+    for t in range(4):
+        r = q.q8_delta_step(ctx, **layer(x), state=state, parent=torch.from_numpy(parent).to(ctx.device), scale=dk ** -0.5)
+        o64, S = ref.step(**layer64(x64), state=S, parent=parent, scale=dk ** -0.5)
+        assert near(r["out"], o64) and near(r["state"], S)
+        lg = q.output_logits_w4(ctx, None, mo, None, t_in=r["out"].reshape(beam, hv * dv), k=0)["logits"]
+        assert near(lg, o64.reshape(beam, -1) @ wo.T)
+        d = q.q8_sample_logits(ctx, lg, torch.rand(beam, device=ctx.device), top_k=5, E_tgt=ctx.f32(emb))
+        tok = np_(d["tokens"])
+        best = np.argsort(-np_(lg), axis=1)[:, :5]
+        assert all(tok[j] in best[j] for j in range(beam))
+        state, x, x64 = r["state"], d["y_emb"], np.asarray(emb[tok], np.float64)
+        parent = rng.integers(0, beam, beam).astype(np.int32)

@@ -677,7 +677,7 @@ q8_status output_logits_w4(q8_ctx *ctx, const q8_readout_weights *ro, const q8_m
  * multiplied by `scale` either way.  g <= 0 (the logarithm of the decay; -inf or the lowest value: the state is forgotten), b in [0, 2], keys of at
  * most unit length keep states bounded; other values are computed as written.  All numbers fp32.  Row t of every table is
  * token t (or slot t): q, k [. x ldq, ldk] with hk dk, v [. x ldv] with hv dv, g, beta [. x ldg, ldb] with hv numbers side by side, of any alignment
- * (states, values and results in whole 16 bytes are faster).  1 <= dk, dv <= 256, hv a multiple of hk. */
+ * (rows in whole 16 bytes are faster), pitches up to 2^22.  1 <= dk, dv <= 256, hv a multiple of hk. */
 typedef struct {
     const float *q, *k, *v, *g, *beta;
     int ldq, ldk, ldv, ldg, ldb;

@@ -2009,7 +2009,7 @@ q8_status output_logits_w4(q8_ctx *ctx, const q8_readout_weights *ro, const q8_m
 // ------------------------------------------------------------------------ the gated delta rule ----
 
 namespace {
-const int kDeltaMaxDim = 256, kDeltaMaxHeads = 1024, kDeltaMaxL = 1 << 24, kDeltaMaxSeq = 65536;
+const int kDeltaMaxDim = 256, kDeltaMaxHeads = 1024, kDeltaMaxL = 1 << 24, kDeltaMaxSeq = 65536, kDeltaMaxPitch = 1 << 22;
 
 q8_status check_delta(q8_ctx *ctx, const q8_delta_inputs *in, int rows, const float *out, int ldo)
 {
@@ -2018,6 +2018,8 @@ q8_status check_delta(q8_ctx *ctx, const q8_delta_inputs *in, int rows, const fl
     if (in->hk <= 0 || in->hv <= 0 || in->hv > kDeltaMaxHeads || in->hv % in->hk) return q8_fail(ctx, Q8_ERR_SHAPE, "delta rule: %d heads of keys, %d of values", in->hk, in->hv);
     if (rows > 1 && (in->ldq < in->hk * in->dk || in->ldk < in->hk * in->dk || in->ldv < in->hv * in->dv || in->ldg < in->hv || in->ldb < in->hv || ldo < in->hv * in->dv))
         return q8_fail(ctx, Q8_ERR_SHAPE, "delta rule: a leading dimension is less than its row");
+    for (const int ld : {in->ldq, in->ldk, in->ldv, ldo})
+        if (rows > 1 && ld > kDeltaMaxPitch) return q8_fail(ctx, Q8_ERR_SHAPE, "delta rule: a leading dimension above %d", kDeltaMaxPitch);
     const void *p4[] = {in->q, in->k, in->v, in->g, in->beta, out};
     for (const void *p : p4)
         if ((uintptr_t)p % 4 != 0) return q8_fail(ctx, Q8_ERR_ALIGN, "delta rule: a buffer is not aligned to 4 bytes");

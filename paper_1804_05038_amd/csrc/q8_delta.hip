@@ -1,10 +1,12 @@
 // q8_delta.hip -- the gated delta rule: per token and head S = a S, u = b (v - S^T k), S = S + k u^T, o = S^T q with a state S of
 // dk x dv numbers; one token for n slots, and whole sequences laid end to end.
 #include "q8_internal.h"
+#include "q8_parts.h"
 
 #include <math.h>
 
 typedef float v4f __attribute__((ext_vector_type(4)));
+typedef _Float16 v4h __attribute__((ext_vector_type(4)));
 
 #define DELTA_EPS 1e-6f              // of the unit length of queries and keys
 #define DELTA_LEAST (-200.0)         // decays below exp(-200) are zeros, and sums of these stay exact enough in 64 bits
@@ -176,7 +178,10 @@ q8_status q8i_delta_step(q8_ctx *ctx, const q8_delta_inputs *in, int n, const fl
 // A first launch forms T and the masked products of queries and keys of all chunks side by side, a second one carries the states
 // from chunk to chunk, a block per sequence, head and 32 columns of the state.
 #define DELTA_C 32
-#define DELTA_ROOM (2 * DELTA_C * DELTA_C + 4 * DELTA_C)     // floats of a chunk and head: T, M, then exp(c) / |k|, exp(c) scale / |q|, exp(c_C - c) / |k|, exp(c_C)
+#define DELTA_MATRIX (DELTA_C * DELTA_C)
+// What the first launch leaves of a chunk and head, in floats: T, M, then per token (6 x 32) exp(c) / |k|, exp(c) scale / |q| and exp(c_C - c) / |k|, each
+// times the power of two of its row, the inverses of those powers of the key's and the query's row, and exp(c_C)
+#define DELTA_ROOM (2 * DELTA_MATRIX + 6 * DELTA_C)
 
 struct DeltaSeqArgs {
     q8_delta_inputs in;
@@ -185,7 +190,7 @@ struct DeltaSeqArgs {
     float *room;
     const float *state;
     float *state_out, *out;
-    int ldo, vec_qk, vec;
+    int ldo, vec_qk, vec;            // vec_qk: rows of queries and keys in whole 16-byte pieces, vec: those of values and results too
 };
 
 __device__ __forceinline__ int delta_first(const DeltaSeqArgs &a, int s) { return min(max(a.off[s], 0), a.L); }
@@ -193,249 +198,393 @@ __device__ __forceinline__ int delta_first(const DeltaSeqArgs &a, int s) { retur
 // tokens of a sequence: offsets that are out of order or out of range give none or fewer
 __device__ __forceinline__ int delta_length(const DeltaSeqArgs &a, int s, int first) { return max(min(max(a.off[s + 1], 0), a.L) - first, 0); }
 
+// A block per chunk and head.  Three waves form a tile of 16 x 16 of both products each (the upper right one is zero) from rows that they load
+// as the matrix operation takes them, the fourth the sums of the decays; then (I + A)^-1 by substitution in blocks of 8, joined as
+// -T22 A21 T11 twice.  (Powers of A instead of substitution would cancel: 32 keys alike give binomials up to 3e8.)
 template <int DKT>                   // dk in units of 32, rounded up
 __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaSeqArgs a)
 {
-    constexpr int DKP = 32 * DKT, P = DKP + 4, PT = DELTA_C + 4;
-    extern __shared__ __align__(16) float s_all[];
-    float *sK = s_all, *sQ = sK + DELTA_C * P, *sA = sQ + DELTA_C * P, *sT = sA + DELTA_C * PT, *s_rk = sT + DELTA_C * PT, *s_rq = s_rk + DELTA_C, *s_b = s_rq + DELTA_C;
-    double *s_c = (double *)(s_b + DELTA_C);
+    constexpr int PT = DELTA_C + 4, PX = 20, STEPS = 2 * DKT < 8 ? 2 * DKT : 8;
+    __shared__ __align__(16) float sA[DELTA_C * PT], sT[DELTA_C * PT], sX[16 * PX], s_rk[DELTA_C], s_rq[DELTA_C], s_mk[DELTA_C], s_mq[DELTA_C], s_b[DELTA_C];
+    __shared__ double s_c[DELTA_C];
+    __shared__ int s_at[2];
     const q8_delta_inputs &p = a.in;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = lane & 15, gq = lane >> 4;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, gq = lane >> 4;
     const int head = blockIdx.x % p.hv, slot = blockIdx.x / p.hv, kh = head / (p.hv / p.hk);
-    // the last sequence whose places begin at or before this one
-    int lo = 0, hi = a.S - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (delta_first(a, mid) / DELTA_C + mid <= slot) lo = mid;
-        else hi = mid - 1;
-    }
-    const int first = delta_first(a, lo), length = delta_length(a, lo, first), t0 = (slot - (first / DELTA_C + lo)) * DELTA_C;
-    if (t0 < 0 || t0 >= length) return;                                     // (a place that no chunk has)
-    const int m = min(DELTA_C, length - t0);
-    const size_t tok = (size_t)first + t0;
-    for (int x = tid; x < DELTA_C * (DKP / 4); x += 256) {
-        const int r = x / (DKP / 4), k = 4 * (x % (DKP / 4)), left = r < m ? p.dk - k : 0;
-        *(v4f *)(sK + r * P + k) = load4(p.k + (tok + r) * p.ldk + (size_t)kh * p.dk + k, left, a.vec_qk);
-        *(v4f *)(sQ + r * P + k) = load4(p.q + (tok + r) * p.ldq + (size_t)kh * p.dk + k, left, a.vec_qk);
-    }
-    if (tid < DELTA_C) {
-        const float g = tid < m ? p.g[(tok + tid) * p.ldg + head] : 0.0f;
-        s_c[tid] = g < (float)DELTA_LEAST ? DELTA_LEAST : (double)g;
-        s_b[tid] = tid < m ? p.beta[(tok + tid) * p.ldb + head] : 0.0f;
-    }
+    if (tid == 0) s_at[1] = 0;
+    for (int x = tid; x < DELTA_C * PT; x += 256) sT[x] = 0.0f;
     __syncthreads();
-    double c = 0.0;
-    if (tid < DELTA_C)
-        for (int t = 0; t <= tid; ++t) c += s_c[t];
-    {
-        const int r = tid >> 3, e0 = tid & 7;                               // eight threads a token
-        float kk = 0.0f, qq = 0.0f;
-        for (int k = 4 * e0; k < DKP; k += 32) {
-            const v4f x = *(const v4f *)(sK + r * P + k), y = *(const v4f *)(sQ + r * P + k);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                kk = fmaf(x[e], x[e], kk);
-                qq = fmaf(y[e], y[e], qq);
-            }
-        }
-        for (int x = 1; x < 8; x *= 2) {
-            kk += __shfl_xor(kk, x);
-            qq += __shfl_xor(qq, x);
-        }
-        if (e0 == 0) {
-            s_rk[r] = p.normalize ? unit_of(kk) : 1.0f;
-            s_rq[r] = (p.normalize ? unit_of(qq) : 1.0f) * p.scale;
+    for (int s = tid; s < a.S; s += 256) {                                  // the sequence that has this place, if any
+        const int first = delta_first(a, s), t0 = (slot - (first / DELTA_C + s)) * DELTA_C, left = delta_length(a, s, first) - t0;
+        if (t0 >= 0 && left > 0) {
+            s_at[0] = first + t0;
+            s_at[1] = min(DELTA_C, left);
         }
     }
     __syncthreads();
-    if (tid < DELTA_C) s_c[tid] = c;
-    // products of 16 x 16 a wave: keys with keys and queries with keys
-    const int mt = wave & 1, nt = wave >> 1;
+    const size_t tok = (size_t)s_at[0];
+    const int m = s_at[1] > 0 ? min(s_at[1], a.L - s_at[0]) : 0;
+    if (m <= 0) return;                                                     // (a place that no chunk has)
+
+    const int mt = wave > 0, nt = wave == 1;
     v4f akk = {0.0f, 0.0f, 0.0f, 0.0f}, aqk = akk;
-    if (mt >= nt)
+    if (wave < 3) {
+        const int r = 16 * mt + i, rn = 16 * nt + i;
+        const float *k = p.k + (tok + r) * p.ldk + (size_t)kh * p.dk + 4 * gq, *q = p.q + (tok + r) * p.ldq + (size_t)kh * p.dk + 4 * gq;
+        const float *kn = p.k + (tok + rn) * p.ldk + (size_t)kh * p.dk + 4 * gq;
+        float kk = 0.0f, qq = 0.0f, mk = 0.0f, mq = 0.0f;
+        for (int t0 = 0; t0 < 2 * DKT; t0 += STEPS) {
+            v4f x[STEPS], y[STEPS], z[STEPS];
 #pragma unroll
-        for (int t = 0; t < DKP / 16; ++t) {
-            const v4f x = *(const v4f *)(sK + (16 * mt + i) * P + 16 * t + 4 * gq), y = *(const v4f *)(sQ + (16 * mt + i) * P + 16 * t + 4 * gq);
-            const v4f z = *(const v4f *)(sK + (16 * nt + i) * P + 16 * t + 4 * gq);
+            for (int t = 0; t < STEPS; ++t) {
+                const int left = p.dk - 16 * (t0 + t) - 4 * gq;
+                x[t] = load4(k + 16 * (t0 + t), r < m ? left : 0, a.vec_qk);
+                y[t] = load4(q + 16 * (t0 + t), r < m ? left : 0, a.vec_qk);
+                z[t] = load4(kn + 16 * (t0 + t), wave == 2 && rn < m ? left : 0, a.vec_qk);
+            }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                akk = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], z[e], akk, 0, 0, 0);
-                aqk = __builtin_amdgcn_mfma_f32_16x16x4f32(y[e], z[e], aqk, 0, 0, 0);
+            for (int t = 0; t < STEPS; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float other = wave == 2 ? z[t][e] : x[t][e];
+                    akk = __builtin_amdgcn_mfma_f32_16x16x4f32(x[t][e], other, akk, 0, 0, 0);
+                    aqk = __builtin_amdgcn_mfma_f32_16x16x4f32(y[t][e], other, aqk, 0, 0, 0);
+                    kk = fmaf(x[t][e], x[t][e], kk);
+                    qq = fmaf(y[t][e], y[t][e], qq);
+                    mk = fmaxf(mk, fabsf(x[t][e]));
+                    mq = fmaxf(mq, fabsf(y[t][e]));
+                }
+        }
+        if (wave < 2) {                                                     // each row once
+#pragma unroll
+            for (int x = 16; x < 64; x *= 2) {
+                kk += __shfl_xor(kk, x);
+                qq += __shfl_xor(qq, x);
+                mk = fmaxf(mk, __shfl_xor(mk, x));
+                mq = fmaxf(mq, __shfl_xor(mq, x));
+            }
+            if (gq == 0) {
+                s_rk[r] = p.normalize ? unit_of(kk) : 1.0f;
+                s_rq[r] = (p.normalize ? unit_of(qq) : 1.0f) * p.scale;
+                s_mk[r] = mk;
+                s_mq[r] = mq;
             }
         }
+    } else {
+        const int t = lane & 31;
+        const float g = t < m ? p.g[(tok + t) * p.ldg + head] : 0.0f;
+        double c = g < (float)DELTA_LEAST ? DELTA_LEAST : (double)g;
+        for (int x = 1; x < 32; x *= 2) {
+            const double d = __shfl_up(c, x, 32);
+            if (t >= x) c += d;
+        }
+        if (lane < DELTA_C) {
+            s_c[t] = c;
+            s_b[t] = t < m ? p.beta[(tok + t) * p.ldb + head] : 0.0f;
+        }
+    }
     __syncthreads();
     float *room = a.room + ((size_t)slot * p.hv + head) * DELTA_ROOM;
-    const int col = 16 * nt + i;
+    if (wave < 3) {                                                         // lane (i, gq): column i, rows 4 gq + e of a tile
+        const int col = 16 * nt + i;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const int row = 16 * mt + 4 * gq + e;
-        const float d = row >= col ? expf((float)(s_c[row] - s_c[col])) * s_rk[col] : 0.0f;
-        sA[row * PT + col] = row > col ? s_b[row] * s_rk[row] * d * akk[e] : 0.0f;
-        room[DELTA_C * DELTA_C + row * DELTA_C + col] = row >= col ? s_rq[row] * d * aqk[e] : 0.0f;
+        for (int e = 0; e < 4; ++e) {
+            const int row = 16 * mt + 4 * gq + e;
+            const float d = row >= col ? expf((float)(s_c[row] - s_c[col])) * s_rk[col] : 0.0f;
+            sA[row * PT + col] = row > col ? s_b[row] * s_rk[row] * d * akk[e] : 0.0f;
+            room[DELTA_MATRIX + row * DELTA_C + col] = row >= col ? s_rq[row] * d * aqk[e] : 0.0f;
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) room[DELTA_MATRIX + (4 * gq + e) * DELTA_C + 16 + i] = 0.0f;
+        if (lane < DELTA_C) {
+            float *v = room + 2 * DELTA_MATRIX, ik, iq;
+            const float ek = parts_scale(s_mk[lane], ik), eq = parts_scale(s_mq[lane], iq), e = expf((float)s_c[lane]);
+            v[lane] = e * s_rk[lane] * ek;
+            v[DELTA_C + lane] = e * s_rq[lane] * eq;
+            v[2 * DELTA_C + lane] = expf((float)(s_c[DELTA_C - 1] - s_c[lane])) * s_rk[lane] * ek;
+            v[3 * DELTA_C + lane] = ik;
+            v[4 * DELTA_C + lane] = iq;
+            v[5 * DELTA_C + lane] = expf((float)s_c[DELTA_C - 1]);
+        }
     }
     __syncthreads();
-    // (I + A)^-1: the two diagonal blocks of 16 by substitution, a lane per column, then -T22 A21 T11
-    if (tid < DELTA_C) {
-        const int base = tid & 16, jc = tid & 15;
-        float x[16];
+    if (tid < DELTA_C) {                                                    // the diagonal blocks of 8, a lane per column
+        const int base = tid & 24, jc = tid & 7;
+        v4f w[8][2];
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
+        for (int r = 1; r < 8; ++r) {
+            w[r][0] = *(const v4f *)(sA + (base + r) * PT + base);
+            w[r][1] = *(const v4f *)(sA + (base + r) * PT + base + 4);
+        }
+        float x[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
             float v = r == jc ? 1.0f : 0.0f;
 #pragma unroll
-            for (int l = 0; l < r; ++l) v = fmaf(-sA[(base + r) * PT + base + l], x[l], v);
+            for (int l = 0; l < r; ++l) v = fmaf(-w[r][l >> 2][l & 3], x[l], v);
             x[r] = v;
             sT[(base + r) * PT + base + jc] = v;
         }
     }
     __syncthreads();
     {
-        const int r = tid >> 4, cc = tid & 15;
+        const int b = 16 * (tid >> 6), r = (tid >> 3) & 7, c = tid & 7;     // two blocks of 16
+        float v = 0.0f;
+        if (tid < 128) {
+#pragma unroll
+            for (int l = 0; l < 8; ++l) v = fmaf(sA[(b + 8 + r) * PT + b + l], sT[(b + l) * PT + b + c], v);
+            sX[(b / 2 + r) * PX + c] = v;
+        }
+        __syncthreads();
+        if (tid < 128) {
+            v = 0.0f;
+#pragma unroll
+            for (int l = 0; l < 8; ++l) v = fmaf(sT[(b + 8 + r) * PT + b + 8 + l], sX[(b / 2 + l) * PX + c], v);
+            sT[(b + 8 + r) * PT + b + c] = -v;
+        }
+    }
+    __syncthreads();
+    {
+        const int r = tid >> 4, c = tid & 15;
         float v = 0.0f;
 #pragma unroll
-        for (int l = 0; l < 16; ++l) v = fmaf(sA[(16 + r) * PT + l], sT[l * PT + cc], v);
-        sT[r * PT + 16 + cc] = v;                                           // (the upper right block holds it for now)
+        for (int l = 0; l < 16; ++l) v = fmaf(sA[(16 + r) * PT + l], sT[l * PT + c], v);
+        sX[r * PX + c] = v;
         __syncthreads();
         v = 0.0f;
 #pragma unroll
-        for (int l = 0; l < 16; ++l) v = fmaf(sT[(16 + r) * PT + 16 + l], sT[l * PT + 16 + cc], v);
-        sT[(16 + r) * PT + cc] = -v;
+        for (int l = 0; l < 16; ++l) v = fmaf(sT[(16 + r) * PT + 16 + l], sX[l * PX + c], v);
+        sT[(16 + r) * PT + c] = -v;
     }
     __syncthreads();
-    for (int x = tid; x < DELTA_C * DELTA_C; x += 256) {
-        const int r = x / DELTA_C, cc = x % DELTA_C;
-        room[x] = r < 16 && cc >= 16 ? 0.0f : sT[r * PT + cc] * s_b[cc];
-    }
-    if (tid < DELTA_C) {
-        float *v = room + 2 * DELTA_C * DELTA_C;
-        const float e = expf((float)c);
-        v[tid] = e * s_rk[tid];
-        v[DELTA_C + tid] = e * s_rq[tid];
-        v[2 * DELTA_C + tid] = expf((float)(s_c[DELTA_C - 1] - c)) * s_rk[tid];
-        v[3 * DELTA_C + tid] = expf((float)s_c[DELTA_C - 1]);
+    {
+        const int r = tid >> 3, c = 4 * (tid & 7);
+        *(v4f *)(room + r * DELTA_C + c) = *(const v4f *)(sT + r * PT + c) * *(const v4f *)(s_b + c);
     }
 }
 
-template <int DKT>
-__global__ __launch_bounds__(256) void delta_carry_kernel(DeltaSeqArgs a)
+// Four tokens (rows of PH halfs from `at` on) of sixteen numbers, transposed: a lane's number of four tokens.
+__device__ __forceinline__ v4h read_transposed(const _Float16 *at)
 {
-    constexpr int DKP = 32 * DKT, P = DKP + 4, PT = DELTA_C + 4, PIECES = DELTA_C * (DKP / 4) / 256;
-    extern __shared__ __align__(16) float s_all[];
-    float *sK = s_all, *sQ = sK + DELTA_C * P, *sS = sQ + DELTA_C * P, *sR = sS + DELTA_C * P, *sU = sR + DELTA_C * PT;      // sS [column][row of the state], sR, sU [column][token]
+#if defined(__HIP_DEVICE_COMPILE__)
+    typedef __fp16 v4fp __attribute__((ext_vector_type(4)));
+    return __builtin_bit_cast(v4h, __builtin_amdgcn_ds_read_tr16_b64_v4f16((__attribute__((address_space(3))) v4fp *)at));
+#else
+    return v4h();
+#endif
+}
+
+__device__ __forceinline__ v8h both(v4h a, v4h b) { return (v8h){a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}; }
+
+// Four numbers at `at`, or zeros past the end.  Loads under no condition: the compiler waits for everything in flight where a load stands in a branch.
+// In single words the row's end is looked at for each (`left` numbers are the row's).
+template <bool VEC>
+__device__ __forceinline__ v4f fetch4(__amdgpu_buffer_rsrc_t rsrc, unsigned at, int left)
+{
+    v4f v;
+    if constexpr (VEC) {
+        v = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(rsrc, (int)at, 0, 0));
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = __int_as_float(__builtin_amdgcn_raw_buffer_load_b32(rsrc, (int)(left > e ? at + 4 * e : Q8_OOB), 0, 0));
+    }
+    return v;
+}
+
+// A block per sequence, head and 32 columns of the state, which stays in registers as fp32.  Its products run on the fp16 matrix cores with both sides in two
+// parts (hi hi + hi lo + lo hi, within 2^-21): rows of keys and queries with a power of two each, columns of the state and of the updates too, so
+// that what a column loses goes by its own size.  The two small products, of 32 x 32 with T and M, are fp32 ones.  Four waves multiply the
+// keys and make the updates, four multiply the queries and make the results; all convert, and all keep an eighth of the state.  The next chunk's rows are on
+// their way while one is worked on, each number in one thread's load and from there in LDS: loads of what several lanes need each cost the most here.
+template <int DKT, bool VEC>         // VEC: rows of queries, keys, values and results in whole 16-byte pieces
+__global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(DeltaSeqArgs a)
+{
+    constexpr int DKP = 32 * DKT, PH = DKP + 8, PT = DELTA_C + 4, OWN = DKT / 2;      // of a thread: pieces of four numbers of the keys, of the queries and of the state
+    static_assert(DKT % 2 == 0, "eight waves share the state's tiles");
+    extern __shared__ __align__(16) uint8_t s_all[];
+    _Float16 *sK = (_Float16 *)s_all, *sQ = sK + 2 * DELTA_C * PH, *sS = sQ + 2 * DELTA_C * PH;      // [hi, lo][token or column][row of the state]
+    float *sR = (float *)(sS + 2 * 32 * PH), *sM = sR + 32 * PT, *sV = sM + 2 * 32 * PT, *s_vec = sV + 32 * PT, *s_top = s_vec + 6 * DELTA_C, *s_wtop = s_top + 128;
+    float *sU = (float *)sS, *sW = sU + 32 * PT;                            // sR, sU, sW [column][token], sM [T, M][token][token], sV values and results [token][column]
+    static_assert(2 * 32 * PT * sizeof(float) <= 2 * 32 * PH * sizeof(_Float16), "the updates fit where the state's parts were: they have been read by then");
     const q8_delta_inputs &p = a.in;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = lane & 15, gq = lane >> 4, mt = wave & 1, nt = wave >> 1;
-    const int head = blockIdx.x % p.hv, s = blockIdx.x / p.hv, kh = head / (p.hv / p.hk), v0 = blockIdx.y * 32, col = v0 + 16 * nt + i;
-    const int first = delta_first(a, s), length = delta_length(a, s, first);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, gq = lane >> 4, mt = wave & 1, nt = (wave >> 1) & 1, queries = wave >> 2;
+    const int head = blockIdx.x % p.hv, s = blockIdx.x / p.hv, kh = head / (p.hv / p.hk), v0 = blockIdx.y * 32, lc = 16 * nt + i, col = v0 + lc;
+    const int first = __builtin_amdgcn_readfirstlane(delta_first(a, s)), length = __builtin_amdgcn_readfirstlane(delta_length(a, s, first));
     const bool live = col < p.dv;
-    // rows 16 (2 t + mt) + 4 gq + e of column `col` of the state
-    v4f st[DKT];
+    const int tile0 = 2 * queries + mt, r0 = 16 * mt + 4 * gq;
+    // rows 16 (4 t + tile0) + 4 gq + e of column `col` of the state
+    v4f st[OWN];
     const size_t at = ((size_t)s * p.hv + head) * p.dk * p.dv + col;
 #pragma unroll
-    for (int t = 0; t < DKT; ++t)
+    for (int t = 0; t < OWN; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const int row = 16 * (2 * t + mt) + 4 * gq + e;
+            const int row = 16 * (4 * t + tile0) + 4 * gq + e;
             st[t][e] = a.state && live && row < p.dk ? a.state[at + (size_t)row * p.dv] : 0.0f;
         }
-    v4f pk[PIECES], pq[PIECES], pT[2], pM[2], pv, pe, pf, pd;
-    float decay;
+    // a thread's pieces: of keys and queries, of T and M, of values and results (half of the threads), of the tokens' numbers (48 threads); offsets
+    // inside a chunk: rows past its end lie past the end of what is described
+    unsigned ok[OWN], oq[OWN];
+#pragma unroll
+    for (int x = 0; x < OWN; ++x) {
+        const int y = tid + 512 * x, r = y / (DKP / 4), k = 4 * (y % (DKP / 4));
+        ok[x] = k < p.dk ? 4u * ((unsigned)r * (unsigned)p.ldk + k) : Q8_OOB;
+        oq[x] = k < p.dk ? 4u * ((unsigned)r * (unsigned)p.ldq + k) : Q8_OOB;
+    }
+    const int vr = (tid & 255) >> 3, vc = 4 * (tid & 7), vleft = tid < 256 ? p.dv - v0 - vc : 0;
+    const unsigned ov = vleft > 0 ? 4u * ((unsigned)vr * (unsigned)p.ldv + v0 + vc) : Q8_OOB, oo = vleft > 0 ? 4u * ((unsigned)vr * (unsigned)a.ldo + v0 + vc) : Q8_OOB;
+    const unsigned oe = tid < 48 ? 4u * (2 * DELTA_MATRIX + 4 * tid) : Q8_OOB;
+    v4f pk[OWN], pq[OWN], pm, pv, pe;
     auto fetch = [&](int t0) {
         const int m = min(DELTA_C, length - t0);
         const size_t tok = (size_t)first + t0;
+        // (a chunk's rows are below 2^31 bytes: pitches are at most 2^22)
+        const __amdgpu_buffer_rsrc_t rr = q8_rsrc(a.room + ((size_t)(first / DELTA_C + s + t0 / DELTA_C) * p.hv + head) * DELTA_ROOM, 4 * DELTA_ROOM);
+        const __amdgpu_buffer_rsrc_t rk = q8_rsrc(p.k + tok * p.ldk + (size_t)kh * p.dk, 4 * ((size_t)(m - 1) * p.ldk + p.dk));
+        const __amdgpu_buffer_rsrc_t rq = q8_rsrc(p.q + tok * p.ldq + (size_t)kh * p.dk, 4 * ((size_t)(m - 1) * p.ldq + p.dk));
+        const __amdgpu_buffer_rsrc_t rv = q8_rsrc(p.v + tok * p.ldv + (size_t)head * p.dv, 4 * ((size_t)(m - 1) * p.ldv + p.dv));
+        pe = fetch4<true>(rr, oe, 4);
 #pragma unroll
-        for (int x = 0; x < PIECES; ++x) {
-            const int y = tid + 256 * x, r = y / (DKP / 4), k = 4 * (y % (DKP / 4)), left = r < m ? p.dk - k : 0;
-            pk[x] = load4(p.k + (tok + r) * p.ldk + (size_t)kh * p.dk + k, left, a.vec_qk);
-            pq[x] = load4(p.q + (tok + r) * p.ldq + (size_t)kh * p.dk + k, left, a.vec_qk);
+        for (int x = 0; x < OWN; ++x) {
+            const int left = p.dk - 4 * ((tid + 512 * x) % (DKP / 4));
+            pk[x] = fetch4<VEC>(rk, ok[x], left);
+            pq[x] = fetch4<VEC>(rq, oq[x], left);
         }
-        const float *room = a.room + ((size_t)(first / DELTA_C + s + t0 / DELTA_C) * p.hv + head) * DELTA_ROOM;
-        const float *vec = room + 2 * DELTA_C * DELTA_C;
-        const int r0 = 16 * mt + 4 * gq;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            pT[t] = *(const v4f *)(room + (16 * mt + i) * DELTA_C + 16 * t + 4 * gq);
-            pM[t] = *(const v4f *)(room + DELTA_C * DELTA_C + (16 * mt + i) * DELTA_C + 16 * t + 4 * gq);
-        }
-        pe = *(const v4f *)(vec + r0);
-        pf = *(const v4f *)(vec + DELTA_C + r0);
-        pd = *(const v4f *)(vec + 2 * DELTA_C + r0);
-        decay = vec[3 * DELTA_C];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) pv[e] = live && r0 + e < m ? p.v[(tok + r0 + e) * p.ldv + (size_t)head * p.dv + col] : 0.0f;
+        pm = fetch4<true>(rr, 16u * tid, 4);
+        pv = fetch4<VEC>(rv, ov, vleft);
     };
-    if (length > 0) fetch(0);
-    for (int t0 = 0; t0 < length; t0 += DELTA_C) {
-        const int m = min(DELTA_C, length - t0);
+    // the largest of a column's numbers that this wave has
+    auto leave_top = [&](float top, float *to) {
+        top = fmaxf(top, __int_as_float(lane_xor_i<16>(__float_as_int(top), lane)));
+        top = fmaxf(top, __int_as_float(lane_xor_i<32>(__float_as_int(top), lane)));
+        if (gq == 0) to[lc] = top;
+    };
+    auto leave_state = [&] {                                                // ... and the next chunk's numbers of the tokens
+        float top = 0.0f;
 #pragma unroll
-        for (int x = 0; x < PIECES; ++x) {
-            const int y = tid + 256 * x, r = y / (DKP / 4), k = 4 * (y % (DKP / 4));
-            *(v4f *)(sK + r * P + k) = pk[x];
-            *(v4f *)(sQ + r * P + k) = pq[x];
+        for (int t = 0; t < OWN; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(st[t][e]));
+        leave_top(top, s_top + 32 * tile0);
+        if (tid < 48) *(v4f *)(s_vec + 4 * tid) = pe;
+    };
+    auto results = [&](int t0) {                                            // of the chunk at t0, from LDS
+        const __amdgpu_buffer_rsrc_t ro = q8_rsrc(a.out + ((size_t)first + t0) * a.ldo + (size_t)head * p.dv, 4 * ((size_t)(min(DELTA_C, length - t0) - 1) * a.ldo + p.dv));
+        const v4f o = *(const v4f *)(sV + vr * PT + vc);
+        if constexpr (VEC) {
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, o), ro, (int)oo, 0, 0);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) __builtin_amdgcn_raw_buffer_store_b32(__float_as_int(o[e]), ro, (int)(vleft > e ? oo + 4 * e : Q8_OOB), 0, 0);
+        }
+    };
+    if (length > 0) {
+        fetch(0);
+        leave_state();
+        __syncthreads();
+    }
+    for (int t0 = 0; t0 < length; t0 += DELTA_C) {
+        float inv;
+        const float cs = parts_scale(fmaxf(fmaxf(s_top[lc], s_top[32 + lc]), fmaxf(s_top[64 + lc], s_top[96 + lc])), inv);
+#pragma unroll
+        for (int t = 0; t < OWN; ++t) {
+            uint2 hi, lo;
+            parts4(st[t][0], st[t][1], st[t][2], st[t][3], inv, hi, lo);
+            _Float16 *to = sS + lc * PH + 16 * (4 * t + tile0) + 4 * gq;
+            *(uint2 *)to = hi;
+            *(uint2 *)(to + 32 * PH) = lo;
         }
 #pragma unroll
-        for (int t = 0; t < DKT; ++t) *(v4f *)(sS + (16 * nt + i) * P + 16 * (2 * t + mt) + 4 * gq) = st[t];
-        const v4f T[2] = {pT[0], pT[1]}, M[2] = {pM[0], pM[1]}, v = pv, ek = pe, eq = pf, el = pd;
-        const float keep = decay;
+        for (int x = 0; x < OWN; ++x) {
+            const int y = tid + 512 * x, r = y / (DKP / 4), to = r * PH + 4 * (y % (DKP / 4));
+            uint2 hi, lo;
+            parts4(pk[x][0], pk[x][1], pk[x][2], pk[x][3], s_vec[3 * DELTA_C + r], hi, lo);
+            *(uint2 *)(sK + to) = hi;
+            *(uint2 *)(sK + DELTA_C * PH + to) = lo;
+            parts4(pq[x][0], pq[x][1], pq[x][2], pq[x][3], s_vec[4 * DELTA_C + r], hi, lo);
+            *(uint2 *)(sQ + to) = hi;
+            *(uint2 *)(sQ + DELTA_C * PH + to) = lo;
+        }
+        *(v4f *)(sM + (tid >> 3) * PT + 4 * (tid & 7)) = pm;
+        if (t0 > 0 && tid < 256) results(t0 - DELTA_C);                     // (a thread's piece of the results, then of the values, in one place)
+        if (tid < 256) *(v4f *)(sV + vr * PT + vc) = pv;
         __syncthreads();
         if (t0 + DELTA_C < length) fetch(t0 + DELTA_C);
-        v4f ks = {0.0f, 0.0f, 0.0f, 0.0f}, qs = ks;
+        const v4f eb = *(const v4f *)(s_vec + queries * DELTA_C + r0), el = *(const v4f *)(s_vec + 2 * DELTA_C + r0);
+        const float keep = s_vec[5 * DELTA_C];
+        v4f x0 = {0.0f, 0.0f, 0.0f, 0.0f}, x1 = x0, x2 = x0;                // keys or queries times the state
+        const _Float16 *rows = (queries ? sQ : sK) + (16 * mt + i) * PH + 8 * gq, *columns = sS + lc * PH + 8 * gq;
 #pragma unroll
-        for (int t = 0; t < DKP / 16; ++t) {
-            const v4f x = *(const v4f *)(sK + (16 * mt + i) * P + 16 * t + 4 * gq), y = *(const v4f *)(sQ + (16 * mt + i) * P + 16 * t + 4 * gq);
-            const v4f z = *(const v4f *)(sS + (16 * nt + i) * P + 16 * t + 4 * gq);
+        for (int t = 0; t < DKT; ++t) {
+            const v8h xh = *(const v8h *)(rows + 32 * t), xl = *(const v8h *)(rows + DELTA_C * PH + 32 * t);
+            const v8h sh = *(const v8h *)(columns + 32 * t), sl = *(const v8h *)(columns + 32 * PH + 32 * t);
+            x0 = __builtin_amdgcn_mfma_f32_16x16x32_f16(xh, sh, x0, 0, 0, 0);
+            x1 = __builtin_amdgcn_mfma_f32_16x16x32_f16(xh, sl, x1, 0, 0, 0);
+            x2 = __builtin_amdgcn_mfma_f32_16x16x32_f16(xl, sh, x2, 0, 0, 0);
+        }
+        const v4f xs = eb * ((x0 + (x1 + x2)) * cs);
+        // lane (i, gq): column i, tokens r0 + (0 .. 3)
+        if (!queries) {
+            v4f v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = sV[(r0 + e) * PT + lc];
+            *(v4f *)(sR + lc * PT + r0) = v - xs;
+        }
+        __syncthreads();
+        auto small = [&](const float *from, v4f o) {                        // T or M times a column, in two chains
+            const float *m = sM + (32 * queries + 16 * mt + i) * PT + 4 * gq;
+            const v4f m0 = *(const v4f *)m, m1 = *(const v4f *)(m + 16), y = *(const v4f *)(from + lc * PT + 4 * gq), z = *(const v4f *)(from + lc * PT + 16 + 4 * gq);
+            v4f o2 = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                ks = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], z[e], ks, 0, 0, 0);
-                qs = __builtin_amdgcn_mfma_f32_16x16x4f32(y[e], z[e], qs, 0, 0, 0);
+                o = __builtin_amdgcn_mfma_f32_16x16x4f32(m0[e], y[e], o, 0, 0, 0);
+                o2 = __builtin_amdgcn_mfma_f32_16x16x4f32(m1[e], z[e], o2, 0, 0, 0);
             }
-        }
-        // lane (i, gq): column i, tokens 16 mt + 4 gq + e
-        *(v4f *)(sR + (16 * nt + i) * PT + 16 * mt + 4 * gq) = v - ek * ks;
-        __syncthreads();
-        v4f u = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const v4f z = *(const v4f *)(sR + (16 * nt + i) * PT + 16 * t + 4 * gq);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) u = __builtin_amdgcn_mfma_f32_16x16x4f32(T[t][e], z[e], u, 0, 0, 0);
-        }
-        // the state takes the updates times exp(c_C - c_j) / |k_j|, the results those themselves
-        *(v4f *)(sU + (16 * nt + i) * PT + 16 * mt + 4 * gq) = u;
-        __syncthreads();
-        v4f *dst = (v4f *)(sR + (16 * nt + i) * PT + 16 * mt + 4 * gq);
-        *dst = u * el;                                                      // (its readers are past the barrier)
-        v4f o = eq * qs;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const v4f z = *(const v4f *)(sU + (16 * nt + i) * PT + 16 * t + 4 * gq);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o = __builtin_amdgcn_mfma_f32_16x16x4f32(M[t][e], z[e], o, 0, 0, 0);
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int r = 16 * mt + 4 * gq + e;
-            if (live && r < m) a.out[((size_t)first + t0 + r) * a.ldo + (size_t)head * p.dv + col] = o[e];
+            return o + o2;
+        };
+        if (!queries) {
+            const v4f u = small(sR, (v4f){0.0f, 0.0f, 0.0f, 0.0f});
+            // the results take the updates, the state takes them times exp(c_C - c_j) / |k_j|
+            const v4f w = u * el;
+            *(v4f *)(sU + lc * PT + r0) = u;
+            *(v4f *)(sW + lc * PT + r0) = w;
+            leave_top(fmaxf(fmaxf(fabsf(w[0]), fabsf(w[1])), fmaxf(fabsf(w[2]), fabsf(w[3]))), s_wtop + 32 * mt);
         }
         __syncthreads();
+        // tokens 8 gq + (0 .. 7) of column i
+        const float cw = parts_scale(fmaxf(s_wtop[lc], s_wtop[32 + lc]), inv);
+        const v4f z0 = *(const v4f *)(sW + lc * PT + 8 * gq), z1 = *(const v4f *)(sW + lc * PT + 8 * gq + 4);
+        union { uint2 u[2]; v8h h; } wh, wl;
+        parts4(z0[0], z0[1], z0[2], z0[3], inv, wh.u[0], wl.u[0]);
+        parts4(z1[0], z1[1], z1[2], z1[3], inv, wh.u[1], wl.u[1]);
 #pragma unroll
-        for (int t = 0; t < DKT; ++t) st[t] *= keep;
+        for (int t = 0; t < OWN; ++t) {
+            const _Float16 *k = sK + (8 * gq + (i >> 2)) * PH + 16 * (4 * t + tile0) + 4 * (i & 3);
+            const v8h kh_ = both(read_transposed(k), read_transposed(k + 4 * PH));
+            const v8h kl = both(read_transposed(k + DELTA_C * PH), read_transposed(k + (DELTA_C + 4) * PH));
+            v4f d = {0.0f, 0.0f, 0.0f, 0.0f};
+            d = __builtin_amdgcn_mfma_f32_16x16x32_f16(kl, wh.h, d, 0, 0, 0);
+            d = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh_, wl.h, d, 0, 0, 0);
+            d = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh_, wh.h, d, 0, 0, 0);
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const v4f z = *(const v4f *)(sR + (16 * nt + i) * PT + 16 * t + 4 * gq);
+            for (int e = 0; e < 4; ++e) st[t][e] = fmaf(cw, d[e], keep * st[t][e]);
+        }
+        leave_state();
+        if (queries) {
+            const v4f o = small(sU, xs);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-#pragma unroll
-                for (int x = 0; x < DKT; ++x)
-                    st[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(sK[(16 * t + 4 * gq + e) * P + 16 * (2 * x + mt) + i], z[e], st[x], 0, 0, 0);
+            for (int e = 0; e < 4; ++e) sV[(r0 + e) * PT + lc] = o[e];
         }
         __syncthreads();
     }
+    if (length > 0 && tid < 256) results((length - 1) / DELTA_C * DELTA_C);
     if (a.state_out && live)
 #pragma unroll
-        for (int t = 0; t < DKT; ++t)
+        for (int t = 0; t < OWN; ++t)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int row = 16 * (2 * t + mt) + 4 * gq + e;
+                const int row = 16 * (4 * t + tile0) + 4 * gq + e;
                 if (row < p.dk) a.state_out[at + (size_t)row * p.dv] = st[t][e];
             }
 }
@@ -443,17 +592,16 @@ __global__ __launch_bounds__(256) void delta_carry_kernel(DeltaSeqArgs a)
 template <int DKT> static q8_status launch_sequence(q8_ctx *ctx, const DeltaSeqArgs &a)
 {
     static Q8OncePerDevice once[2];
-    constexpr size_t row = (32 * DKT + 4) * sizeof(float), small = DELTA_C * (DELTA_C + 4) * sizeof(float);
-    const size_t s1 = 2 * DELTA_C * row + 2 * small + 5 * DELTA_C * sizeof(float), s2 = 3 * DELTA_C * row + 2 * small;
-    q8_status st = q8i_lds(ctx, once[0], (const void *)delta_chunk_kernel<DKT>, s1, "delta sequence");
-    if (!st) st = q8i_lds(ctx, once[1], (const void *)delta_carry_kernel<DKT>, s2, "delta sequence");
+    constexpr size_t smem = 3 * 2 * 32 * (32 * DKT + 8) * sizeof(_Float16) + (4 * 32 * (DELTA_C + 4) + 6 * DELTA_C + 192) * sizeof(float);
+    void (*const carry)(DeltaSeqArgs) = a.vec ? delta_carry_kernel<DKT, true> : delta_carry_kernel<DKT, false>;
+    q8_status st = q8i_lds(ctx, once[a.vec], (const void *)carry, smem, "delta sequence");
     if (st) return st;
     if (a.L > 0) {
-        hipLaunchKernelGGL(delta_chunk_kernel<DKT>, dim3((unsigned)((size_t)a.slots * a.in.hv)), dim3(256), s1, ctx->stream, a);
+        hipLaunchKernelGGL(delta_chunk_kernel<DKT>, dim3((unsigned)((size_t)a.slots * a.in.hv)), dim3(256), 0, ctx->stream, a);
         st = q8i_launch_check(ctx, "delta sequence");
         if (st) return st;
     }
-    hipLaunchKernelGGL(delta_carry_kernel<DKT>, dim3((unsigned)((size_t)a.S * a.in.hv), (a.in.dv + 31) / 32), dim3(256), s2, ctx->stream, a);
+    hipLaunchKernelGGL(carry, dim3((unsigned)((size_t)a.S * a.in.hv), (a.in.dv + 31) / 32), dim3(512), smem, ctx->stream, a);
     return q8i_launch_check(ctx, "delta sequence");
 }
 
@@ -463,7 +611,8 @@ q8_status q8i_delta_sequence(q8_ctx *ctx, const q8_delta_inputs *in, int L, cons
 {
     DeltaSeqArgs a = {*in, off, S, L, L / DELTA_C + S, room, state, state_out, out, ldo, 0, 0};
     a.vec_qk = in->dk % 4 == 0 && whole16(in->q, in->ldq) && whole16(in->k, in->ldk);
-    if (in->dk <= 32) return launch_sequence<1>(ctx, a);
+    a.vec = a.vec_qk && in->dv % 4 == 0 && whole16(in->v, in->ldv) && whole16(out, ldo);
+    if (L <= 1) a.in.ldq = a.in.ldk = in->hk * in->dk, a.in.ldv = a.ldo = in->hv * in->dv;      // (a pitch that nothing uses, but bounds are formed with)
     if (in->dk <= 64) return launch_sequence<2>(ctx, a);
     if (in->dk <= 128) return launch_sequence<4>(ctx, a);
     return launch_sequence<8>(ctx, a);

@@ -1,13 +1,13 @@
 // q8_w4.hip -- 4-bit weights with a scale and a zero point per group of 32, 64 or 128 columns of a row: quantization, and the
 // product with fp32 vectors, Y[j][i] = sum_g s[i,g] sum_{k in g} (c[i,k] - z[i,g]) X[j][k] + bias[i].
 #include "q8_internal.h"
+#include "q8_parts.h"
 
 #include <math.h>
 
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef _Float16 v2h __attribute__((ext_vector_type(2)));
-typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 
 #define W4_BLOCK 128                 // columns of a block: 64 bytes of codes, one, two or four groups
 #define W4_SPLIT 512                 // bytes of a block of a vector in its two fp16 parts
@@ -113,31 +113,6 @@ q8_status q8i_quantize_w4(q8_ctx *ctx, const float *X, int rows, int cols, int l
 // in fp32, and what is lost is below what sums in fp32 lose.  A group's sum is formed in whole numbers and fractions of X alone and
 // multiplied by its scale once.
 
-// The power of two for values up to m: 2^-e m in [2^13, 2^14), as (inv = 2^-e, returned 2^e); m < 2^-100 counts as zeros.
-__device__ __forceinline__ float w4_scale_of(float m, float &inv)
-{
-    if (m < 0x1p-100f) { inv = 0.0f; return 1.0f; }
-    const unsigned e = (__float_as_uint(m) >> 23) - 13u;                    // 14 .. 241
-    inv = __uint_as_float((254u - e) << 23);
-    return __uint_as_float(e << 23);
-}
-
-__device__ __forceinline__ float w4_finite_abs(float v) { return fabsf(v) < INFINITY ? fabsf(v) : 0.0f; }
-
-// Four values times inv as hi and lo parts.
-__device__ __forceinline__ void w4_parts(const float4 v, float inv, uint2 &hi, uint2 &lo)
-{
-    const float x[4] = {v.x * inv, v.y * inv, v.z * inv, v.w * inv};
-    union { _Float16 h[4]; uint2 u; } a, b;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        a.h[e] = (_Float16)x[e];
-        b.h[e] = (_Float16)(x[e] - (float)a.h[e]);
-    }
-    hi = a.u;
-    lo = b.u;
-}
-
 // Eight weights c - z from a word of codes.  A code in the fraction of 1024.0 is 1024 + c, one four bits higher 1024 + 16 c.
 // z1 = -(1024 + z), z2 = -(64 + z), twice each.
 __device__ __forceinline__ v8h w4_expand(unsigned c, v2h z1, v2h z2)
@@ -228,11 +203,11 @@ __global__ __launch_bounds__(512) void w4_stream_kernel(W4GemmArgs a)
             if (k + 1 < a.cols) v.y = x[1];
             if (k + 2 < a.cols) v.z = x[2];
         }
-        const float top = w4_group_max<32>(fmaxf(fmaxf(w4_finite_abs(v.x), w4_finite_abs(v.y)), fmaxf(w4_finite_abs(v.z), w4_finite_abs(v.w))));
+        const float top = w4_group_max<32>(fmaxf(fmaxf(finite_abs(v.x), finite_abs(v.y)), fmaxf(finite_abs(v.z), finite_abs(v.w))));
         float inv;
-        const float sx = w4_scale_of(top, inv);
+        const float sx = parts_scale(top, inv);
         uint2 hi, lo;
-        w4_parts(v, inv, hi, lo);
+        parts4(v.x, v.y, v.z, v.w, inv, hi, lo);
         uint8_t *at = s_x + (size_t)j * a.pitch + blk * W4_SPLIT + 8 * q;
         *(uint2 *)at = hi;
         *(uint2 *)(at + W4_SPLIT / 2) = lo;
@@ -353,21 +328,21 @@ __global__ __launch_bounds__(256) void w4_parts_kernel(const float *X, int cols,
         const float4 v = load(t * 1024 + 4 * tid);
         if (t == 0) keep[0] = v;
         if (t == 1) keep[1] = v;
-        m = fmaxf(m, fmaxf(fmaxf(w4_finite_abs(v.x), w4_finite_abs(v.y)), fmaxf(w4_finite_abs(v.z), w4_finite_abs(v.w))));
+        m = fmaxf(m, fmaxf(fmaxf(finite_abs(v.x), finite_abs(v.y)), fmaxf(finite_abs(v.z), finite_abs(v.w))));
     }
     m = wave_max_f(m);
     if ((tid & 63) == 0) s_max[tid >> 6] = m;
     __syncthreads();
     m = fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3]));
     float inv;
-    const float s = w4_scale_of(m, inv);
+    const float s = parts_scale(m, inv);
     if (tid == 0) sx[j] = s;
     for (int t = 0; t * 1024 < nb * W4_BLOCK; ++t) {
         const int k = t * 1024 + 4 * tid;
         if (k >= nb * W4_BLOCK) break;
         const float4 v = t == 0 ? keep[0] : t == 1 ? keep[1] : load(k);
         uint2 hi, lo;
-        w4_parts(v, inv, hi, lo);
+        parts4(v.x, v.y, v.z, v.w, inv, hi, lo);
         uint8_t *at = parts + ((size_t)j * nb + (k >> 7)) * W4_SPLIT + 2 * (k & 127);
         *(uint2 *)at = hi;
         *(uint2 *)(at + W4_SPLIT / 2) = lo;

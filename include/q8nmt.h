@@ -660,7 +660,7 @@ q8_status q8_quantize_matrix_w4(q8_ctx *ctx, const float *X, int rows, int cols,
 /* Y[j][i] = sum_k W[i][k] X[j][k] + bias[i] (bias may be NULL) for n fp32 vectors X [n x ldx] (16-byte aligned, ldx % 4 == 0), Y [n x ldy] fp32,
  * elements past a vector's W->rows untouched.  X is not quantized: its values are held within 2^-22 of themselves (or 2^-38 of the
  * vector's largest; blocks of 128, or vectors, of magnitudes below 2^-100 count as zeros), products and sums in fp32.  A value that is not
- * finite stays with its vector.  Y may overlap X.  1 <= n <= 2^20, as far as a launch holds the results.  Workspace: the context's must have
+ * finite stays with its vector.  Y may overlap X.  1 <= n <= 2^20, as far as a launch holds the results; ldy <= 2^25 for n > 1.  Workspace: the context's must have
  * q8_gemm_w4_bytes(n, W->cols) bytes. */
 size_t q8_gemm_w4_bytes(int n, int cols);
 q8_status q8_gemm_w4(q8_ctx *ctx, const q8_mat_w4 *W, const float *X, int n, int ldx, const float *bias, float *Y, int ldy);

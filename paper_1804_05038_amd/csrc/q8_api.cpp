@@ -161,7 +161,7 @@ size_t q8_workspace_bytes(int max_n, int max_l, int max_rows, int max_ld)
     b += tiles + 65536;
     // calls that lay their room out otherwise: less than the above, unless the matrices have few rows
     const size_t layer = Q8_WS_HEADER + 5 * up256((size_t)max_n * max_rows * 4) + 4 * up256((size_t)max_n * ((max_ld + 15) & ~15)) +
-                         3 * up256((size_t)max_n * 4) + up256((size_t)max_n * (max_ld / 128 + 4)) + up256(q8i_gemm_w4_parts(max_n, max_ld)) + tiles;
+                         3 * up256((size_t)max_n * 4) + up256((size_t)max_n * (max_ld / 128 + 4)) + up256(q8i_gemm_w4_parts(max_n, max_ld)) + up256(q8i_gemm_w4_scales(max_n) * 4) + tiles;
     return std::max({b, layer, q8_gemm_f8_bytes(max_n, max_ld), q8_gemm_w4_bytes(max_n, max_ld), q8_sample_bytes(max_n, max_rows)});
 }
 
@@ -1893,7 +1893,7 @@ q8_status output_logits_blocks(q8_ctx *ctx, const q8_readout_weights *ro, const 
     }
     // the hidden vectors as the product takes them: codes and scales, or parts and scales
     q8_mat_f8 tq = {nullptr, nullptr, n, R, f8_pitch(R), f8_scale_pitch(R)};
-    uint8_t *codes = cv.take<uint8_t>(W4 ? q8i_gemm_w4_parts(n, R) : (size_t)n * tq.ld), *scale = cv.take<uint8_t>(W4 ? (size_t)n * 4 : (size_t)n * tq.lds);
+    uint8_t *codes = cv.take<uint8_t>(W4 ? q8i_gemm_w4_parts(n, R) : (size_t)n * tq.ld), *scale = cv.take<uint8_t>(W4 ? q8i_gemm_w4_scales(n) * 4 : (size_t)n * tq.lds);
     const size_t tiles = k > 0 ? (size_t)q8i_out_tiles(V) * n : 0;
     float *pm = k > 0 ? cv.take<float>(tiles) : nullptr;
     double *ps = k > 0 ? cv.take<double>(tiles) : nullptr;
@@ -1953,6 +1953,8 @@ q8_status q8_sample_logits(q8_ctx *ctx, const float *logits, int n, int V, int l
 // ------------------------------------------------------------------------------- 4-bit weights ----
 
 namespace {
+const int kW4MaxPitch = 1 << 25;
+
 q8_status check_mat_w4(q8_ctx *ctx, const q8_mat_w4 *W, const char *name)
 {
     if (!W || !W->data || !W->scale) return q8_fail(ctx, Q8_ERR_NULL, "%s: NULL matrix", name);
@@ -1980,7 +1982,7 @@ q8_status q8_quantize_matrix_w4(q8_ctx *ctx, const float *X, int rows, int cols,
 size_t q8_gemm_w4_bytes(int n, int cols)
 {
     if (n <= 0 || n > kF8MaxN || cols <= 0 || cols > kMaxLd) return Q8_WS_HEADER;
-    return Q8_WS_HEADER + up256(q8i_gemm_w4_parts(n, cols)) + up256((size_t)n * 4);
+    return Q8_WS_HEADER + up256(q8i_gemm_w4_parts(n, cols)) + up256(q8i_gemm_w4_scales(n) * 4);
 }
 
 q8_status q8_gemm_w4(q8_ctx *ctx, const q8_mat_w4 *W, const float *X, int n, int ldx, const float *bias, float *Y, int ldy)
@@ -1990,9 +1992,10 @@ q8_status q8_gemm_w4(q8_ctx *ctx, const q8_mat_w4 *W, const float *X, int n, int
     if (n <= 0 || n > kF8MaxN) return q8_fail(ctx, Q8_ERR_SHAPE, "n = %d outside [1, %d]", n, kF8MaxN);
     TRY(check_vecs(ctx, X, n == 1 ? W->cols + ((4 - W->cols % 4) % 4) : ldx, W->cols, "X"));
     TRY(check_result_f8(ctx, bias, Y, n, W->rows, ldy));
+    if (n > 1 && ldy > kW4MaxPitch) return q8_fail(ctx, Q8_ERR_SHAPE, "ldy %d above %d", ldy, kW4MaxPitch);
     Carver cv(ctx);
     uint8_t *parts = cv.take<uint8_t>(q8i_gemm_w4_parts(n, W->cols));
-    float *sx = cv.take<float>(n);
+    float *sx = cv.take<float>(q8i_gemm_w4_scales(n));
     if (!cv.ok) return q8_fail(ctx, Q8_ERR_WORKSPACE, "q8_gemm_w4: workspace too small");
     return q8i_gemm_w4(ctx, W, X, n, ldx, bias, Y, ldy, parts, sx);
 }

@@ -347,9 +347,10 @@ q8_status q8i_select_logits(q8_ctx *ctx, const float *part_max, const double *pa
 q8_status q8i_quantize_f8(q8_ctx *ctx, const float *X, int rows, int cols, int ldx, uint8_t *codes, int ld, uint8_t *scale, int lds);
 // X in codes, or Xf in fp32 with X the room for its codes
 q8_status q8i_gemm_f8(q8_ctx *ctx, const q8_mat_f8 *W, const q8_mat_f8 *X, const float *Xf, int ldxf, const float *bias, float *Y, int ldy);
-// 4-bit weights: parts (q8i_gemm_w4_parts bytes) and sx [n] are room for the vectors
+// 4-bit weights: parts (q8i_gemm_w4_parts bytes) and sx (q8i_gemm_w4_scales floats) are room for the vectors
 q8_status q8i_quantize_w4(q8_ctx *ctx, const float *X, int rows, int cols, int ldx, const q8_mat_w4 *out);
 size_t q8i_gemm_w4_parts(int n, int cols);
+size_t q8i_gemm_w4_scales(int n);
 q8_status q8i_gemm_w4(q8_ctx *ctx, const q8_mat_w4 *W, const float *X, int n, int ldx, const float *bias, float *Y, int ldy, uint8_t *parts, float *sx);
 // the gated delta rule; room: q8i_delta_room bytes
 q8_status q8i_delta_step(q8_ctx *ctx, const q8_delta_inputs *in, int n, const float *state, int slots, const int *parent, float *state_out, float *out, int ldo);

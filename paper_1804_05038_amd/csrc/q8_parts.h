@@ -15,8 +15,6 @@ __device__ __forceinline__ float parts_scale(float m, float &inv)
     return __uint_as_float(e << 23);
 }
 
-__device__ __forceinline__ float finite_abs(float v) { return fabsf(v) < INFINITY ? fabsf(v) : 0.0f; }
-
 // Four values times inv as hi and lo parts (two conversions an instruction, the rest in one that takes an fp16 number as it is).
 __device__ __forceinline__ void parts4(float x, float y, float z, float w, float inv, uint2 &hi, uint2 &lo)
 {

@@ -4,6 +4,7 @@
 #include "q8_parts.h"
 
 #include <math.h>
+#include <type_traits>
 
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v16f __attribute__((ext_vector_type(16)));
@@ -114,16 +115,24 @@ q8_status q8i_quantize_w4(q8_ctx *ctx, const float *X, int rows, int cols, int l
 // multiplied by its scale once.
 
 // Eight weights c - z from a word of codes.  A code in the fraction of 1024.0 is 1024 + c, one four bits higher 1024 + 16 c.
-// z1 = -(1024 + z), z2 = -(64 + z), twice each.
-__device__ __forceinline__ v8h w4_expand(unsigned c, v2h z1, v2h z2)
+// z1 = -(1024 + z), z2 = -(64 + z), twice each; magic = 1024.0 twice, in a register of the lanes: and-or takes one number of
+// the wave's registers, which the mask is, and none of its own code.
+__device__ __forceinline__ v8h w4_expand(unsigned c, v2h z1, v2h z2, unsigned magic)
 {
     const v2h sixteenth = {(_Float16)0.0625f, (_Float16)0.0625f};
     const unsigned d = c >> 8;
-    const v2h a = __builtin_bit_cast(v2h, (c & 0x000f000fu) | 0x64006400u) + z1;
-    const v2h b = __builtin_elementwise_fma(__builtin_bit_cast(v2h, (c & 0x00f000f0u) | 0x64006400u), sixteenth, z2);
-    const v2h e = __builtin_bit_cast(v2h, (d & 0x000f000fu) | 0x64006400u) + z1;
-    const v2h f = __builtin_elementwise_fma(__builtin_bit_cast(v2h, (d & 0x00f000f0u) | 0x64006400u), sixteenth, z2);
+    const v2h a = __builtin_bit_cast(v2h, (c & 0x000f000fu) | magic) + z1;
+    const v2h b = __builtin_elementwise_fma(__builtin_bit_cast(v2h, (c & 0x00f000f0u) | magic), sixteenth, z2);
+    const v2h e = __builtin_bit_cast(v2h, (d & 0x000f000fu) | magic) + z1;
+    const v2h f = __builtin_elementwise_fma(__builtin_bit_cast(v2h, (d & 0x00f000f0u) | magic), sixteenth, z2);
     return (v8h){a[0], a[1], b[0], b[1], e[0], e[1], f[0], f[1]};
+}
+
+__device__ __forceinline__ unsigned w4_magic()
+{
+    unsigned m = 0x64006400u;
+    asm("" : "+v"(m));
+    return m;
 }
 
 __device__ __forceinline__ void w4_zeros(unsigned word, v2h &z1, v2h &z2)
@@ -142,22 +151,21 @@ struct W4GemmArgs {
     const float *bias;
     float *Y;
     int rows, n, cols, ldw, lds, ng, ldx, ldy, nb;
-    int vec;                         // the vectors begin at 16-byte boundaries
     int pitch, split, span;          // few vectors: bytes of a vector in LDS; waves for a row's columns, blocks of columns of each
     int row_tiles, col_tiles;
 };
 
 // ------------------------------------------------------------------------- few vectors ----
 
-#define W4_STREAM_BLOCKS 128         // blocks of all vectors together, at most: their parts, pitches, scales and the waves' sums fit
-#define W4_STREAM_LDS (W4_STREAM_BLOCKS * W4_SPLIT + 16 * 16 + 64 * W4_STREAM_BLOCKS + 1024 * 8)
+#define W4_STREAM_BLOCKS 160         // blocks of all vectors together, at most: their parts, pitches, scales (a vector has at least a block) and the waves' sums fit
+#define W4_STREAM_LDS (W4_STREAM_BLOCKS * W4_SPLIT + 16 * 16 + 64 * W4_STREAM_BLOCKS + 1024 * 16)
 
-// Up to 16 vectors: the codes go from memory to registers once; the vectors lie in LDS in parts, put there by every block for
+// Up to 16 vectors (at 16-byte boundaries): the codes go from memory to registers once; the vectors lie in LDS in parts, put there by every block for
 // itself.  A wave multiplies 16 rows at a time, four blocks of columns a turn; `split` waves share the rows, each with its range of
 // the columns.  Lane (i, g) has row i and of every block the 16-byte piece g, whose word t belongs to columns 32 t + 8 g + (0 .. 7):
 // a matrix operation takes 32 columns in a row, so that groups of 32 have their sums too.
 template <int PER>                   // groups of a block
-__global__ __launch_bounds__(512) void w4_stream_kernel(W4GemmArgs a)
+__global__ __launch_bounds__(1024) void w4_stream_kernel(W4GemmArgs a)
 {
     extern __shared__ __align__(16) uint8_t s_x[];                          // [n][pitch], scales [nb][16], the waves' sums [waves][64]
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6, i = lane & 15, g = lane >> 4;
@@ -173,7 +181,7 @@ __global__ __launch_bounds__(512) void w4_stream_kernel(W4GemmArgs a)
         rs = q8_rsrc(a.sw + (size_t)r0 * a.lds, (size_t)left * a.lds * 4);
         row_at = i < left ? (unsigned)i * (unsigned)a.ldw + 16 * g : Q8_OOB;
         scale_at = i < left ? (unsigned)i * (unsigned)a.lds * 4 : Q8_OOB;
-        bias = a.bias && i < left ? a.bias[r0 + i] : 0.0f;
+        bias = a.bias && left > 0 ? a.bias[min(r0 + i, a.rows - 1)] : -0.0f;     // (y + -0 is y)
     };
     v4u w[4], sc[PER];
     auto codes = [&](int s) {
@@ -182,42 +190,63 @@ __global__ __launch_bounds__(512) void w4_stream_kernel(W4GemmArgs a)
     auto scales = [&](int p) {                                              // words 4 p .. 4 p + 3 of the turn's
         return __builtin_bit_cast(v4u, __builtin_amdgcn_raw_buffer_load_b128(rs, (int)(b * PER + 4 * p < a.lds && scale_at != Q8_OOB ? scale_at + 4 * (b * PER + 4 * p) : Q8_OOB), 0, 0));
     };
+    // ---- the vectors, a half wave per block of columns, four values a lane; the first ones are asked for before the codes, which come from farther
+    // away: loads come back in order
+    float *s_scale = (float *)(s_x + (size_t)n * a.pitch);
+    const int q = lane & 31, units = n * a.nb, halves = 2 * waves;
+    const __amdgpu_buffer_rsrc_t rx = q8_rsrc(a.X, 4 * ((size_t)(n - 1) * a.ldx + a.cols));
+    auto load = [&](int u) {
+        const int j = u / a.nb, k = (u - j * a.nb) * W4_BLOCK + 4 * q;
+        const unsigned off = 4u * ((unsigned)j * (unsigned)a.ldx + k);
+        v4u v = __builtin_bit_cast(v4u, __builtin_amdgcn_raw_buffer_load_b128(rx, (int)(u < units && k + 3 < a.cols ? off : Q8_OOB), 0, 0));
+        if (a.cols & 3) {                                                   // the row's last piece
+#pragma unroll
+            for (int e = 0; e < 3; ++e) v[e] |= __builtin_amdgcn_raw_buffer_load_b32(rx, (int)(u < units && k + 3 >= a.cols && k + e < a.cols ? off + 4 * e : Q8_OOB), 0, 0);
+        }
+        return __builtin_bit_cast(v4f, v);
+    };
+    auto put = [&](int u, v4f v) {
+        if (u >= units) return;                                             // (a half wave as one)
+        const int j = u / a.nb, blk = u - j * a.nb;
+        const float top = w4_group_max<32>(fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3]))));
+        float inv;
+        const float sx = parts_scale(top, inv);
+        uint2 hi, lo;
+        parts4(v[0], v[1], v[2], v[3], inv, hi, lo);
+        uint8_t *at = s_x + (size_t)j * a.pitch + blk * W4_SPLIT + 8 * q;
+        *(uint2 *)at = hi;
+        *(uint2 *)(at + W4_SPLIT / 2) = lo;
+        if (q == 0) s_scale[blk * 16 + j] = sx;
+    };
+    constexpr int AHEAD = 3;
+    const int u0 = tid >> 5;
+    v4f xv[AHEAD];
+#pragma unroll
+    for (int t = 0; t < AHEAD; ++t) xv[t] = load(u0 + t * halves);
+    __builtin_amdgcn_s_barrier();                                           // (of all waves: a compute unit's loads come back in order too)
     rows_of(tile);
 #pragma unroll
     for (int s = 0; s < 4; ++s) w[s] = codes(s);
 #pragma unroll
     for (int p = 0; p < PER; ++p) sc[p] = scales(p);
-
-    // ---- the vectors, a half wave per block of columns, four values a lane
-    float *s_scale = (float *)(s_x + (size_t)n * a.pitch);
-    const int q = lane & 31, units = n * a.nb, halves = 2 * waves;
-    for (int u = tid >> 5; u < units; u += halves) {
-        const int j = u / a.nb, blk = u - j * a.nb, k = blk * W4_BLOCK + 4 * q;
-        const float *x = a.X + (size_t)j * a.ldx + k;
-        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (k + 3 < a.cols) {
-            if (a.vec) v = *(const float4 *)x;
-            else v = make_float4(x[0], x[1], x[2], x[3]);
-        } else {
-            if (k < a.cols) v.x = x[0];
-            if (k + 1 < a.cols) v.y = x[1];
-            if (k + 2 < a.cols) v.z = x[2];
-        }
-        const float top = w4_group_max<32>(fmaxf(fmaxf(finite_abs(v.x), finite_abs(v.y)), fmaxf(finite_abs(v.z), finite_abs(v.w))));
-        float inv;
-        const float sx = parts_scale(top, inv);
-        uint2 hi, lo;
-        parts4(v.x, v.y, v.z, v.w, inv, hi, lo);
-        uint8_t *at = s_x + (size_t)j * a.pitch + blk * W4_SPLIT + 8 * q;
-        *(uint2 *)at = hi;
-        *(uint2 *)(at + W4_SPLIT / 2) = lo;
-        if (q == 0) s_scale[blk * 16 + j] = sx;
-    }
+#pragma unroll
+    for (int t = 0; t < AHEAD; ++t) put(u0 + t * halves, xv[t]);
+    for (int u = u0 + AHEAD * halves; u < units; u += halves) put(u, load(u));
     __syncthreads();
 
     v4f *s_sum = (v4f *)(s_scale + 16 * a.nb);
+    const unsigned magic = w4_magic();
     v4f total = {0.0f, 0.0f, 0.0f, 0.0f};
     const uint8_t *px = s_x + (size_t)min(i, n - 1) * a.pitch + 16 * g;
+    // rows r0 .. r0 + 15 of all vectors, dropped past the end instead of branches (pitches are at most 2^24)
+    auto store = [&](int r0, v4f y, float add) {
+        const int some = min(16, a.rows - r0);
+        const __amdgpu_buffer_rsrc_t ry = q8_rsrc(a.Y + r0, 4 * ((size_t)(n - 1) * a.ldy + some));
+        const unsigned at = i < some ? 4u * i : Q8_OOB;
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+            __builtin_amdgcn_raw_buffer_store_b32(__float_as_int(y[v] + add), ry, (int)(4 * g + v < n ? at + 4u * (unsigned)(4 * g + v) * (unsigned)a.ldy : Q8_OOB), 0, 0);
+    };
     while (tile < tiles) {
         const int at = b, from = tile;
         const float add = bias;
@@ -240,8 +269,6 @@ __global__ __launch_bounds__(512) void w4_stream_kernel(W4GemmArgs a)
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
             if (at + s >= b1) break;
-            const uint8_t *x = px + (at + s) * W4_SPLIT;
-            const v4f sx = *(const v4f *)(s_scale + (at + s) * 16 + 4 * g);
             v4f hi, lo;
             v2h z1, z2;
             float sw = 0.0f;
@@ -252,12 +279,14 @@ __global__ __launch_bounds__(512) void w4_stream_kernel(W4GemmArgs a)
                     const unsigned e = (at + s) * PER + t / (4 / PER) < a.ng ? cs[word >> 2][word & 3] : 0u;
                     w4_zeros(e, z1, z2);
                     sw = __uint_as_float(e & 0xffff0000u);
-                    hi = lo = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
                 }
-                const v8h wv = w4_expand(cw[s][t], z1, z2);
-                hi = __builtin_amdgcn_mfma_f32_16x16x32_f16(*(const v8h *)(x + 64 * t), wv, hi, 0, 0, 0);
-                lo = __builtin_amdgcn_mfma_f32_16x16x32_f16(*(const v8h *)(x + 64 * t + W4_SPLIT / 2), wv, lo, 0, 0, 0);
+                const v8h wv = w4_expand(cw[s][t], z1, z2, magic);
+                const v4f none = {0.0f, 0.0f, 0.0f, 0.0f};
+                const uint8_t *x = px + (at + s) * W4_SPLIT + 64 * t;
+                hi = __builtin_amdgcn_mfma_f32_16x16x32_f16(*(const v8h *)x, wv, t % (4 / PER) == 0 ? none : hi, 0, 0, 0);
+                lo = __builtin_amdgcn_mfma_f32_16x16x32_f16(*(const v8h *)(x + W4_SPLIT / 2), wv, t % (4 / PER) == 0 ? none : lo, 0, 0, 0);
                 if (t % (4 / PER) == 4 / PER - 1) {
+                    const v4f sx = *(const v4f *)(s_scale + (at + s) * 16 + 4 * g);
 #pragma unroll
                     for (int v = 0; v < 4; ++v) total[v] = fmaf((hi[v] + lo[v]) * sw, sx[v], total[v]);      // (sw sx alone may pass fp32's range)
                 }
@@ -268,29 +297,23 @@ __global__ __launch_bounds__(512) void w4_stream_kernel(W4GemmArgs a)
         total = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
         if (split > 1) { s_sum[wave * 64 + lane] = sum; break; }
         // lane (i, g): row i, vectors 4 g + (0 .. 3)
-        const int r = 16 * from + i;
-#pragma unroll
-        for (int v = 0; v < 4; ++v)
-            if (r < a.rows && 4 * g + v < n) a.Y[(size_t)(4 * g + v) * a.ldy + r] = a.bias ? sum[v] + add : sum[v];
+        store(16 * from, sum, add);
     }
     if (split == 1) return;
     __syncthreads();                                                        // the ranges' sums, in one order
-    const int from = blockIdx.x + gridDim.x * (wave / split), r = 16 * from + i;
-    if (part || r >= a.rows) return;
+    const int from = blockIdx.x + gridDim.x * (wave / split);
+    if (part || from >= tiles) return;
     v4f sum = s_sum[wave * 64 + lane];
     for (int p = 1; p < split; ++p)
         if (p * a.span < a.nb) sum += s_sum[(wave + p) * 64 + lane];
-    const float add = a.bias ? a.bias[r] : 0.0f;
-#pragma unroll
-    for (int v = 0; v < 4; ++v)
-        if (4 * g + v < n) a.Y[(size_t)(4 * g + v) * a.ldy + r] = a.bias ? sum[v] + add : sum[v];
+    store(16 * from, sum, a.bias ? a.bias[min(16 * from + i, a.rows - 1)] : -0.0f);
 }
 
 // split: waves for a row's columns, a power of two, at most `waves`.  A part is a multiple of four blocks of columns, so that the last ones
 // may have none: these leave no sums, and none are added.
-static q8_status launch_stream_w4(q8_ctx *ctx, W4GemmArgs &a, int per_block, int waves, int split)
+template <int PER> static q8_status launch_stream_w4(q8_ctx *ctx, W4GemmArgs &a, int waves, int split)
 {
-    static Q8OncePerDevice once[3];
+    static Q8OncePerDevice once;
     a.split = split;
     a.span = ((a.nb + split - 1) / split + 3) / 4 * 4;
     a.pitch = a.nb * W4_SPLIT + 16;
@@ -298,28 +321,26 @@ static q8_status launch_stream_w4(q8_ctx *ctx, W4GemmArgs &a, int per_block, int
     int blocks = (tiles + per - 1) / per;
     if (split == 1 && blocks > 512) blocks = 512;
     const size_t smem = (size_t)a.n * a.pitch + 64 * a.nb + (split > 1 ? 1024 * waves : 0);
-    void (*const kernel)(W4GemmArgs) = per_block == 4 ? w4_stream_kernel<4> : per_block == 2 ? w4_stream_kernel<2> : w4_stream_kernel<1>;
-    const q8_status st = smem > 65536 ? q8i_lds(ctx, once[per_block >> 1], (const void *)kernel, W4_STREAM_LDS, "w4 product") : Q8_OK;
+    const q8_status st = smem > 65536 ? q8i_lds(ctx, once, (const void *)w4_stream_kernel<PER>, W4_STREAM_LDS, "w4 product") : Q8_OK;
     if (st) return st;
-    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(64 * waves), smem, ctx->stream, a);
+    hipLaunchKernelGGL(w4_stream_kernel<PER>, dim3(blocks), dim3(64 * waves), smem, ctx->stream, a);
     return q8i_launch_check(ctx, "product w4");
 }
 
 // ------------------------------------------------------------------------------ many vectors ----
 
 // A vector's parts and scale, a block per vector.
-__global__ __launch_bounds__(256) void w4_parts_kernel(const float *X, int cols, int ldx, int vec, int nb, uint8_t *parts, float *sx)
+__global__ __launch_bounds__(256) void w4_parts_kernel(const float *X, int cols, int ldx, int nb, uint8_t *parts, float *sx)
 {
     __shared__ float s_max[4];
     const int j = blockIdx.x, tid = threadIdx.x;
     const float *x = X + (size_t)j * ldx;
     auto load = [&](int k) {
         float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (k + 3 < cols && vec) return *(const float4 *)(x + k);
+        if (k + 3 < cols) return *(const float4 *)(x + k);
         if (k < cols) v.x = x[k];
         if (k + 1 < cols) v.y = x[k + 1];
         if (k + 2 < cols) v.z = x[k + 2];
-        if (k + 3 < cols) v.w = x[k + 3];
         return v;
     };
     float4 keep[2];                                                         // the first 2048 columns stay in registers
@@ -328,7 +349,7 @@ __global__ __launch_bounds__(256) void w4_parts_kernel(const float *X, int cols,
         const float4 v = load(t * 1024 + 4 * tid);
         if (t == 0) keep[0] = v;
         if (t == 1) keep[1] = v;
-        m = fmaxf(m, fmaxf(fmaxf(finite_abs(v.x), finite_abs(v.y)), fmaxf(finite_abs(v.z), finite_abs(v.w))));
+        m = fmaxf(m, fmaxf(fmaxf(fabsf(v.x), fabsf(v.y)), fmaxf(fabsf(v.z), fabsf(v.w))));
     }
     m = wave_max_f(m);
     if ((tid & 63) == 0) s_max[tid >> 6] = m;
@@ -357,31 +378,48 @@ __device__ __forceinline__ void w4_to_lds(__amdgpu_buffer_rsrc_t rsrc, uint8_t *
 #endif
 }
 
-// Block of WM x WN waves, each with 32 TM rows x 32 TN vectors; the vectors' parts come in stages of 128 columns (half a kilobyte a vector)
-// from memory to LDS, one on its way while the one before is multiplied; each wave reads its rows' codes (64 bytes a stage) by itself.
-// Lane (i, h) of a row tile has the 16-byte pieces h and 2 + h of row i: word t of piece 2 p + h belongs to columns 32 t + 16 p + 8 h + (0 .. 7),
-// operation (t, p) of a stage to columns 32 t + 16 p + (0 .. 15).  In LDS a vector's 32 pieces of 16 bytes are exchanged by its number mod 8, so that
-// lanes that read together find theirs on different banks.
-template <int PER, int WM, int WN, int TM, int TN>
-__global__ __launch_bounds__(64 * WM * WN) void w4_gemm_kernel(W4GemmArgs a)
+// The tile of a block.  Consecutive blocks run on different XCDs, each with an L2 cache of its own: each XCD gets a range of the tiles in a row, those
+// of the same rows one after the other, so that it reads its rows' codes from memory once.
+__device__ __forceinline__ unsigned w4_tile_of()
 {
-    constexpr int VECS = 32 * WN * TN, THREADS = 64 * WM * WN, STAGE = VECS * W4_SPLIT, LX = VECS * 32 / THREADS;
-    static_assert(VECS * 32 % THREADS == 0, "even shares of a stage");
-    extern __shared__ __align__(16) uint8_t s_x[];                          // [2][STAGE]
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave % WM, wn = wave / WM, i = lane & 31, h = lane >> 5;
-    const int tr = blockIdx.x / a.col_tiles, tc = blockIdx.x % a.col_tiles;
-    const int r0 = 32 * TM * (tr * WM + wm), c0 = tc * VECS, left = min(VECS, a.n - c0);
+    const unsigned total = gridDim.x, per = total / 8, over = total % 8, xcd = blockIdx.x % 8, idx = blockIdx.x / 8;
+    return xcd * per + min(xcd, over) + idx;
+}
+
+template <int PER> struct W4Words;                                          // a block's words of a row, in one load
+template <> struct W4Words<1> { typedef unsigned type; };
+template <> struct W4Words<2> { typedef v2u type; };
+template <> struct W4Words<4> { typedef v4u type; };
+
+// Block of WM x WN waves, each with 32 TM rows x 32 TN vectors; the vectors' parts come in stages of 64 columns (256 bytes a vector) from memory to
+// LDS, one on its way while the one before is multiplied; each wave reads its rows' codes (64 bytes for two stages) by itself, the next ones ahead.
+// Lane (i, h) of a row tile has the 16-byte pieces h and 2 + h of row i: word t of piece 2 p + h belongs to columns 32 t + 16 p + 8 h + (0 .. 7),
+// operation (t, p) of a block to columns 32 t + 16 p + (0 .. 15).  In LDS a vector's 16 pieces (hi, lo) are exchanged by its number mod 16, so that
+// lanes that read together find theirs on different banks.
+// KS > 1: KS such groups of waves take turns at the blocks of columns; their sums meet in LDS, in one order.  PAST: the results go past the caches.
+template <int PER, int WM, int WN, int TM, int TN, int KS, bool PAST>
+__global__ __launch_bounds__(64 * WM * WN * KS, TM * TN <= 4 ? 2 : 1) void w4_gemm_kernel(W4GemmArgs a)
+{
+    constexpr int VECS = 32 * WN * TN, THREADS = 64 * WM * WN, STAGE = VECS * 256, LX = VECS * 16 / THREADS, EACH = 4 / PER;      // EACH: operations t of a group
+    static_assert(VECS * 16 % THREADS == 0, "even shares of a stage");
+    typedef typename W4Words<PER>::type Words;
+    extern __shared__ __align__(16) uint8_t s_all[];                        // [KS][2][STAGE]
+    const int ks = KS > 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x / THREADS) : 0, tid = (int)threadIdx.x - ks * THREADS;
+    uint8_t *s_x = s_all + ks * 2 * STAGE;
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave % WM, wn = wave / WM, i = lane & 31, h = lane >> 5;
+    const unsigned tile = w4_tile_of(), tr = tile / (unsigned)a.col_tiles, tc = tile % (unsigned)a.col_tiles;
+    const int r0 = 32 * TM * ((int)tr * WM + wm), c0 = (int)tc * VECS, left = min(VECS, a.n - c0);
     const __amdgpu_buffer_rsrc_t rx = q8_rsrc(a.parts + (size_t)c0 * a.nb * W4_SPLIT, (size_t)left * a.nb * W4_SPLIT);
-    unsigned ox[LX];                                                        // piece p of a stage: vector p / 32 (beyond the last: the last again)
+    unsigned ox[LX];                                                        // place p of a stage: vector p / 16 (beyond the last: the last again)
 #pragma unroll
     for (int u = 0; u < LX; ++u) {
-        const int p = u * THREADS + tid, v = p >> 5;
-        ox[u] = (unsigned)min(v, left - 1) * (unsigned)(a.nb * W4_SPLIT) + 16u * (unsigned)((p & 31) ^ (v & 7));
+        const int p = u * THREADS + tid, v = p >> 4, piece = (p & 15) ^ (v & 15);
+        ox[u] = (unsigned)min(v, left - 1) * (unsigned)(a.nb * W4_SPLIT) + (piece >> 3) * (W4_SPLIT / 2) + 16u * (piece & 7);
     }
-    auto request = [&](int b, int stage) {
-        uint8_t *at = s_x + stage * STAGE + wave * 1024;
+    auto request = [&](int stage) {
+        uint8_t *at = s_x + (stage & 1) * STAGE + wave * 1024;
 #pragma unroll
-        for (int u = 0; u < LX; ++u) w4_to_lds(rx, at + u * THREADS * 16, ox[u], b * W4_SPLIT);
+        for (int u = 0; u < LX; ++u) w4_to_lds(rx, at + u * THREADS * 16, ox[u], (stage >> 1) * W4_SPLIT + (stage & 1) * 128);
     };
     const uint8_t *pw[TM];
     const unsigned *ps[TM];
@@ -391,78 +429,63 @@ __global__ __launch_bounds__(64 * WM * WN) void w4_gemm_kernel(W4GemmArgs a)
         pw[t] = a.W + row * a.ldw + 16 * h;
         ps[t] = a.sw + row * a.lds;
     }
-    v4u w[TM][2];
-    unsigned sc[TM][PER];
+    v4u w[TM][2], cw[TM][2];
+    Words sc[TM];
+    unsigned cs[TM][PER];
     auto codes = [&](int b) {
 #pragma unroll
         for (int t = 0; t < TM; ++t) {
             w[t][0] = *(const v4u *)(pw[t] + 64 * b);
             w[t][1] = *(const v4u *)(pw[t] + 64 * b + 32);
-#pragma unroll
-            for (int p = 0; p < PER; ++p) sc[t][p] = b * PER + p < a.ng ? ps[t][b * PER + p] : 0u;
+            sc[t] = *(const Words *)(ps[t] + b * PER);
         }
     };
-    v16f acc[TM][TN];
+    v16f acc[TM][TN], sum[TM][TN];
 #pragma unroll
     for (int t = 0; t < TM; ++t)
 #pragma unroll
         for (int u = 0; u < TN; ++u)
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[t][u][e] = 0.0f;
-    const int twist = i & 7, lx = (32 * wn * TN + i) * W4_SPLIT;
-    codes(0);
-    request(0, 0);
-#pragma unroll 1
-    for (int b = 0; b < a.nb; ++b) {
-        __syncthreads();                                                    // this stage is there, the other one is free
-        if (b + 1 < a.nb) request(b + 1, (b + 1) & 1);
-        v4u cw[TM][2];
-        unsigned cs[TM][PER];
+    const int lx = (32 * wn * TN + i) * 256, twist = i & 15;
+    v2h z1[TM], z2[TM];
+    const unsigned magic = w4_magic();
+    // half a block: operations t = 2 half, 2 half + 1
+    auto multiply = [&](auto half_) {
+        constexpr int half = decltype(half_)::value;
+        const uint8_t *px = s_x + half * STAGE + lx;
 #pragma unroll
-        for (int t = 0; t < TM; ++t) {
-            cw[t][0] = w[t][0];
-            cw[t][1] = w[t][1];
+        for (int q = 0; q < 2; ++q) {
+            constexpr int t0 = 2 * half;
+            const int t = t0 + q, group = t / EACH;
+            const bool begins = t % EACH == 0;
+            if (begins) {
 #pragma unroll
-            for (int p = 0; p < PER; ++p) cs[t][p] = sc[t][p];
-        }
-        if (b + 1 < a.nb) codes(b + 1);
-        const uint8_t *px = s_x + (b & 1) * STAGE + lx;
-        v16f sum[TM][TN];
-        v2h z1[TM], z2[TM];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            if (t % (4 / PER) == 0) {
-#pragma unroll
-                for (int m = 0; m < TM; ++m) {
-                    w4_zeros(cs[m][t / (4 / PER)], z1[m], z2[m]);
-#pragma unroll
-                    for (int u = 0; u < TN; ++u)
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) sum[m][u][e] = 0.0f;
-                }
+                for (int m = 0; m < TM; ++m) w4_zeros(cs[m][group], z1[m], z2[m]);
             }
 #pragma unroll
             for (int p = 0; p < 2; ++p) {
-                const int piece = 4 * t + 2 * p + h;
+                const int piece = 4 * q + 2 * p + h;
                 v8h xh[TN], xl[TN];
 #pragma unroll
                 for (int u = 0; u < TN; ++u) {
-                    xh[u] = *(const v8h *)(px + u * 32 * W4_SPLIT + 16 * (piece ^ twist));
-                    xl[u] = *(const v8h *)(px + u * 32 * W4_SPLIT + 16 * ((16 + piece) ^ twist));
+                    xh[u] = *(const v8h *)(px + u * 32 * 256 + 16 * (piece ^ twist));
+                    xl[u] = *(const v8h *)(px + u * 32 * 256 + 16 * ((8 + piece) ^ twist));
                 }
 #pragma unroll
                 for (int m = 0; m < TM; ++m) {
-                    const v8h wv = w4_expand(cw[m][p][t], z1[m], z2[m]);
+                    const v8h wv = w4_expand(cw[m][p][t], z1[m], z2[m], magic);
+                    const v16f none = {};
 #pragma unroll
-                    for (int u = 0; u < TN; ++u) sum[m][u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(xh[u], wv, sum[m][u], 0, 0, 0);
+                    for (int u = 0; u < TN; ++u) sum[m][u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(xh[u], wv, begins && p == 0 ? none : sum[m][u], 0, 0, 0);
 #pragma unroll
                     for (int u = 0; u < TN; ++u) sum[m][u] = __builtin_amdgcn_mfma_f32_32x32x16_f16(xl[u], wv, sum[m][u], 0, 0, 0);
                 }
             }
-            if (t % (4 / PER) == 4 / PER - 1) {
+            if (t % EACH == EACH - 1) {
 #pragma unroll
                 for (int m = 0; m < TM; ++m) {
-                    const float sw = __uint_as_float(cs[m][t / (4 / PER)] & 0xffff0000u);
+                    const float sw = __uint_as_float(cs[m][group] & 0xffff0000u);
 #pragma unroll
                     for (int u = 0; u < TN; ++u)
 #pragma unroll
@@ -470,70 +493,157 @@ __global__ __launch_bounds__(64 * WM * WN) void w4_gemm_kernel(W4GemmArgs a)
                 }
             }
         }
+    };
+    const int turns = (a.nb + KS - 1) / KS;
+    if (ks < a.nb) {
+        codes(ks);
+        request(2 * ks);
     }
-    // lane (i, h): row i of a row tile, vectors 8 q + 4 h + (0 .. 3) of a tile of vectors
-    float bias[TM];
+#pragma unroll 1
+    for (int turn = 0; turn < turns; ++turn) {
+        const int b = turn * KS + ks;
+        const bool more = b + KS < a.nb;
 #pragma unroll
-    for (int t = 0; t < TM; ++t) bias[t] = a.bias ? a.bias[min(r0 + 32 * t + i, a.rows - 1)] : 0.0f;
+        for (int t = 0; t < TM; ++t) {
+            cw[t][0] = w[t][0];
+            cw[t][1] = w[t][1];
 #pragma unroll
-    for (int u = 0; u < TN; ++u) {
-        const int v0 = c0 + 32 * (wn * TN + u) + 4 * h;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int v = v0 + 8 * (e >> 2) + (e & 3);
-            const float s = a.sx[min(v, a.n - 1)];
-#pragma unroll
-            for (int t = 0; t < TM; ++t) {
-                const int row = r0 + 32 * t + i;
-                const float y = acc[t][u][e] * s;
-                if (row < a.rows && v < a.n) a.Y[(size_t)v * a.ldy + row] = a.bias ? y + bias[t] : y;
+            for (int p = 0; p < PER; ++p) {                                 // (past the last group: anything)
+                unsigned word;
+                if constexpr (PER == 1) word = sc[t];
+                else word = sc[t][p];
+                cs[t][p] = b * PER + p < a.ng ? word : 0u;
             }
         }
+        q8_stores_performed();                                              // (what this wave asked for is in LDS: the barrier alone does not wait for it)
+        __syncthreads();                                                    // this stage is there, the other one is free
+        if (b < a.nb) request(2 * b + 1);
+        if (more) codes(b + KS);
+        if (b < a.nb) multiply(std::integral_constant<int, 0>());
+        q8_stores_performed();
+        __syncthreads();
+        if (more) request(2 * (b + KS));
+        if (b < a.nb) multiply(std::integral_constant<int, 1>());
+    }
+    if constexpr (KS > 1) {
+        // the groups' sums, a group's where its stages were: [wave][t][u][e][lane]
+        static_assert(STAGE * 2 >= TM * TN * 16 * THREADS * 4, "a group's sums fit where its stages were");
+        __syncthreads();
+        float *mine = (float *)s_x + wave * TM * TN * 1024 + lane;
+        if (ks > 0) {
+#pragma unroll
+            for (int t = 0; t < TM; ++t)
+#pragma unroll
+                for (int u = 0; u < TN; ++u)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) mine[((t * TN + u) * 16 + e) * 64] = acc[t][u][e];
+        }
+        __syncthreads();
+        if (ks > 0) return;
+#pragma unroll
+        for (int g = 1; g < KS; ++g) {
+            const float *o = (const float *)(s_all + g * 2 * STAGE) + wave * TM * TN * 1024 + lane;
+#pragma unroll
+            for (int t = 0; t < TM; ++t)
+#pragma unroll
+                for (int u = 0; u < TN; ++u)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) acc[t][u][e] += o[((t * TN + u) * 16 + e) * 64];
+        }
+    }
+    // lane (i, h): row i of a row tile, vectors 8 q + 4 h + (0 .. 3) of a tile of vectors.
+    // (All loads first, and stores that are dropped past the end of eight vectors instead of branches: a branch would wait for the store before.)
+    const int row = r0 + i;
+    v4f sx[TN][4];                                                          // the vectors' scales (room for whole tiles is there)
+#pragma unroll
+    for (int u = 0; u < TN; ++u)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) sx[u][q] = *(const v4f *)(a.sx + c0 + 32 * (wn * TN + u) + 8 * q + 4 * h);
+    float bias[TM];
+#pragma unroll
+    for (int t = 0; t < TM; ++t) bias[t] = a.bias ? a.bias[min(row + 32 * t, a.rows - 1)] : -0.0f;       // (y + -0 is y)
+#pragma unroll
+    for (int t = 0; t < TM; ++t) {
+        const unsigned at = row + 32 * t < a.rows ? 4u * i : Q8_OOB;        // (pitches are at most 2^25: eight vectors lie below 2^30 bytes)
+#pragma unroll
+        for (int u = 0; u < TN; ++u)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int v0 = c0 + 32 * (wn * TN + u) + 8 * q, some = min(8, a.n - v0), first = r0 + 32 * t;
+                const __amdgpu_buffer_rsrc_t ry = q8_rsrc(a.Y + (size_t)v0 * a.ldy + first, some > 0 && first < a.rows ? 4 * ((size_t)(some - 1) * a.ldy + min(32, a.rows - first)) : 0);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)                                 // (y times the power of two is exact but for the range)
+                    __builtin_amdgcn_raw_buffer_store_b32(__float_as_int(fmaf(acc[t][u][4 * q + e], sx[u][q][e], bias[t])), ry,
+                                                          (int)(at + 4u * (unsigned)(4 * h + e) * (unsigned)a.ldy), 0, PAST ? 2 : 0);
+            }
     }
 }
 
-template <int PER, int WM, int WN, int TM, int TN> static q8_status launch_w4(q8_ctx *ctx, W4GemmArgs &a)
+template <int PER, int WM, int WN, int TM, int TN, int KS = 1> static q8_status launch_w4(q8_ctx *ctx, W4GemmArgs &a)
 {
-    static Q8OncePerDevice once;
-    const size_t smem = (size_t)2 * 32 * WN * TN * W4_SPLIT;
+    constexpr size_t smem = (size_t)KS * 2 * 32 * WN * TN * 256;
     a.row_tiles = (a.rows + 32 * WM * TM - 1) / (32 * WM * TM);
     a.col_tiles = (a.n + 32 * WN * TN - 1) / (32 * WN * TN);
     const size_t tiles = (size_t)a.row_tiles * a.col_tiles;
-    if (tiles * (64 * WM * WN) > 0xffffffffu)                               // a launch has fewer than 2^32 threads
+    if (tiles * (64 * WM * WN * KS) > 0xffffffffu)                          // a launch has fewer than 2^32 threads
         return q8_fail(ctx, Q8_ERR_SHAPE, "w4 product: %d x %d results are too many for a launch", a.rows, a.n);
-    const q8_status st = q8i_lds(ctx, once, (const void *)w4_gemm_kernel<PER, WM, WN, TM, TN>, smem, "w4 product");
+    // past the caches where blocks do not share the 64-byte pieces that memory takes, which the caches put together
+    const bool past = a.ldy % 16 == 0 && ((uintptr_t)a.Y & 63) == 0;
+    void (*const kernel)(W4GemmArgs) = past ? w4_gemm_kernel<PER, WM, WN, TM, TN, KS, true> : w4_gemm_kernel<PER, WM, WN, TM, TN, KS, false>;
+    static Q8OncePerDevice once[2];
+    const q8_status st = q8i_lds(ctx, once[past], (const void *)kernel, smem, "w4 product");
     if (st) return st;
-    hipLaunchKernelGGL((w4_gemm_kernel<PER, WM, WN, TM, TN>), dim3((unsigned)tiles), dim3(64 * WM * WN), smem, ctx->stream, a);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)tiles), dim3(64 * WM * WN * KS), smem, ctx->stream, a);
     return q8i_launch_check(ctx, "product w4");
 }
 
+// Tiles by what each costs (us, both launches; rows x columns x vectors / group).  Where 64 x 32 tiles are few and rows longer than two blocks, groups of waves
+// share the columns: 64 x 32 in four groups while they are at most one round (8000 x 1024 x 64 / 64 10.7 against 14.6 in 128 x 32, 1024 x 1024 x 256 / 64 11.2
+// against 15.7, 4096 x 2048 x 128 / 128 15.6 against 25.0), 32 x 32 for the fewest of long rows (600 x 2000 x 100 / 32 13.7 against 14.9, 2048 x 2048 x 32 / 128 12.4
+// against 13.6; 20000 x 512 x 32 12.1 against 9.8), two groups up to two rounds (20000 x 512 x 32 / 128 9.2 against 9.8 in four and 10.3 in 128 x 32; 50000 x 512 x 17 / 64
+// in 128 x 32 10.9, four groups 13.1).  Else 128 x 64 where the vectors fill them (50000 x 512 x 40 / 128 14.4 against 15.8, x 1024 142 against 156 in 128 x 32; tiles of 256 x 64 and
+// 128 x 128, in which a wave holds 64 rows, 149 to 161: fewer waves cover less of each other's stores), and 128 x 32 (63644 x 620 x 77 / 32 28.4 against 34.0; 128 x 96 28.5).
 template <int PER> static q8_status gemm_w4_tiles(q8_ctx *ctx, W4GemmArgs &a)
 {
-    if (a.n <= 32) return launch_w4<PER, 4, 1, 1, 1>(ctx, a);
-    return launch_w4<PER, 4, 1, 1, 2>(ctx, a);
+    const long long few = (long long)((a.rows + 63) / 64) * ((a.n + 31) / 32);
+    if (a.nb >= 8 && few <= 64) return launch_w4<PER, 1, 1, 1, 1, 4>(ctx, a);
+    if (a.nb > 2 && few <= 256) return launch_w4<PER, 2, 1, 1, 1, 4>(ctx, a);
+    if (a.nb > 2 && few <= 512) return launch_w4<PER, 2, 1, 1, 1, 2>(ctx, a);
+    if (a.n > 32 && (a.n + 63) / 64 * 256ll <= 7ll * a.n) return launch_w4<PER, 4, 1, 1, 2>(ctx, a);
+    return launch_w4<PER, 4, 1, 1, 1>(ctx, a);
 }
 
 // Every block makes the vectors' parts for itself, which saves a launch and costs time with their number.
 static bool gemm_w4_streams(int n, int nb) { return n <= 16 && (long long)n * nb <= W4_STREAM_BLOCKS; }
 
+size_t q8i_gemm_w4_scales(int n) { return ((size_t)n + 255) / 256 * 256; }
+
 size_t q8i_gemm_w4_parts(int n, int cols) { return (size_t)n * ((cols + W4_BLOCK - 1) / W4_BLOCK) * W4_SPLIT; }
+
+template <int PER> static q8_status gemm_w4(q8_ctx *ctx, W4GemmArgs &a, bool streams)
+{
+    if (!streams) return gemm_w4_tiles<PER>(ctx, a);
+    const int tiles = (a.rows + 15) / 16;
+    int split = 1;
+    while (split < 8 && a.nb > 4 * split && tiles * split < 2048) split *= 2;
+    int waves = tiles < 1024 && split == 1 ? 4 : 8;
+    if (split == 8 && a.nb > 32 && tiles <= 256) waves = split = 16;
+    return launch_stream_w4<PER>(ctx, a, waves, split);
+}
 
 q8_status q8i_gemm_w4(q8_ctx *ctx, const q8_mat_w4 *W, const float *X, int n, int ldx, const float *bias, float *Y, int ldy, uint8_t *parts, float *sx)
 {
     W4GemmArgs a = {W->data, W->scale, X, parts, sx, bias, Y, W->rows, n, W->cols, W->ld, W->lds, (W->cols + W->group - 1) / W->group, ldx, ldy,
-                    (W->cols + W4_BLOCK - 1) / W4_BLOCK, 0, 0, 0, 0, 0, 0};
-    a.vec = ldx % 4 == 0 && ((uintptr_t)X & 15) == 0;
+                    (W->cols + W4_BLOCK - 1) / W4_BLOCK, 0, 0, 0, 0, 0};
     const int per = W4_BLOCK / W->group;
+    if (n == 1) a.ldx = a.cols, a.ldy = a.rows;                             // (pitches that nothing uses, but bounds are formed with)
     // (results over the vectors: these are read first, as a whole)
     const uintptr_t x0 = (uintptr_t)X, x1 = x0 + 4 * ((size_t)(n - 1) * ldx + a.cols), y0 = (uintptr_t)Y, y1 = y0 + 4 * ((size_t)(n - 1) * ldy + a.rows);
-    if (gemm_w4_streams(n, a.nb) && !(x0 < y1 && y0 < x1)) {
-        const int tiles = (a.rows + 15) / 16;
-        int split = 1;
-        while (split < 8 && a.nb > 4 * split && tiles * split < 2048) split *= 2;
-        return launch_stream_w4(ctx, a, per, tiles < 1024 && split == 1 ? 4 : 8, split);
+    const bool streams = gemm_w4_streams(n, a.nb) && ldx <= 1 << 24 && a.ldy <= 1 << 24 && !(x0 < y1 && y0 < x1);
+    if (!streams) {
+        hipLaunchKernelGGL(w4_parts_kernel, dim3(n), dim3(256), 0, ctx->stream, X, a.cols, ldx, a.nb, parts, sx);
+        const q8_status st = q8i_launch_check(ctx, "parts w4");
+        if (st) return st;
     }
-    hipLaunchKernelGGL(w4_parts_kernel, dim3(n), dim3(256), 0, ctx->stream, X, a.cols, ldx, a.vec, a.nb, parts, sx);
-    const q8_status st = q8i_launch_check(ctx, "parts w4");
-    if (st) return st;
-    return per == 4 ? gemm_w4_tiles<4>(ctx, a) : per == 2 ? gemm_w4_tiles<2>(ctx, a) : gemm_w4_tiles<1>(ctx, a);
+    return per == 4 ? gemm_w4<4>(ctx, a, streams) : per == 2 ? gemm_w4<2>(ctx, a, streams) : gemm_w4<1>(ctx, a, streams);
 }

@@ -59,7 +59,7 @@ def test_products(lib):
     call = lambda x=P, n=4, ldx=64, b=None, y=P, ldy=32: lib.q8_gemm_w4(c, mat(), x, n, ldx, b, y, ldy)
     assert lib.q8_gemm_w4(None, mat(), P, 4, 64, None, P, 32) == lib.q8_gemm_w4(c, None, P, 4, 64, None, P, 32) == NULL
     assert call(x=None) == call(y=None) == NULL
-    assert call(n=0) == call(n=-3) == call(n=(1 << 20) + 1) == call(ldx=60) == call(ldy=31) == SHAPE
+    assert call(n=0) == call(n=-3) == call(n=(1 << 20) + 1) == call(ldx=60) == call(ldy=31) == call(ldy=(1 << 25) + 4) == SHAPE
     assert call(ldx=66) == call(x=P + 4) == call(y=P + 2) == call(b=P + 1) == ALIGN
     assert call(n=1 << 20) == call(n=1000) == WORKSPACE
     assert call() == call(n=1, ldx=0, ldy=0) == DEVICE

@@ -598,18 +598,24 @@ template <int PER, int WM, int WN, int TM, int TN, int KS = 1> static q8_status 
 }
 
 // Tiles by what each costs (us, both launches; rows x columns x vectors / group).  Where 64 x 32 tiles are few and rows longer than two blocks, groups of waves
-// share the columns: 64 x 32 in four groups while they are at most one round (8000 x 1024 x 64 / 64 10.7 against 14.6 in 128 x 32, 1024 x 1024 x 256 / 64 11.2
-// against 15.7, 4096 x 2048 x 128 / 128 15.6 against 25.0), 32 x 32 for the fewest of long rows (600 x 2000 x 100 / 32 13.7 against 14.9, 2048 x 2048 x 32 / 128 12.4
-// against 13.6; 20000 x 512 x 32 12.1 against 9.8), two groups up to two rounds (20000 x 512 x 32 / 128 9.2 against 9.8 in four and 10.3 in 128 x 32; 50000 x 512 x 17 / 64
-// in 128 x 32 10.9, four groups 13.1).  Else 128 x 64 where the vectors fill them (50000 x 512 x 40 / 128 14.4 against 15.8, x 1024 142 against 156 in 128 x 32; tiles of 256 x 64 and
-// 128 x 128, in which a wave holds 64 rows, 149 to 161: fewer waves cover less of each other's stores), and 128 x 32 (63644 x 620 x 77 / 32 28.4 against 34.0; 128 x 96 28.5).
+// share the columns: 64 x 32 in four groups while they are at most one round (4096 x 2048 x 128 / 128 13.9 against 23.6 in 128 x 32, 1024 x 1024 x 256 / 64 11.2
+// against 15.7), 32 x 32 for the fewest of long rows (600 x 2000 x 100 / 32 13.7 against 14.9, 2048 x 2048 x 32 / 128 12.4 against 13.6), two groups up to two
+// rounds (20000 x 512 x 32 / 128 7.7 against 8.1 in four and 8.9 in 128 x 32, 30000 x 1000 x 24 / 64 10.8, 11.0 and 13.5; 50000 x 512 x 17 / 64 10.3, 11.6 and 9.5).  Else
+// 256 x 64 where there are many and the vectors fill them (50000 x 512 x 1024 / 128 124; 128 x 64 131, 128 x 32 146), 128 x 64 where these are more than a
+// round (50000 x 512 x 40 / 128 12.3 against 13.6 in 128 x 32; 8000 x 1024 x 200 / 64 17.7 against 15.9), 128 x 96 for 65 to 96 vectors of many rows
+// (63644 x 620 x 77 / 32 24.4 against 25.8 in 128 x 32 and 29.3 in 128 x 64), and 128 x 32.
 template <int PER> static q8_status gemm_w4_tiles(q8_ctx *ctx, W4GemmArgs &a)
 {
     const long long few = (long long)((a.rows + 63) / 64) * ((a.n + 31) / 32);
+    auto tiles = [&](int r, int v) { return (long long)((a.rows + r - 1) / r) * ((a.n + v - 1) / v); };
     if (a.nb >= 8 && few <= 64) return launch_w4<PER, 1, 1, 1, 1, 4>(ctx, a);
     if (a.nb > 2 && few <= 256) return launch_w4<PER, 2, 1, 1, 1, 4>(ctx, a);
     if (a.nb > 2 && few <= 512) return launch_w4<PER, 2, 1, 1, 1, 2>(ctx, a);
-    if (a.n > 32 && (a.n + 63) / 64 * 256ll <= 7ll * a.n) return launch_w4<PER, 4, 1, 1, 2>(ctx, a);
+    if (a.n > 64 && a.n <= 96 && tiles(128, 96) >= 400) return launch_w4<PER, 4, 1, 1, 3>(ctx, a);
+    if ((a.n + 63) / 64 * 320ll <= 8ll * a.n) {
+        if (tiles(256, 64) >= 1024) return launch_w4<PER, 4, 1, 2, 2>(ctx, a);
+        if (tiles(128, 64) >= 320) return launch_w4<PER, 4, 1, 1, 2>(ctx, a);
+    }
     return launch_w4<PER, 4, 1, 1, 1>(ctx, a);
 }
 

@@ -415,14 +415,18 @@ __global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(Delt
     const int tile0 = 2 * queries + mt, r0 = 16 * mt + 4 * gq;
     // rows 16 (4 t + tile0) + 4 gq + e of column `col` of the state
     v4f st[OWN];
-    const size_t at = ((size_t)s * p.hv + head) * p.dk * p.dv + col;
+    const size_t own = ((size_t)s * p.hv + head) * p.dk * p.dv, bytes = 4 * (size_t)p.dk * p.dv;
+    auto state_at = [&](int t, int e) {
+        const int row = 16 * (4 * t + tile0) + 4 * gq + e;
+        return (int)(live && row < p.dk ? 4u * ((unsigned)row * (unsigned)p.dv + col) : Q8_OOB);
+    };
+    {
+        const __amdgpu_buffer_rsrc_t rs = q8_rsrc(a.state + own, a.state ? bytes : 0);      // (none: zeros)
 #pragma unroll
-    for (int t = 0; t < OWN; ++t)
+        for (int t = 0; t < OWN; ++t)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int row = 16 * (4 * t + tile0) + 4 * gq + e;
-            st[t][e] = a.state && live && row < p.dk ? a.state[at + (size_t)row * p.dv] : 0.0f;
-        }
+            for (int e = 0; e < 4; ++e) st[t][e] = __int_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, state_at(t, e), 0, 0));
+    }
     // a thread's pieces: of keys and queries, of T and M, of values and results (half of the threads), of the tokens' numbers (48 threads); offsets
     // inside a chunk: rows past its end lie past the end of what is described
     unsigned ok[OWN], oq[OWN];
@@ -579,14 +583,11 @@ __global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(Delt
         __syncthreads();
     }
     if (length > 0 && tid < 256) results((length - 1) / DELTA_C * DELTA_C);
-    if (a.state_out && live)
+    const __amdgpu_buffer_rsrc_t rs = q8_rsrc(a.state_out + own, a.state_out ? bytes : 0);
 #pragma unroll
-        for (int t = 0; t < OWN; ++t)
+    for (int t = 0; t < OWN; ++t)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int row = 16 * (4 * t + tile0) + 4 * gq + e;
-                if (row < p.dk) a.state_out[at + (size_t)row * p.dv] = st[t][e];
-            }
+        for (int e = 0; e < 4; ++e) __builtin_amdgcn_raw_buffer_store_b32(__float_as_int(st[t][e]), rs, state_at(t, e), 0, 0);
 }
 
 template <int DKT> static q8_status launch_sequence(q8_ctx *ctx, const DeltaSeqArgs &a)

@@ -2050,7 +2050,7 @@ size_t q8_delta_bytes(int L, int n_seq, int hv, int dk, int dv)
 {
     if (L < 0 || L > kDeltaMaxL || n_seq <= 0 || n_seq > kDeltaMaxSeq || hv <= 0 || hv > kDeltaMaxHeads || dk <= 0 || dk > kDeltaMaxDim || dv <= 0 || dv > kDeltaMaxDim)
         return Q8_WS_HEADER;
-    return Q8_WS_HEADER + up256(q8i_delta_room(L, n_seq, hv));
+    return Q8_WS_HEADER + up256(q8i_delta_room(L, n_seq, hv, dk, dv));
 }
 
 q8_status q8_delta_sequence(q8_ctx *ctx, const q8_delta_inputs *in, int L, const int32_t *off, int n_seq, const float *state, float *state_out,
@@ -2066,7 +2066,7 @@ q8_status q8_delta_sequence(q8_ctx *ctx, const q8_delta_inputs *in, int L, const
     const uintptr_t a0 = (uintptr_t)state, b0 = (uintptr_t)state_out;
     if (state && state_out && a0 != b0 && a0 < b0 + all && b0 < a0 + all) return q8_fail(ctx, Q8_ERR_SHAPE, "q8_delta_sequence: state_out lies over states that are still to be read");
     Carver cv(ctx);
-    float *room = (float *)cv.take<char>(q8i_delta_room(L, n_seq, in->hv));
+    float *room = (float *)cv.take<char>(q8i_delta_room(L, n_seq, in->hv, in->dk, in->dv));
     if (!cv.ok) return q8_fail(ctx, Q8_ERR_WORKSPACE, "q8_delta_sequence: workspace too small");
     return q8i_delta_sequence(ctx, in, L, off, n_seq, state, state_out, out, ldo, room);
 }

@@ -3,6 +3,7 @@
 #include "q8_internal.h"
 #include "q8_parts.h"
 
+#include <algorithm>
 #include <math.h>
 
 typedef float v4f __attribute__((ext_vector_type(4)));
@@ -191,6 +192,8 @@ struct DeltaSeqArgs {
     const float *state;
     float *state_out, *out;
     int ldo, vec_qk, vec;            // vec_qk: rows of queries and keys in whole 16-byte pieces, vec: those of values and results too
+    int seg, segs;                   // 0: a block carries a whole sequence; else segments of `seg` chunks, places of segments (as those of chunks)
+    float *ends, *moves;             // per place and head: the state that a segment ends with [dk x dv], and what it makes of a state [dk x dk]
 };
 
 __device__ __forceinline__ int delta_first(const DeltaSeqArgs &a, int s) { return min(max(a.off[s], 0), a.L); }
@@ -302,7 +305,8 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaSeqArgs a)
             const float ek = parts_scale(s_mk[lane], ik), eq = parts_scale(s_mq[lane], iq), e = expf((float)s_c[lane]);
             v[lane] = e * s_rk[lane] * ek;
             v[DELTA_C + lane] = e * s_rq[lane] * eq;
-            v[2 * DELTA_C + lane] = expf((float)(s_c[DELTA_C - 1] - s_c[lane])) * s_rk[lane] * ek;
+            // (a key of zeros: no power of two of its own, so its update, which counts for nothing, must not be what a column's scale goes by)
+            v[2 * DELTA_C + lane] = ik > 0.0f ? expf((float)(s_c[DELTA_C - 1] - s_c[lane])) * s_rk[lane] * ek : 0.0f;
             v[3 * DELTA_C + lane] = ik;
             v[4 * DELTA_C + lane] = iq;
             v[5 * DELTA_C + lane] = expf((float)s_c[DELTA_C - 1]);
@@ -397,7 +401,8 @@ __device__ __forceinline__ v4f fetch4(__amdgpu_buffer_rsrc_t rsrc, unsigned at, 
 // that what a column loses goes by its own size.  The two small products, of 32 x 32 with T and M, are fp32 ones.  Four waves multiply the
 // keys and make the updates, four multiply the queries and make the results; all convert, and all keep an eighth of the state.  The next chunk's rows are on
 // their way while one is worked on, each number in one thread's load and from there in LDS: loads of what several lanes need each cost the most here.
-template <int DKT, bool VEC>         // VEC: rows of queries, keys, values and results in whole 16-byte pieces
+// SEGMENTS: in place of a sequence a block carries a part of it (below).  MOVES: nothing is read, no results.
+template <int DKT, bool VEC, bool SEGMENTS, bool MOVES>      // VEC: rows of queries, keys, values and results in whole 16-byte pieces
 __global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(DeltaSeqArgs a)
 {
     constexpr int DKP = 32 * DKT, PH = DKP + 8, PT = DELTA_C + 4, OWN = DKT / 2;      // of a thread: pieces of four numbers of the keys, of the queries and of the state
@@ -409,19 +414,54 @@ __global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(Delt
     static_assert(2 * 32 * PT * sizeof(float) <= 2 * 32 * PH * sizeof(_Float16), "the updates fit where the state's parts were: they have been read by then");
     const q8_delta_inputs &p = a.in;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, gq = lane >> 4, mt = wave & 1, nt = (wave >> 1) & 1, queries = wave >> 2;
-    const int head = blockIdx.x % p.hv, s = blockIdx.x / p.hv, kh = head / (p.hv / p.hk), v0 = blockIdx.y * 32, lc = 16 * nt + i, col = v0 + lc;
-    const int first = __builtin_amdgcn_readfirstlane(delta_first(a, s)), length = __builtin_amdgcn_readfirstlane(delta_length(a, s, first));
-    const bool live = col < p.dv;
+    const int head = blockIdx.x % p.hv, place = blockIdx.x / p.hv, kh = head / (p.hv / p.hk), lc = 16 * nt + i;
+    int s = place, segment = 0, first, length;
+    bool last = true;
+    if constexpr (SEGMENTS) {
+        int *s_at = (int *)s_all;
+        if (tid == 0) s_at[0] = -1;
+        __syncthreads();
+        for (int x = tid; x < a.S; x += 512) {                              // the sequence that has this place, if any (one without tokens has one)
+            const int f = delta_first(a, x), g = place - (f / (DELTA_C * a.seg) + x);
+            if (g >= 0 && g <= max(delta_length(a, x, f) - 1, 0) / (DELTA_C * a.seg)) s_at[0] = x;
+        }
+        __syncthreads();
+        s = __builtin_amdgcn_readfirstlane(s_at[0]);
+        if (s < 0) return;
+        __syncthreads();
+        first = __builtin_amdgcn_readfirstlane(delta_first(a, s));
+        length = __builtin_amdgcn_readfirstlane(delta_length(a, s, first));
+        segment = place - (first / (DELTA_C * a.seg) + s);
+        last = segment >= max(length - 1, 0) / (DELTA_C * a.seg);
+        first += segment * DELTA_C * a.seg;
+        length = min(length - segment * DELTA_C * a.seg, DELTA_C * a.seg);
+    } else {
+        first = __builtin_amdgcn_readfirstlane(delta_first(a, s));
+        length = __builtin_amdgcn_readfirstlane(delta_length(a, s, first));
+    }
+    // MOVES: columns of the state from zeros (a sequence's first segment: from its state), then those of what the segment makes of any state, from the
+    // unit vectors and without values; neither is asked of a sequence's last segment
+    const int slices = (p.dv + 31) / 32;
+    const bool unit = MOVES && (int)blockIdx.y >= slices;
+    if (MOVES && (last || (unit && segment == 0))) return;
+    const int v0 = 32 * ((int)blockIdx.y - (unit ? slices : 0)), col = v0 + lc, dv = unit ? p.dk : p.dv;
+    const bool live = col < dv;
     const int tile0 = 2 * queries + mt, r0 = 16 * mt + 4 * gq;
     // rows 16 (4 t + tile0) + 4 gq + e of column `col` of the state
     v4f st[OWN];
-    const size_t own = ((size_t)s * p.hv + head) * p.dk * p.dv, bytes = 4 * (size_t)p.dk * p.dv;
+    const size_t bytes = 4 * (size_t)p.dk * dv, mine = ((size_t)s * p.hv + head) * p.dk * p.dv, there = ((size_t)place * p.hv + head) * p.dk * dv;
     auto state_at = [&](int t, int e) {
         const int row = 16 * (4 * t + tile0) + 4 * gq + e;
-        return (int)(live && row < p.dk ? 4u * ((unsigned)row * (unsigned)p.dv + col) : Q8_OOB);
+        return (int)(live && row < p.dk ? 4u * ((unsigned)row * (unsigned)dv + col) : Q8_OOB);
     };
-    {
-        const __amdgpu_buffer_rsrc_t rs = q8_rsrc(a.state + own, a.state ? bytes : 0);      // (none: zeros)
+    if (unit) {
+#pragma unroll
+        for (int t = 0; t < OWN; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) st[t][e] = 16 * (4 * t + tile0) + 4 * gq + e == col ? 1.0f : 0.0f;
+    } else {                                                                // (a later segment's state is where the one before ends; none: zeros)
+        const float *from = segment == 0 ? a.state + mine : a.ends + there - (size_t)p.hv * p.dk * p.dv;
+        const __amdgpu_buffer_rsrc_t rs = q8_rsrc(from, (segment == 0 ? a.state != nullptr : !MOVES) ? bytes : 0);
 #pragma unroll
         for (int t = 0; t < OWN; ++t)
 #pragma unroll
@@ -436,7 +476,7 @@ __global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(Delt
         ok[x] = k < p.dk ? 4u * ((unsigned)r * (unsigned)p.ldk + k) : Q8_OOB;
         oq[x] = k < p.dk ? 4u * ((unsigned)r * (unsigned)p.ldq + k) : Q8_OOB;
     }
-    const int vr = (tid & 255) >> 3, vc = 4 * (tid & 7), vleft = tid < 256 ? p.dv - v0 - vc : 0;
+    const int vr = (tid & 255) >> 3, vc = 4 * (tid & 7), vleft = tid < 256 && !unit ? p.dv - v0 - vc : 0;
     const unsigned ov = vleft > 0 ? 4u * ((unsigned)vr * (unsigned)p.ldv + v0 + vc) : Q8_OOB, oo = vleft > 0 ? 4u * ((unsigned)vr * (unsigned)a.ldo + v0 + vc) : Q8_OOB;
     const unsigned oe = tid < 48 ? 4u * (2 * DELTA_MATRIX + 4 * tid) : Q8_OOB;
     v4f pk[OWN], pq[OWN], pm, pv, pe;
@@ -453,7 +493,7 @@ __global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(Delt
         for (int x = 0; x < OWN; ++x) {
             const int left = p.dk - 4 * ((tid + 512 * x) % (DKP / 4));
             pk[x] = fetch4<VEC>(rk, ok[x], left);
-            pq[x] = fetch4<VEC>(rq, oq[x], left);
+            if constexpr (!MOVES) pq[x] = fetch4<VEC>(rq, oq[x], left);
         }
         pm = fetch4<true>(rr, 16u * tid, 4);
         pv = fetch4<VEC>(rv, ov, vleft);
@@ -506,12 +546,14 @@ __global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(Delt
             parts4(pk[x][0], pk[x][1], pk[x][2], pk[x][3], s_vec[3 * DELTA_C + r], hi, lo);
             *(uint2 *)(sK + to) = hi;
             *(uint2 *)(sK + DELTA_C * PH + to) = lo;
-            parts4(pq[x][0], pq[x][1], pq[x][2], pq[x][3], s_vec[4 * DELTA_C + r], hi, lo);
-            *(uint2 *)(sQ + to) = hi;
-            *(uint2 *)(sQ + DELTA_C * PH + to) = lo;
+            if constexpr (!MOVES) {
+                parts4(pq[x][0], pq[x][1], pq[x][2], pq[x][3], s_vec[4 * DELTA_C + r], hi, lo);
+                *(uint2 *)(sQ + to) = hi;
+                *(uint2 *)(sQ + DELTA_C * PH + to) = lo;
+            }
         }
         *(v4f *)(sM + (tid >> 3) * PT + 4 * (tid & 7)) = pm;
-        if (t0 > 0 && tid < 256) results(t0 - DELTA_C);                     // (a thread's piece of the results, then of the values, in one place)
+        if (!MOVES && t0 > 0 && tid < 256) results(t0 - DELTA_C);                     // (a thread's piece of the results, then of the values, in one place)
         if (tid < 256) *(v4f *)(sV + vr * PT + vc) = pv;
         __syncthreads();
         if (t0 + DELTA_C < length) fetch(t0 + DELTA_C);
@@ -519,6 +561,7 @@ __global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(Delt
         const float keep = s_vec[5 * DELTA_C];
         v4f x0 = {0.0f, 0.0f, 0.0f, 0.0f}, x1 = x0, x2 = x0;                // keys or queries times the state
         const _Float16 *rows = (queries ? sQ : sK) + (16 * mt + i) * PH + 8 * gq, *columns = sS + lc * PH + 8 * gq;
+        if (!MOVES || !queries)
 #pragma unroll
         for (int t = 0; t < DKT; ++t) {
             const v8h xh = *(const v8h *)(rows + 32 * t), xl = *(const v8h *)(rows + DELTA_C * PH + 32 * t);
@@ -575,42 +618,150 @@ __global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(Delt
             for (int e = 0; e < 4; ++e) st[t][e] = fmaf(cw, d[e], keep * st[t][e]);
         }
         leave_state();
-        if (queries) {
+        if (!MOVES && queries) {
             const v4f o = small(sU, xs);
 #pragma unroll
             for (int e = 0; e < 4; ++e) sV[(r0 + e) * PT + lc] = o[e];
         }
         __syncthreads();
     }
-    if (length > 0 && tid < 256) results((length - 1) / DELTA_C * DELTA_C);
-    const __amdgpu_buffer_rsrc_t rs = q8_rsrc(a.state_out + own, a.state_out ? bytes : 0);
+    if (!MOVES && length > 0 && tid < 256) results((length - 1) / DELTA_C * DELTA_C);
+    float *to = MOVES ? (unit ? a.moves : a.ends) + there : a.state_out + mine;
+    const __amdgpu_buffer_rsrc_t rs = q8_rsrc(to, MOVES || (last && a.state_out) ? bytes : 0);
 #pragma unroll
     for (int t = 0; t < OWN; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e) __builtin_amdgcn_raw_buffer_store_b32(__float_as_int(st[t][e]), rs, state_at(t, e), 0, 0);
 }
 
-template <int DKT> static q8_status launch_sequence(q8_ctx *ctx, const DeltaSeqArgs &a)
+// Few long sequences leave most of the device idle: a sequence's chunks come one after the other.  A segment of them makes F S + B of a state S, as the
+// rule is linear in it: B is what it makes of zeros, F what it makes of the unit vectors without values.  These come from all segments side by side
+// (MOVES), this kernel goes from segment to segment, ends[g] = F[g] ends[g - 1] + ends[g], and the results from all segments side by side again, each from
+// the state that the one before ends with.  About 2.7 times the work.  A block per sequence, head and 32 columns; products in fp32.
+template <int DKT, bool VEC>         // VEC: dk in whole 16-byte pieces
+__global__ __launch_bounds__(512) void delta_join_kernel(DeltaSeqArgs a)
 {
-    static Q8OncePerDevice once[2];
-    constexpr size_t smem = 3 * 2 * 32 * (32 * DKT + 8) * sizeof(_Float16) + (4 * 32 * (DELTA_C + 4) + 6 * DELTA_C + 192) * sizeof(float);
-    void (*const carry)(DeltaSeqArgs) = a.vec ? delta_carry_kernel<DKT, true> : delta_carry_kernel<DKT, false>;
-    q8_status st = q8i_lds(ctx, once[a.vec], (const void *)carry, smem, "delta sequence");
-    if (st) return st;
-    if (a.L > 0) {
-        hipLaunchKernelGGL(delta_chunk_kernel<DKT>, dim3((unsigned)((size_t)a.slots * a.in.hv)), dim3(256), 0, ctx->stream, a);
-        st = q8i_launch_check(ctx, "delta sequence");
-        if (st) return st;
+    constexpr int DKP = 32 * DKT, P = DKP + 4, OWN = DKT / 2;
+    __shared__ __align__(16) float sS[32 * P];                              // [column][row of the state]
+    const q8_delta_inputs &p = a.in;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, gq = lane >> 4, nt = wave & 1, tile0 = wave >> 1;
+    const int head = blockIdx.x % p.hv, s = blockIdx.x / p.hv, lc = 16 * nt + i, col = blockIdx.y * 32 + lc;
+    const int first = __builtin_amdgcn_readfirstlane(delta_first(a, s)), length = __builtin_amdgcn_readfirstlane(delta_length(a, s, first));
+    const int n = (length + DELTA_C * a.seg - 1) / (DELTA_C * a.seg), place = first / (DELTA_C * a.seg) + s;
+    if (n < 3) return;
+    const size_t size = (size_t)p.dk * p.dv, square = (size_t)p.dk * p.dk;
+    auto at = [&](int t, int e) {
+        const int row = 16 * (4 * t + tile0) + 4 * gq + e;
+        return (int)(col < p.dv && row < p.dk ? 4u * ((unsigned)row * (unsigned)p.dv + col) : Q8_OOB);
+    };
+    v4f st[OWN], b[OWN], f[OWN][2 * DKT];
+    auto fetch = [&](int g) {
+        const __amdgpu_buffer_rsrc_t rb = q8_rsrc(a.ends + ((size_t)(place + g) * p.hv + head) * size, 4 * size);
+        const __amdgpu_buffer_rsrc_t rf = q8_rsrc(a.moves + ((size_t)(place + g) * p.hv + head) * square, g > 0 ? 4 * square : 0);
+#pragma unroll
+        for (int t = 0; t < OWN; ++t) {
+            const int row = 16 * (4 * t + tile0) + i;
+#pragma unroll
+            for (int k = 0; k < 2 * DKT; ++k) {
+                const int c = 16 * k + 4 * gq;
+                f[t][k] = fetch4<VEC>(rf, row < p.dk && c < p.dk ? 4u * (unsigned)(row * p.dk + c) : Q8_OOB, row < p.dk ? p.dk - c : 0);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) b[t][e] = __int_as_float(__builtin_amdgcn_raw_buffer_load_b32(rb, at(t, e), 0, 0));
+        }
+    };
+    fetch(0);
+    for (int g = 0; g < n - 1; ++g) {                                       // (the last segment's end is nobody's start)
+        if (g == 0) {
+#pragma unroll
+            for (int t = 0; t < OWN; ++t) st[t] = b[t];
+        } else {
+#pragma unroll
+            for (int t = 0; t < OWN; ++t) {
+                v4f x = b[t], y = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int k = 0; k < 2 * DKT; ++k) {
+                    const v4f z = *(const v4f *)(sS + lc * P + 16 * k + 4 * gq);
+#pragma unroll
+                    for (int e = 0; e < 4; e += 2) {
+                        x = __builtin_amdgcn_mfma_f32_16x16x4f32(f[t][k][e], z[e], x, 0, 0, 0);
+                        y = __builtin_amdgcn_mfma_f32_16x16x4f32(f[t][k][e + 1], z[e + 1], y, 0, 0, 0);
+                    }
+                }
+                st[t] = x + y;
+            }
+            const __amdgpu_buffer_rsrc_t rb = q8_rsrc(a.ends + ((size_t)(place + g) * p.hv + head) * size, 4 * size);
+#pragma unroll
+            for (int t = 0; t < OWN; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) __builtin_amdgcn_raw_buffer_store_b32(__float_as_int(st[t][e]), rb, at(t, e), 0, 0);
+        }
+        if (g + 2 >= n) break;
+        fetch(g + 1);
+        __syncthreads();                                                    // the state before has been read
+#pragma unroll
+        for (int t = 0; t < OWN; ++t) *(v4f *)(sS + lc * P + 16 * (4 * t + tile0) + 4 * gq) = st[t];
+        __syncthreads();
     }
-    hipLaunchKernelGGL(carry, dim3((unsigned)((size_t)a.S * a.in.hv), (a.in.dv + 31) / 32), dim3(512), smem, ctx->stream, a);
-    return q8i_launch_check(ctx, "delta sequence");
 }
 
-size_t q8i_delta_room(int L, int S, int hv) { return ((size_t)L / DELTA_C + S) * hv * DELTA_ROOM * sizeof(float); }
+// Chunks of a segment, 0 where sequences are carried whole (us; chunks one after the other cost 2.6 each, blocks side by side 3.75 for 512 at a time):
+// few blocks, long sequences, and segments that give each compute unit two blocks.
+static int delta_segment(int L, int S, int hv, int dv)
+{
+    const long long heads = (long long)hv * ((dv + 31) / 32), chunks = L / DELTA_C;
+    if (heads * S > 96 || chunks < 24ll * S) return 0;
+    const long long parts = 512 / heads, seg = (chunks + parts - 1) / parts;
+    return 2 * std::max(seg, 4ll) * S > chunks ? 0 : (int)std::max(seg, 4ll);
+}
+
+template <int DKT> static q8_status launch_sequence(q8_ctx *ctx, const DeltaSeqArgs &a)
+{
+    static Q8OncePerDevice once[6];
+    constexpr size_t smem = 3 * 2 * 32 * (32 * DKT + 8) * sizeof(_Float16) + (4 * 32 * (DELTA_C + 4) + 6 * DELTA_C + 192) * sizeof(float);
+    auto carry = [&](void (*kernel)(DeltaSeqArgs), int form, int rows, int slices) {
+        const q8_status st = q8i_lds(ctx, once[form], (const void *)kernel, smem, "delta sequence");
+        if (st) return st;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)((size_t)rows * a.in.hv), slices), dim3(512), smem, ctx->stream, a);
+        return q8i_launch_check(ctx, "delta sequence");
+    };
+    const int slices = (a.in.dv + 31) / 32;
+    q8_status st;
+    if (a.L > 0) {
+        hipLaunchKernelGGL(delta_chunk_kernel<DKT>, dim3((unsigned)((size_t)a.slots * a.in.hv)), dim3(256), 0, ctx->stream, a);
+        if ((st = q8i_launch_check(ctx, "delta sequence"))) return st;
+    }
+    if (!a.seg) return a.vec ? carry(delta_carry_kernel<DKT, true, false, false>, 0, a.S, slices) : carry(delta_carry_kernel<DKT, false, false, false>, 1, a.S, slices);
+    const int more = (a.in.dk + 31) / 32;
+    st = a.vec ? carry(delta_carry_kernel<DKT, true, true, true>, 2, a.segs, slices + more) : carry(delta_carry_kernel<DKT, false, true, true>, 3, a.segs, slices + more);
+    if (st) return st;
+    void (*const join)(DeltaSeqArgs) = a.in.dk % 4 == 0 ? delta_join_kernel<DKT, true> : delta_join_kernel<DKT, false>;
+    hipLaunchKernelGGL(join, dim3((unsigned)((size_t)a.S * a.in.hv), slices), dim3(512), 0, ctx->stream, a);
+    if ((st = q8i_launch_check(ctx, "delta sequence"))) return st;
+    return a.vec ? carry(delta_carry_kernel<DKT, true, true, false>, 4, a.segs, slices) : carry(delta_carry_kernel<DKT, false, true, false>, 5, a.segs, slices);
+}
+
+static size_t delta_chunk_room(int L, int S, int hv) { return ((size_t)L / DELTA_C + S) * hv * DELTA_ROOM; }
+
+// floats of the segments' ends and moves
+static size_t delta_segment_room(int segs, int hv, int dk, int dv) { return (size_t)segs * hv * dk * ((size_t)dv + dk); }
+
+static int delta_segments(int L, int S, int seg) { return L / (DELTA_C * seg) + S; }
+
+size_t q8i_delta_room(int L, int S, int hv, int dk, int dv)
+{
+    const int seg = delta_segment(L, S, hv, dv);
+    return (delta_chunk_room(L, S, hv) + (seg ? delta_segment_room(delta_segments(L, S, seg), hv, dk, dv) : 0)) * sizeof(float);
+}
 
 q8_status q8i_delta_sequence(q8_ctx *ctx, const q8_delta_inputs *in, int L, const int *off, int S, const float *state, float *state_out, float *out, int ldo, float *room)
 {
-    DeltaSeqArgs a = {*in, off, S, L, L / DELTA_C + S, room, state, state_out, out, ldo, 0, 0};
+    DeltaSeqArgs a = {*in, off, S, L, L / DELTA_C + S, room, state, state_out, out, ldo, 0, 0, delta_segment(L, S, in->hv, in->dv), 0, nullptr, nullptr};
+    if (a.seg) {
+        a.segs = delta_segments(L, S, a.seg);
+        a.ends = room + delta_chunk_room(L, S, in->hv);
+        a.moves = a.ends + (size_t)a.segs * in->hv * in->dk * in->dv;
+    }
     a.vec_qk = in->dk % 4 == 0 && whole16(in->q, in->ldq) && whole16(in->k, in->ldk);
     a.vec = a.vec_qk && in->dv % 4 == 0 && whole16(in->v, in->ldv) && whole16(out, ldo);
     if (L <= 1) a.in.ldq = a.in.ldk = in->hk * in->dk, a.in.ldv = a.ldo = in->hv * in->dv;      // (a pitch that nothing uses, but bounds are formed with)

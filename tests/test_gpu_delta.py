@@ -350,3 +350,48 @@ def test_a_decoder_of_them(q):
         assert all(tok[j] in best[j] for j in range(beam))
         state, x, x64 = r["state"], d["y_emb"], np.asarray(emb[tok], np.float64)
         parent = rng.integers(0, beam, beam).astype(np.int32)
+
+
+# ---- few long sequences: in segments ----
+
+@pytest.mark.parametrize("lengths", [[2048], [1537], [1000, 3, 0, 2300], [0, 3500]], ids=str)
+@pytest.mark.parametrize("hk,hv,dk,dv,edges", [(1, 1, 32, 32, False), (1, 2, 33, 20, True), (2, 2, 128, 40, False), (1, 1, 130, 64, True)])
+def test_long_sequences(q, lengths, hk, hv, dk, dv, edges):
+    rng = np.random.default_rng(sum(lengths) + dk)
+    front = 5
+    off = [front] + [front + int(c) for c in np.cumsum(lengths)]
+    L, S = off[-1] + 3, len(lengths)
+    ctx = q.Context(workspace_bytes=q.q8_delta_bytes(L, S, hv, dk, dv))
+    assert q.q8_delta_bytes(L, S, hv, dk, dv) - q.q8_delta_bytes(L, S, hv, dk, 1) >= 4 * hv * dk * (dv - 1)      # (there is room for segments' states)
+    x = _inputs(rng, L, hk, hv, dk, dv)
+    x["g"] *= np.float32(0.01)                          # states that last over many segments
+    if edges:
+        _edges(rng, x)
+        x["g"][700:1400] = 0.0
+    st = rng.standard_normal((S, hv, dk, dv)).astype(np.float32)
+    out = torch.full((L, hv, dv), 5.0, device=ctx.device)
+    state = ctx.f32(st)
+    call = lambda: q.q8_delta_sequence(ctx, **_dev(ctx, x), sent_off=torch.tensor(off, dtype=torch.int32, device=ctx.device), scale=0.3, state=state, out=out)
+    got = call()
+    first = np_(out).copy(), np_(got["state"]).copy()
+    assert (first[0][:front] == 5.0).all() and (first[0][off[-1]:] == 5.0).all()
+    again = call()
+    assert (np_(out) == first[0]).all() and (np_(again["state"]) == first[1]).all()
+    out[:front] = 0.0
+    out[off[-1]:] = 0.0
+    want, bound = ref.sequence(**x, off=off, scale=0.3, state=st), ref.sequence_bound(**x, off=off, scale=0.3, state=st)
+    # a segment's matrix is as far off as a state, in each of its dk columns, and multiplies a state once more
+    _close(got, want, (bound[0] * (1 + np.sqrt(dk)), bound[1] * (1 + np.sqrt(dk))), dk)
+    q.q8_delta_sequence(ctx, **_dev(ctx, x), sent_off=torch.tensor(off, dtype=torch.int32, device=ctx.device), scale=0.3, state=state, state_out=state, out=out)
+    assert (np_(state) == first[1]).all()
+
+
+def test_a_key_of_zeros_costs_the_others_nothing(q, ctx):
+    """Between keys as they are met: results as exact as without it."""
+    rng = np.random.default_rng(20)
+    x = _inputs(rng, 320, 1, 2, 64, 64)
+    x["k"][5::32] = 0.0
+    x["v"][5::32] *= np.float32(100)
+    off = [0, 320]
+    got = q.q8_delta_sequence(ctx, **_dev(ctx, x), sent_off=torch.tensor(off, dtype=torch.int32, device=ctx.device))
+    _close(got, ref.sequence(**x, off=off), ref.sequence_bound(**x, off=off), 64)

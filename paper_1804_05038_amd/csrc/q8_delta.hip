@@ -368,7 +368,7 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaSeqArgs a)
     }
 }
 
-// Four tokens (rows of PH halfs from `at` on) of sixteen numbers, transposed: a lane's number of four tokens.
+// Sixteen lanes that point at four numbers each, sixteen of four rows (row l / 4 in lane l), transposed: a lane's number of the four rows.
 __device__ __forceinline__ v4h read_transposed(const _Float16 *at)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -380,6 +380,17 @@ __device__ __forceinline__ v4h read_transposed(const _Float16 *at)
 }
 
 __device__ __forceinline__ v8h both(v4h a, v4h b) { return (v8h){a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}; }
+
+// Where number k of a row of fp16 parts lies: a row's pieces of 16 bytes are exchanged by its number, so that sixteen rows' same piece, and four rows' same
+// two pieces, lie on different banks.
+template <int DKT>
+__device__ __forceinline__ int delta_place(int row, int k)
+{
+    return row * 32 * DKT + 8 * ((k >> 3) ^ (DKT >= 4 ? row & 15 : (row >> 1) & 7)) + (k & 7);
+}
+
+// Bytes of LDS for the state's parts, and for the updates later.
+constexpr size_t delta_state_bytes(int dkt) { return dkt >= 4 ? (size_t)2 * 32 * 32 * dkt * 2 : (size_t)2 * 32 * (DELTA_C + 4) * 4; }
 
 // Four numbers at `at`, or zeros past the end.  Loads under no condition: the compiler waits for everything in flight where a load stands in a branch.
 // In single words the row's end is looked at for each (`left` numbers are the row's).
@@ -405,13 +416,12 @@ __device__ __forceinline__ v4f fetch4(__amdgpu_buffer_rsrc_t rsrc, unsigned at, 
 template <int DKT, bool VEC, bool SEGMENTS, bool MOVES>      // VEC: rows of queries, keys, values and results in whole 16-byte pieces
 __global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(DeltaSeqArgs a)
 {
-    constexpr int DKP = 32 * DKT, PH = DKP + 8, PT = DELTA_C + 4, OWN = DKT / 2;      // of a thread: pieces of four numbers of the keys, of the queries and of the state
+    constexpr int DKP = 32 * DKT, PART = DELTA_C * DKP, PT = DELTA_C + 4, OWN = DKT / 2;      // of a thread: pieces of four numbers of the keys, of the queries and of the state
     static_assert(DKT % 2 == 0, "eight waves share the state's tiles");
     extern __shared__ __align__(16) uint8_t s_all[];
-    _Float16 *sK = (_Float16 *)s_all, *sQ = sK + 2 * DELTA_C * PH, *sS = sQ + 2 * DELTA_C * PH;      // [hi, lo][token or column][row of the state]
-    float *sR = (float *)(sS + 2 * 32 * PH), *sM = sR + 32 * PT, *sV = sM + 2 * 32 * PT, *s_vec = sV + 32 * PT, *s_top = s_vec + 6 * DELTA_C, *s_wtop = s_top + 128;
-    float *sU = (float *)sS, *sW = sU + 32 * PT;                            // sR, sU, sW [column][token], sM [T, M][token][token], sV values and results [token][column]
-    static_assert(2 * 32 * PT * sizeof(float) <= 2 * 32 * PH * sizeof(_Float16), "the updates fit where the state's parts were: they have been read by then");
+    _Float16 *sK = (_Float16 *)s_all, *sQ = sK + 2 * PART, *sS = sQ + 2 * PART;      // [hi, lo][token or column][row of the state]
+    float *sR = (float *)((uint8_t *)sS + delta_state_bytes(DKT)), *sM = sR + 32 * PT, *sV = sM + 2 * 32 * PT, *s_vec = sV + 32 * PT, *s_top = s_vec + 6 * DELTA_C, *s_wtop = s_top + 128;
+    float *sU = (float *)sS, *sW = sU + 32 * PT;                            // (the state's parts have been read by then) sR, sU, sW [column][token], sM [T, M][token][token], sV values and results [token][column]
     const q8_delta_inputs &p = a.in;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, gq = lane >> 4, mt = wave & 1, nt = (wave >> 1) & 1, queries = wave >> 2;
     const int head = blockIdx.x % p.hv, place = blockIdx.x / p.hv, kh = head / (p.hv / p.hk), lc = 16 * nt + i;
@@ -535,21 +545,21 @@ __global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(Delt
         for (int t = 0; t < OWN; ++t) {
             uint2 hi, lo;
             parts4(st[t][0], st[t][1], st[t][2], st[t][3], inv, hi, lo);
-            _Float16 *to = sS + lc * PH + 16 * (4 * t + tile0) + 4 * gq;
+            _Float16 *to = sS + delta_place<DKT>(lc, 16 * (4 * t + tile0) + 4 * gq);
             *(uint2 *)to = hi;
-            *(uint2 *)(to + 32 * PH) = lo;
+            *(uint2 *)(to + PART) = lo;
         }
 #pragma unroll
         for (int x = 0; x < OWN; ++x) {
-            const int y = tid + 512 * x, r = y / (DKP / 4), to = r * PH + 4 * (y % (DKP / 4));
+            const int y = tid + 512 * x, r = y / (DKP / 4), to = delta_place<DKT>(r, 4 * (y % (DKP / 4)));
             uint2 hi, lo;
             parts4(pk[x][0], pk[x][1], pk[x][2], pk[x][3], s_vec[3 * DELTA_C + r], hi, lo);
             *(uint2 *)(sK + to) = hi;
-            *(uint2 *)(sK + DELTA_C * PH + to) = lo;
+            *(uint2 *)(sK + PART + to) = lo;
             if constexpr (!MOVES) {
                 parts4(pq[x][0], pq[x][1], pq[x][2], pq[x][3], s_vec[4 * DELTA_C + r], hi, lo);
                 *(uint2 *)(sQ + to) = hi;
-                *(uint2 *)(sQ + DELTA_C * PH + to) = lo;
+                *(uint2 *)(sQ + PART + to) = lo;
             }
         }
         *(v4f *)(sM + (tid >> 3) * PT + 4 * (tid & 7)) = pm;
@@ -560,12 +570,12 @@ __global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(Delt
         const v4f eb = *(const v4f *)(s_vec + queries * DELTA_C + r0), el = *(const v4f *)(s_vec + 2 * DELTA_C + r0);
         const float keep = s_vec[5 * DELTA_C];
         v4f x0 = {0.0f, 0.0f, 0.0f, 0.0f}, x1 = x0, x2 = x0;                // keys or queries times the state
-        const _Float16 *rows = (queries ? sQ : sK) + (16 * mt + i) * PH + 8 * gq, *columns = sS + lc * PH + 8 * gq;
+        const _Float16 *rows = queries ? sQ : sK;
         if (!MOVES || !queries)
 #pragma unroll
         for (int t = 0; t < DKT; ++t) {
-            const v8h xh = *(const v8h *)(rows + 32 * t), xl = *(const v8h *)(rows + DELTA_C * PH + 32 * t);
-            const v8h sh = *(const v8h *)(columns + 32 * t), sl = *(const v8h *)(columns + 32 * PH + 32 * t);
+            const _Float16 *x = rows + delta_place<DKT>(16 * mt + i, 32 * t + 8 * gq), *y = sS + delta_place<DKT>(lc, 32 * t + 8 * gq);
+            const v8h xh = *(const v8h *)x, xl = *(const v8h *)(x + PART), sh = *(const v8h *)y, sl = *(const v8h *)(y + PART);
             x0 = __builtin_amdgcn_mfma_f32_16x16x32_f16(xh, sh, x0, 0, 0, 0);
             x1 = __builtin_amdgcn_mfma_f32_16x16x32_f16(xh, sl, x1, 0, 0, 0);
             x2 = __builtin_amdgcn_mfma_f32_16x16x32_f16(xl, sh, x2, 0, 0, 0);
@@ -599,17 +609,18 @@ __global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(Delt
             leave_top(fmaxf(fmaxf(fabsf(w[0]), fabsf(w[1])), fmaxf(fabsf(w[2]), fabsf(w[3]))), s_wtop + 32 * mt);
         }
         __syncthreads();
-        // tokens 8 gq + (0 .. 7) of column i
+        // tokens 8 gq + (0, 2, 4, 6, 1, 3, 5, 7) of column i: four rows of the keys that are read together lie two apart, on different banks
         const float cw = parts_scale(fmaxf(s_wtop[lc], s_wtop[32 + lc]), inv);
         const v4f z0 = *(const v4f *)(sW + lc * PT + 8 * gq), z1 = *(const v4f *)(sW + lc * PT + 8 * gq + 4);
         union { uint2 u[2]; v8h h; } wh, wl;
-        parts4(z0[0], z0[1], z0[2], z0[3], inv, wh.u[0], wl.u[0]);
-        parts4(z1[0], z1[1], z1[2], z1[3], inv, wh.u[1], wl.u[1]);
+        parts4(z0[0], z0[2], z1[0], z1[2], inv, wh.u[0], wl.u[0]);
+        parts4(z0[1], z0[3], z1[1], z1[3], inv, wh.u[1], wl.u[1]);
 #pragma unroll
         for (int t = 0; t < OWN; ++t) {
-            const _Float16 *k = sK + (8 * gq + (i >> 2)) * PH + 16 * (4 * t + tile0) + 4 * (i & 3);
-            const v8h kh_ = both(read_transposed(k), read_transposed(k + 4 * PH));
-            const v8h kl = both(read_transposed(k + DELTA_C * PH), read_transposed(k + (DELTA_C + 4) * PH));
+            const int row = 8 * gq + 2 * (i >> 2), c = 16 * (4 * t + tile0) + 4 * (i & 3);
+            const _Float16 *k0 = sK + delta_place<DKT>(row, c), *k1 = sK + delta_place<DKT>(row + 1, c);
+            const v8h kh_ = both(read_transposed(k0), read_transposed(k1));
+            const v8h kl = both(read_transposed(k0 + PART), read_transposed(k1 + PART));
             v4f d = {0.0f, 0.0f, 0.0f, 0.0f};
             d = __builtin_amdgcn_mfma_f32_16x16x32_f16(kl, wh.h, d, 0, 0, 0);
             d = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh_, wl.h, d, 0, 0, 0);
@@ -718,7 +729,7 @@ static int delta_segment(int L, int S, int hv, int dv)
 template <int DKT> static q8_status launch_sequence(q8_ctx *ctx, const DeltaSeqArgs &a)
 {
     static Q8OncePerDevice once[6];
-    constexpr size_t smem = 3 * 2 * 32 * (32 * DKT + 8) * sizeof(_Float16) + (4 * 32 * (DELTA_C + 4) + 6 * DELTA_C + 192) * sizeof(float);
+    constexpr size_t smem = 2 * 2 * 32 * 32 * DKT * sizeof(_Float16) + delta_state_bytes(DKT) + (4 * 32 * (DELTA_C + 4) + 6 * DELTA_C + 192) * sizeof(float);
     auto carry = [&](void (*kernel)(DeltaSeqArgs), int form, int rows, int slices) {
         const q8_status st = q8i_lds(ctx, once[form], (const void *)kernel, smem, "delta sequence");
         if (st) return st;

@@ -15,14 +15,22 @@ __device__ __forceinline__ float parts_scale(float m, float &inv)
     return __uint_as_float(e << 23);
 }
 
-// Four values times inv as hi and lo parts (two conversions an instruction, the rest in one that takes an fp16 number as it is).
+// x minus the low or high fp16 number of a pair, in one instruction that takes it as it is (the compiler converts first).
+__device__ __forceinline__ float minus_half(float x, unsigned pair, bool high)
+{
+    float r;
+    if (high) asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(r) : "v"(pair), "v"(x));
+    else asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(r) : "v"(pair), "v"(x));
+    return r;
+}
+
+// Four values times inv as hi and lo parts (two conversions an instruction).
 __device__ __forceinline__ void parts4(float x, float y, float z, float w, float inv, uint2 &hi, uint2 &lo)
 {
     typedef float v2f __attribute__((ext_vector_type(2)));
     typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+    auto pair = [](float a, float b) { return __builtin_bit_cast(unsigned, __builtin_convertvector(((v2f){a, b}), v2h)); };
     const float v[4] = {x * inv, y * inv, z * inv, w * inv};
-    const v2h a = __builtin_convertvector(((v2f){v[0], v[1]}), v2h), b = __builtin_convertvector(((v2f){v[2], v[3]}), v2h);
-    const v2f c = {fmaf((float)a[0], -1.0f, v[0]), fmaf((float)a[1], -1.0f, v[1])}, d = {fmaf((float)b[0], -1.0f, v[2]), fmaf((float)b[1], -1.0f, v[3])};
-    hi = make_uint2(__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, b));
-    lo = make_uint2(__builtin_bit_cast(unsigned, __builtin_convertvector(c, v2h)), __builtin_bit_cast(unsigned, __builtin_convertvector(d, v2h)));
+    hi = make_uint2(pair(v[0], v[1]), pair(v[2], v[3]));
+    lo = make_uint2(pair(minus_half(v[0], hi.x, false), minus_half(v[1], hi.x, true)), pair(minus_half(v[2], hi.y, false), minus_half(v[3], hi.y, true)));
 }

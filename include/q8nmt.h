@@ -694,8 +694,8 @@ q8_status q8_delta_step(q8_ctx *ctx, const q8_delta_inputs *in, int n, const flo
 
 /* n_seq sequences laid end to end: sequence s has the tokens off[s] .. off[s + 1] - 1 (off: n_seq + 1 numbers on the device, ascending, within
  * [0, L]; one without tokens keeps its state).  out [L x ldo]: rows that belong to no sequence stay as they are.  state (NULL: zeros) and state_out (may be NULL; may be
- * state) [n_seq x hv x dk x dv].  L <= 2^24, n_seq <= 65536, and (L / 32 + n_seq) hv, n_seq hv < 2^24.  out overlaps no input.  Workspace: the context's must have
- * q8_delta_bytes(L, n_seq, hv, dk, dv) bytes. */
+ * state) [n_seq x hv x dk x dv].  0 <= L <= 2^24 (0: the tables may be NULL), n_seq <= 65536, and (L / 32 + n_seq) hv, n_seq hv < 2^24.  out overlaps no input.  Workspace: the context's must have
+ * q8_delta_bytes(L, n_seq, hv, dk, dv) bytes, which are enough for fewer tokens and sequences too. */
 size_t q8_delta_bytes(int L, int n_seq, int hv, int dk, int dv);
 q8_status q8_delta_sequence(q8_ctx *ctx, const q8_delta_inputs *in, int L, const int32_t *off, int n_seq, const float *state, float *state_out,
                             float *out, int ldo);

@@ -2016,7 +2016,7 @@ const int kDeltaMaxDim = 256, kDeltaMaxHeads = 1024, kDeltaMaxL = 1 << 24, kDelt
 
 q8_status check_delta(q8_ctx *ctx, const q8_delta_inputs *in, int rows, const float *out, int ldo)
 {
-    if (!in || !in->q || !in->k || !in->v || !in->g || !in->beta || !out) return q8_fail(ctx, Q8_ERR_NULL, "delta rule: NULL argument");
+    if (!in || (rows > 0 && (!in->q || !in->k || !in->v || !in->g || !in->beta || !out))) return q8_fail(ctx, Q8_ERR_NULL, "delta rule: NULL argument");
     if (in->dk <= 0 || in->dk > kDeltaMaxDim || in->dv <= 0 || in->dv > kDeltaMaxDim) return q8_fail(ctx, Q8_ERR_SHAPE, "delta rule: heads of %d x %d", in->dk, in->dv);
     if (in->hk <= 0 || in->hv <= 0 || in->hv > kDeltaMaxHeads || in->hv % in->hk) return q8_fail(ctx, Q8_ERR_SHAPE, "delta rule: %d heads of keys, %d of values", in->hk, in->hv);
     if (rows > 1 && (in->ldq < in->hk * in->dk || in->ldk < in->hk * in->dk || in->ldv < in->hv * in->dv || in->ldg < in->hv || in->ldb < in->hv || ldo < in->hv * in->dv))
@@ -2050,7 +2050,7 @@ size_t q8_delta_bytes(int L, int n_seq, int hv, int dk, int dv)
 {
     if (L < 0 || L > kDeltaMaxL || n_seq <= 0 || n_seq > kDeltaMaxSeq || hv <= 0 || hv > kDeltaMaxHeads || dk <= 0 || dk > kDeltaMaxDim || dv <= 0 || dv > kDeltaMaxDim)
         return Q8_WS_HEADER;
-    return Q8_WS_HEADER + up256(q8i_delta_room(L, n_seq, hv, dk, dv));
+    return Q8_WS_HEADER + up256(q8i_delta_most_room(L, n_seq, hv, dk, dv));
 }
 
 q8_status q8_delta_sequence(q8_ctx *ctx, const q8_delta_inputs *in, int L, const int32_t *off, int n_seq, const float *state, float *state_out,

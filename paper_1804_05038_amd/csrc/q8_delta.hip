@@ -201,10 +201,25 @@ __device__ __forceinline__ int delta_first(const DeltaSeqArgs &a, int s) { retur
 // tokens of a sequence: offsets that are out of order or out of range give none or fewer
 __device__ __forceinline__ int delta_length(const DeltaSeqArgs &a, int s, int first) { return max(min(max(a.off[s + 1], 0), a.L) - first, 0); }
 
+// Four numbers at `at`, or zeros past the end.  Loads under no condition: the compiler waits for everything in flight where a load stands in a branch.
+// In single words the row's end is looked at for each (`left` numbers are the row's).
+template <bool VEC>
+__device__ __forceinline__ v4f fetch4(__amdgpu_buffer_rsrc_t rsrc, unsigned at, int left)
+{
+    v4f v;
+    if constexpr (VEC) {
+        v = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(rsrc, (int)at, 0, 0));
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = __int_as_float(__builtin_amdgcn_raw_buffer_load_b32(rsrc, (int)(left > e && at < Q8_OOB ? at + 4 * e : Q8_OOB), 0, 0));
+    }
+    return v;
+}
+
 // A block per chunk and head.  Three waves form a tile of 16 x 16 of both products each (the upper right one is zero) from rows that they load
 // as the matrix operation takes them, the fourth the sums of the decays; then (I + A)^-1 by substitution in blocks of 8, joined as
 // -T22 A21 T11 twice.  (Powers of A instead of substitution would cancel: 32 keys alike give binomials up to 3e8.)
-template <int DKT>                   // dk in units of 32, rounded up
+template <int DKT, bool VEC>         // dk in units of 32, rounded up; VEC: rows of queries and keys in whole 16-byte pieces
 __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaSeqArgs a)
 {
     constexpr int PT = DELTA_C + 4, PX = 20, STEPS = 2 * DKT < 8 ? 2 * DKT : 8;
@@ -233,17 +248,20 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaSeqArgs a)
     v4f akk = {0.0f, 0.0f, 0.0f, 0.0f}, aqk = akk;
     if (wave < 3) {
         const int r = 16 * mt + i, rn = 16 * nt + i;
-        const float *k = p.k + (tok + r) * p.ldk + (size_t)kh * p.dk + 4 * gq, *q = p.q + (tok + r) * p.ldq + (size_t)kh * p.dk + 4 * gq;
-        const float *kn = p.k + (tok + rn) * p.ldk + (size_t)kh * p.dk + 4 * gq;
+        // (rows past the chunk's end lie past the end of what is described; its rows are below 2^31 bytes: pitches are at most 2^22)
+        const __amdgpu_buffer_rsrc_t rk = q8_rsrc(p.k + tok * p.ldk + (size_t)kh * p.dk, 4 * ((size_t)(m - 1) * p.ldk + p.dk));
+        const __amdgpu_buffer_rsrc_t rq = q8_rsrc(p.q + tok * p.ldq + (size_t)kh * p.dk, 4 * ((size_t)(m - 1) * p.ldq + p.dk));
+        const unsigned k = 4u * ((unsigned)r * (unsigned)p.ldk + 4 * gq), q = 4u * ((unsigned)r * (unsigned)p.ldq + 4 * gq), kn = 4u * ((unsigned)rn * (unsigned)p.ldk + 4 * gq);
         float kk = 0.0f, qq = 0.0f, mk = 0.0f, mq = 0.0f;
         for (int t0 = 0; t0 < 2 * DKT; t0 += STEPS) {
             v4f x[STEPS], y[STEPS], z[STEPS];
 #pragma unroll
             for (int t = 0; t < STEPS; ++t) {
                 const int left = p.dk - 16 * (t0 + t) - 4 * gq;
-                x[t] = load4(k + 16 * (t0 + t), r < m ? left : 0, a.vec_qk);
-                y[t] = load4(q + 16 * (t0 + t), r < m ? left : 0, a.vec_qk);
-                z[t] = load4(kn + 16 * (t0 + t), wave == 2 && rn < m ? left : 0, a.vec_qk);
+                const unsigned at = 64u * (t0 + t);
+                x[t] = fetch4<VEC>(rk, left > 0 && r < m ? k + at : Q8_OOB, left);
+                y[t] = fetch4<VEC>(rq, left > 0 && r < m ? q + at : Q8_OOB, left);
+                z[t] = fetch4<VEC>(rk, left > 0 && wave == 2 && rn < m ? kn + at : Q8_OOB, left);
             }
 #pragma unroll
             for (int t = 0; t < STEPS; ++t)
@@ -391,21 +409,6 @@ __device__ __forceinline__ int delta_place(int row, int k)
 
 // Bytes of LDS for the state's parts, and for the updates later.
 constexpr size_t delta_state_bytes(int dkt) { return dkt >= 4 ? (size_t)2 * 32 * 32 * dkt * 2 : (size_t)2 * 32 * (DELTA_C + 4) * 4; }
-
-// Four numbers at `at`, or zeros past the end.  Loads under no condition: the compiler waits for everything in flight where a load stands in a branch.
-// In single words the row's end is looked at for each (`left` numbers are the row's).
-template <bool VEC>
-__device__ __forceinline__ v4f fetch4(__amdgpu_buffer_rsrc_t rsrc, unsigned at, int left)
-{
-    v4f v;
-    if constexpr (VEC) {
-        v = __builtin_bit_cast(v4f, __builtin_amdgcn_raw_buffer_load_b128(rsrc, (int)at, 0, 0));
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = __int_as_float(__builtin_amdgcn_raw_buffer_load_b32(rsrc, (int)(left > e ? at + 4 * e : Q8_OOB), 0, 0));
-    }
-    return v;
-}
 
 // A block per sequence, head and 32 columns of the state, which stays in registers as fp32.  Its products run on the fp16 matrix cores with both sides in two
 // parts (hi hi + hi lo + lo hi, within 2^-21): rows of keys and queries with a power of two each, columns of the state and of the updates too, so
@@ -718,10 +721,11 @@ __global__ __launch_bounds__(512) void delta_join_kernel(DeltaSeqArgs a)
 
 // Chunks of a segment, 0 where sequences are carried whole (us; chunks one after the other cost 2.6 each, blocks side by side 3.75 for 512 at a time):
 // few blocks, long sequences, and segments that give each compute unit two blocks.
+#define DELTA_FEW 96
 static int delta_segment(int L, int S, int hv, int dv)
 {
     const long long heads = (long long)hv * ((dv + 31) / 32), chunks = L / DELTA_C;
-    if (heads * S > 96 || chunks < 24ll * S) return 0;
+    if (heads * S > DELTA_FEW || chunks < 24ll * S) return 0;
     const long long parts = 512 / heads, seg = (chunks + parts - 1) / parts;
     return 2 * std::max(seg, 4ll) * S > chunks ? 0 : (int)std::max(seg, 4ll);
 }
@@ -739,7 +743,7 @@ template <int DKT> static q8_status launch_sequence(q8_ctx *ctx, const DeltaSeqA
     const int slices = (a.in.dv + 31) / 32;
     q8_status st;
     if (a.L > 0) {
-        hipLaunchKernelGGL(delta_chunk_kernel<DKT>, dim3((unsigned)((size_t)a.slots * a.in.hv)), dim3(256), 0, ctx->stream, a);
+        hipLaunchKernelGGL((a.vec_qk ? delta_chunk_kernel<DKT, true> : delta_chunk_kernel<DKT, false>), dim3((unsigned)((size_t)a.slots * a.in.hv)), dim3(256), 0, ctx->stream, a);
         if ((st = q8i_launch_check(ctx, "delta sequence"))) return st;
     }
     if (!a.seg) return a.vec ? carry(delta_carry_kernel<DKT, true, false, false>, 0, a.S, slices) : carry(delta_carry_kernel<DKT, false, false, false>, 1, a.S, slices);
@@ -763,6 +767,16 @@ size_t q8i_delta_room(int L, int S, int hv, int dk, int dv)
 {
     const int seg = delta_segment(L, S, hv, dv);
     return (delta_chunk_room(L, S, hv) + (seg ? delta_segment_room(delta_segments(L, S, seg), hv, dk, dv) : 0)) * sizeof(float);
+}
+
+// ... of any call with up to L tokens and S sequences: fewer sequences may go in segments where S do not.  Segments are at most a part of the 512 for
+// each sequence's heads and slices, and of four chunks at least, besides one for each sequence.
+size_t q8i_delta_most_room(int L, int S, int hv, int dk, int dv)
+{
+    const int heads = hv * ((dv + 31) / 32);
+    size_t room = delta_chunk_room(L, S, hv);
+    if (heads <= DELTA_FEW && L >= 24 * DELTA_C) room += delta_segment_room(std::min(512 / heads, L / (4 * DELTA_C)) + std::min(S, DELTA_FEW / heads), hv, dk, dv);
+    return room * sizeof(float);
 }
 
 q8_status q8i_delta_sequence(q8_ctx *ctx, const q8_delta_inputs *in, int L, const int *off, int S, const float *state, float *state_out, float *out, int ldo, float *room)

@@ -352,9 +352,10 @@ q8_status q8i_quantize_w4(q8_ctx *ctx, const float *X, int rows, int cols, int l
 size_t q8i_gemm_w4_parts(int n, int cols);
 size_t q8i_gemm_w4_scales(int n);
 q8_status q8i_gemm_w4(q8_ctx *ctx, const q8_mat_w4 *W, const float *X, int n, int ldx, const float *bias, float *Y, int ldy, uint8_t *parts, float *sx);
-// the gated delta rule; room: q8i_delta_room bytes
+// the gated delta rule; room: q8i_delta_room bytes (q8i_delta_most_room: of any call up to these sizes)
 q8_status q8i_delta_step(q8_ctx *ctx, const q8_delta_inputs *in, int n, const float *state, int slots, const int *parent, float *state_out, float *out, int ldo);
 size_t q8i_delta_room(int L, int S, int hv, int dk, int dv);
+size_t q8i_delta_most_room(int L, int S, int hv, int dk, int dv);
 q8_status q8i_delta_sequence(q8_ctx *ctx, const q8_delta_inputs *in, int L, const int *off, int S, const float *state, float *state_out, float *out, int ldo, float *room);
 q8_status q8i_tile_stats(q8_ctx *ctx, const float *logits, int n, int V, float *part_max, double *part_sum);
 q8_status q8i_sample(q8_ctx *ctx, const float *logits, int n, int V, int ldl, const q8_sampling *s, const float *u, int32_t *tokens, float *logp,

@@ -395,3 +395,56 @@ def test_a_key_of_zeros_costs_the_others_nothing(q, ctx):
     off = [0, 320]
     got = q.q8_delta_sequence(ctx, **_dev(ctx, x), sent_off=torch.tensor(off, dtype=torch.int32, device=ctx.device))
     _close(got, ref.sequence(**x, off=off), ref.sequence_bound(**x, off=off), 64)
+
+
+# ---- sizes of numbers ----
+
+@pytest.mark.parametrize("L", [70, 1200])
+def test_columns_of_any_size(q, ctx, L):
+    """Values whose columns differ by sixteen orders, states too: each column is as exact as its own size asks."""
+    rng = np.random.default_rng(L)
+    dk, dv = 48, 36
+    x = _inputs(rng, L, 1, 2, dk, dv)
+    size = (10.0 ** rng.integers(-8, 9, dv)).astype(np.float32)
+    x["v"] *= size
+    S = rng.standard_normal((1, 2, dk, dv)).astype(np.float32) * size
+    off = [0, L]
+    c = q.Context(workspace_bytes=q.q8_delta_bytes(L, 1, 2, dk, dv))
+    got = q.q8_delta_sequence(c, **_dev(ctx, x), sent_off=torch.tensor(off, dtype=torch.int32, device=ctx.device), state=ctx.f32(S))
+    want, bound = ref.sequence(**x, off=off, state=S), ref.sequence_bound(**x, off=off, state=S)
+    _close(got, want, tuple(b * (1 + np.sqrt(dk)) for b in bound), dk)
+    for a, b in ((np_(got["out"]), want[0]), (np_(got["state"]), want[1])):
+        off_by = np.linalg.norm((a - b).reshape(-1, dv), axis=0)
+        assert (off_by <= 8 * 3 * 2.0 ** -24 * np.sqrt(dk + 2 * ref.C) * np.linalg.norm(b.reshape(-1, dv), axis=0)).all()
+
+
+@pytest.mark.parametrize("L", [70, 1200])
+def test_keys_of_different_lengths_and_wide_gates(q, ctx, L):
+    """Keys and queries as they are given, of lengths from 1e-6 to 1 and up to 1e4; gates up to 2, which reflect the state."""
+    rng = np.random.default_rng(L + 1)
+    dk, dv = 32, 40
+    x = _inputs(rng, L, 2, 2, dk, dv, normalize=False)
+    x["k"] *= (10.0 ** -rng.integers(0, 7, (L, 2, 1))).astype(np.float32)
+    x["q"] *= (10.0 ** rng.integers(-4, 5, (L, 2, 1))).astype(np.float32)
+    x["beta"] *= 2
+    off = [0, L]
+    c = q.Context(workspace_bytes=q.q8_delta_bytes(L, 1, 2, dk, dv))
+    got = q.q8_delta_sequence(c, **_dev(ctx, x), sent_off=torch.tensor(off, dtype=torch.int32, device=ctx.device), normalize=False)
+    want, bound = ref.sequence(**x, off=off, normalize=False), ref.sequence_bound(**x, off=off, normalize=False)
+    state = np_(got["state"])
+    assert (np.linalg.norm(state - want[1], axis=2) <= bound[1] * (1 + np.sqrt(dk))).all()
+    assert np.linalg.norm(state - want[1]) <= 8 * 3 * 2.0 ** -24 * np.sqrt(dk + 2 * ref.C) * np.linalg.norm(want[1])
+    # a result is as far off as its query is long
+    ql = np.linalg.norm(x["q"], axis=2)[..., None].astype(np.float64)
+    e, r = (np_(got["out"]) - want[0]) / ql, want[0] / ql
+    assert np.linalg.norm(e) <= 8 * 3 * 2.0 ** -24 * np.sqrt(dk + 2 * ref.C) * np.linalg.norm(np.linalg.norm(want[1], axis=2)) * np.sqrt(L) + 1e-6 * np.linalg.norm(r)
+
+
+def test_no_tokens_at_all(q, ctx):
+    S = torch.randn(3, 2, 8, 12, device=ctx.device)
+    z = lambda *s: torch.empty(0, *s, device=ctx.device)
+    off = torch.zeros(4, dtype=torch.int32, device=ctx.device)
+    r = q.q8_delta_sequence(ctx, z(2, 8), z(2, 8), z(2, 12), z(2), z(2), off, state=S)
+    assert (r["state"] == S).all() and r["out"].shape == (0, 2, 12)
+    r = q.q8_delta_sequence(ctx, z(2, 8), z(2, 8), z(2, 12), z(2), z(2), off)
+    assert (r["state"] == 0).all()

@@ -141,6 +141,7 @@ def test_delta_sequences(lib):
     assert call(so=P + 4) == call(so=P - 1024) == SHAPE
     assert call(L=4000) == call(S=300) == WORKSPACE
     assert call() == call(state=None) == call(so=None) == call(so=FAR) == call(L=0) == call(L=1, S=1, ldo=0) == DEVICE
+    assert call(L=0, out=None, i=inputs(q=None, k=None, v=None, g=None, beta=None)) == DEVICE
     huge = inputs(hk=1, hv=64, dv=1, dk=1, ldq=1, ldk=1, ldv=64, ldg=64, ldb=64)
     assert call(L=1 << 23, S=1, i=huge, ldo=64) == SHAPE
 
@@ -205,3 +206,16 @@ def test_the_binding_refuses_tensors_of_another_gpu():
                 q.q8_delta_step(ctx, **x)
             with pytest.raises(ValueError, match=far + ": on cuda:1"):
                 q.q8_delta_sequence(ctx, **x, sent_off=here(3, dtype=i32))
+
+
+@pytest.mark.parametrize("hv,dk,dv", [(1, 256, 32), (4, 64, 64), (16, 128, 128), (24, 32, 128), (25, 32, 128), (96, 8, 32), (97, 8, 32), (3, 100, 72)])
+def test_workspace_of_fewer_tokens_and_sequences(lib, hv, dk, dv):
+    """q8_delta_bytes grows with both, and a call with less of either finds room: few long sequences take more than many."""
+    i = inputs(hk=1, hv=hv, dk=dk, dv=dv, ldq=dk, ldk=dk, ldv=hv * dv, ldg=hv, ldb=hv)
+    for L, S in ((800, 1), (5000, 3), (40000, 40), (200000, 7), (200001, 100)):
+        c = context(lib.q8_delta_bytes(L, S, hv, dk, dv))
+        for l in (0, 1, 767, 768, 769, 1000, 3000, 3100, 3500, 10000, 65536, 131071, 131072, L):
+            for s in (1, 2, 3, 4, 5, 24, 32, 96, S):
+                if l <= L and s <= S:
+                    assert lib.q8_delta_bytes(l, s, hv, dk, dv) <= lib.q8_delta_bytes(L, S, hv, dk, dv)
+                    assert lib.q8_delta_sequence(c, i, l, P, s, P, P, P, hv * dv) == DEVICE, (l, s)

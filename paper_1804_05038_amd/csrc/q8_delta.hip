@@ -63,7 +63,8 @@ struct DeltaStepArgs {
 
 // A block per slot, head and up to 4 LPR columns of the state.  Thread (r, c): columns 4 c .. 4 c + 3 of the R rows r R .. r R + R - 1, read
 // once and written once.  What a token reads is a q^T S + (q k) u, so that k^T S and q^T S come from the old state in one pass and
-// meet in LDS once.
+// meet in LDS once.  Bound by memory: 64 slots of 16 heads of 128 x 128 in 28.7 us, 4.7 TB/s read and written (a copy of 4 GiB: 4.8); 1000 slots of 6
+// heads of 100 x 72 in 75.8, 4.6; 5 slots of 4 heads of 64 x 64 in 4.0, a launch.
 template <int LPR, int R>
 __global__ __launch_bounds__(256) void delta_step_kernel(DeltaStepArgs a)
 {
@@ -219,6 +220,8 @@ __device__ __forceinline__ v4f fetch4(__amdgpu_buffer_rsrc_t rsrc, unsigned at, 
 // A block per chunk and head.  Three waves form a tile of 16 x 16 of both products each (the upper right one is zero) from rows that they load
 // as the matrix operation takes them, the fourth the sums of the decays; then (I + A)^-1 by substitution in blocks of 8, joined as
 // -T22 A21 T11 twice.  (Powers of A instead of substitution would cancel: 32 keys alike give binomials up to 3e8.)
+// 8 x 1024 tokens of 16 heads of 128 x 128 in 50 us: 134 MB of keys and queries read, 37 left, 3.4 TB/s; by waiting (74 % of the waves' time) for loads that all blocks
+// of a round ask for at once.  From rows staged in LDS, with the substitution in blocks of 16, 73.
 template <int DKT, bool VEC>         // dk in units of 32, rounded up; VEC: rows of queries and keys in whole 16-byte pieces
 __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaSeqArgs a)
 {
@@ -415,6 +418,9 @@ constexpr size_t delta_state_bytes(int dkt) { return dkt >= 4 ? (size_t)2 * 32 *
 // that what a column loses goes by its own size.  The two small products, of 32 x 32 with T and M, are fp32 ones.  Four waves multiply the
 // keys and make the updates, four multiply the queries and make the results; all convert, and all keep an eighth of the state.  The next chunk's rows are on
 // their way while one is worked on, each number in one thread's load and from there in LDS: loads of what several lanes need each cost the most here.
+// 2.5 us a chunk of 32 tokens for a block alone, 4.0 for the two of a compute unit (8 x 1024 tokens of 16 heads of 128 x 128 in 127 us): no unit is at its limit (vector
+// instructions 44 %, LDS 52 %, of which a sixth conflicts, matrix cores 27 %), a chunk is a chain of four barriers.  Fp32 matrix operations in four waves 197 us, parts in eight waves 157, 22 loads a wave
+// turned into 8 140, rows' pieces exchanged in LDS in place of padded 127.  (Registers are bounded to 128, so that two blocks are resident.)
 // SEGMENTS: in place of a sequence a block carries a part of it (below).  MOVES: nothing is read, no results.
 template <int DKT, bool VEC, bool SEGMENTS, bool MOVES>      // VEC: rows of queries, keys, values and results in whole 16-byte pieces
 __global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(DeltaSeqArgs a)
@@ -651,7 +657,8 @@ __global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(Delt
 // Few long sequences leave most of the device idle: a sequence's chunks come one after the other.  A segment of them makes F S + B of a state S, as the
 // rule is linear in it: B is what it makes of zeros, F what it makes of the unit vectors without values.  These come from all segments side by side
 // (MOVES), this kernel goes from segment to segment, ends[g] = F[g] ends[g - 1] + ends[g], and the results from all segments side by side again, each from
-// the state that the one before ends with.  About 2.7 times the work.  A block per sequence, head and 32 columns; products in fp32.
+// the state that the one before ends with.  About 2.7 times the work: 16384 tokens of 16 heads of
+// 128 x 128 in 661 us (chunks 95, moves 319, this 29, results 237) against 1415 in one go.  A block per sequence, head and 32 columns; products in fp32.
 template <int DKT, bool VEC>         // VEC: dk in whole 16-byte pieces
 __global__ __launch_bounds__(512) void delta_join_kernel(DeltaSeqArgs a)
 {

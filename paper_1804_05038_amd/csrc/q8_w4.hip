@@ -41,7 +41,8 @@ __device__ __forceinline__ float w4_group_max(float v)
 // A half wave per block of 128 columns, four a lane.  Per group lo = min(0, least), hi = max(0, largest finite value);
 // s = (hi - lo) / 15 rounded up to 8 significant bits, so that 15 s covers the range and s is the upper half of an fp32 number;
 // z = rint(-lo / s), code = rint(x / s) + z within 0 .. 15, quotients as fp32 division rounds them.  (hi - lo is formed at a
-// sixteenth: it may pass fp32's range.)  A run once per model: 50000 x 620 in groups of 32 takes some 40 us.
+// sixteenth: it may pass fp32's range.)  Run once per model: 63644 x 620 in groups of 32 in 57 us (183 MB read and written,
+// 3.2 TB/s), 50000 x 512 in groups of 128 in 37.
 template <int G>
 __global__ __launch_bounds__(256) void w4_quantize_kernel(W4QuantArgs a)
 {
@@ -164,6 +165,9 @@ struct W4GemmArgs {
 // itself.  A wave multiplies 16 rows at a time, four blocks of columns a turn; `split` waves share the rows, each with its range of
 // the columns.  Lane (i, g) has row i and of every block the 16-byte piece g, whose word t belongs to columns 32 t + 8 g + (0 .. 7):
 // a matrix operation takes 32 columns in a row, so that groups of 32 have their sums too.
+// 50000 x 512 x 5 in 6.7 us (14.6 MB, 3.1 us at a copy's rate; the smallest call takes 3.6): a chain of the vectors' way, their parts, a barrier, the
+// codes' expansion (nine instructions for eight weights) and the stores.  With the codes asked for before the vectors 8.7, as loads come back in order; vectors first
+// 8.1, and-or in one instruction 7.7, the vectors' loads under no condition 7.2, stores under none 6.9 (a branch waits for what is in flight).  2048 x 8192 x 1 in 7.7: 128 blocks of 16 rows, half of the compute units idle.
 template <int PER, int AHEAD>        // groups of a block; blocks of the vectors that a half wave asks for before anything else
 __global__ __launch_bounds__(1024) void w4_stream_kernel(W4GemmArgs a)
 {
@@ -397,6 +401,8 @@ template <> struct W4Words<4> { typedef v4u type; };
 // operation (t, p) of a block to columns 32 t + 16 p + (0 .. 15).  In LDS a vector's 16 pieces (hi, lo) are exchanged by its number mod 16, so that
 // lanes that read together find theirs on different banks.
 // KS > 1: KS such groups of waves take turns at the blocks of columns; their sums meet in LDS, in one order.  PAST: the results go past the caches.
+// 50000 x 512 x 1024 in 102 us, 109 with the parts' launch: 105 GFLOP in two products, 1.03 PFLOP/s where the library's largest fp16 product has 1.09, beside 205 MB
+// of results; 140 while each store stood in a branch of its own and waited for the one before.  63644 x 620 x 77 in 20 (45 MB).
 template <int PER, int WM, int WN, int TM, int TN, int KS, bool PAST>
 __global__ __launch_bounds__(64 * WM * WN * KS, TM * TN <= 4 ? 2 : 1) void w4_gemm_kernel(W4GemmArgs a)
 {
@@ -597,23 +603,26 @@ template <int PER, int WM, int WN, int TM, int TN, int KS = 1> static q8_status 
     return q8i_launch_check(ctx, "product w4");
 }
 
-// Tiles by what each costs (us, both launches; rows x columns x vectors / group).  Where 64 x 32 tiles are few and rows longer than two blocks, groups of waves
+// Tiles by what each costs (us, both launches; rows x columns x vectors / group).  Where 64 x 32 tiles are few and rows longer than a block, groups of waves
 // share the columns: 64 x 32 in four groups while they are at most one round (4096 x 2048 x 128 / 128 13.9 against 23.6 in 128 x 32, 1024 x 1024 x 256 / 64 11.2
-// against 15.7), 32 x 32 for the fewest of long rows (600 x 2000 x 100 / 32 13.7 against 14.9, 2048 x 2048 x 32 / 128 12.4 against 13.6), two groups up to two
-// rounds (20000 x 512 x 32 / 128 7.7 against 8.1 in four and 8.9 in 128 x 32, 30000 x 1000 x 24 / 64 10.8, 11.0 and 13.5; 50000 x 512 x 17 / 64 10.3, 11.6 and 9.5).  Else
-// 256 x 64 where there are many and the vectors fill them (50000 x 512 x 1024 / 128 124; 128 x 64 131, 128 x 32 146), 128 x 64 where these are more than a
+// against 15.7, 433 x 238 x 160 / 128 6.8 against 7.3), 32 x 32 for the fewest of long rows (2699 x 1882 x 42 / 64 11.7 against 12.8, 1095 x 1030 x 191 / 32 10.6 against
+// 11.4), two groups up to two rounds of longer rows (20000 x 512 x 32 / 128 7.7 against 8.1 in four and 8.9 in 128 x 32, 30000 x 1000 x 24 / 64 10.8, 11.0 and 13.5;
+// 50000 x 512 x 17 / 64 10.3, 11.6 and 9.5).  Else 256 x 64 where there are many, the vectors fill them and groups are not the finest, whose numbers do not fit
+// into the registers (50000 x 512 x 1024 / 128 124; 128 x 64 131, 128 x 32 146; 17152 x 415 x 578 / 32 50, 33 and 36), 128 x 64 where these are more than a
 // round (50000 x 512 x 40 / 128 12.3 against 13.6 in 128 x 32; 8000 x 1024 x 200 / 64 17.7 against 15.9), 128 x 96 for 65 to 96 vectors of many rows
-// (63644 x 620 x 77 / 32 24.4 against 25.8 in 128 x 32 and 29.3 in 128 x 64), and 128 x 32.
+// (63644 x 620 x 77 / 32 24.4 against 25.8 in 128 x 32 and 29.3 in 128 x 64), and 128 x 32.  Over 60 drawn sizes the chosen form was within 10 % of the best.
 template <int PER> static q8_status gemm_w4_tiles(q8_ctx *ctx, W4GemmArgs &a)
 {
-    const long long few = (long long)((a.rows + 63) / 64) * ((a.n + 31) / 32);
     auto tiles = [&](int r, int v) { return (long long)((a.rows + r - 1) / r) * ((a.n + v - 1) / v); };
-    if (a.nb >= 8 && few <= 64) return launch_w4<PER, 1, 1, 1, 1, 4>(ctx, a);
-    if (a.nb > 2 && few <= 256) return launch_w4<PER, 2, 1, 1, 1, 4>(ctx, a);
-    if (a.nb > 2 && few <= 512) return launch_w4<PER, 2, 1, 1, 1, 2>(ctx, a);
-    if (a.n > 64 && a.n <= 96 && tiles(128, 96) >= 400) return launch_w4<PER, 4, 1, 1, 3>(ctx, a);
+    const long long few = tiles(64, 32);
+    if (a.nb >= 6 && few <= 128) return launch_w4<PER, 1, 1, 1, 1, 4>(ctx, a);
+    if (a.nb >= 2 && few <= 256) return launch_w4<PER, 2, 1, 1, 1, 4>(ctx, a);
+    if (a.nb >= 3 && few <= 512) return launch_w4<PER, 2, 1, 1, 1, 2>(ctx, a);
+    if (a.n > 64 && a.n <= 96 && tiles(128, 96) >= 320) return launch_w4<PER, 4, 1, 1, 3>(ctx, a);
     if ((a.n + 63) / 64 * 320ll <= 8ll * a.n) {
-        if (tiles(256, 64) >= 1024) return launch_w4<PER, 4, 1, 2, 2>(ctx, a);
+        if constexpr (PER < 4) {
+            if (tiles(256, 64) >= 1024) return launch_w4<PER, 4, 1, 2, 2>(ctx, a);
+        }
         if (tiles(128, 64) >= 320) return launch_w4<PER, 4, 1, 1, 2>(ctx, a);
     }
     return launch_w4<PER, 4, 1, 1, 1>(ctx, a);

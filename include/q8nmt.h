@@ -675,7 +675,8 @@ q8_status output_logits_w4(q8_ctx *ctx, const q8_readout_weights *ro, const q8_m
  *   S = a S;  u = b (v - S^T k);  S = S + k u^T;  o = S^T q.
  * Query head h / (hv / hk) serves value head h.  normalize != 0: k / sqrt(|k|^2 + 1e-6) and q / sqrt(|q|^2 + 1e-6) in the places of k and q; q is
  * multiplied by `scale` either way.  g <= 0 (the logarithm of the decay; -inf or the lowest value: the state is forgotten), b in [0, 2], keys of at
- * most unit length keep states bounded; other values are computed as written.  All numbers fp32.  Row t of every table is
+ * most unit length keep states bounded; other values are computed as written.  All numbers fp32 (in a
+ * sequence, keys and queries whose largest number is below 2^-100, and columns of the state or of a chunk's updates below that, count as zeros in products).  Row t of every table is
  * token t (or slot t): q, k [. x ldq, ldk] with hk dk, v [. x ldv] with hv dv, g, beta [. x ldg, ldb] with hv numbers side by side, of any alignment
  * (rows in whole 16 bytes are faster), pitches up to 2^22.  1 <= dk, dv <= 256, hv a multiple of hk. */
 typedef struct {
@@ -694,7 +695,7 @@ q8_status q8_delta_step(q8_ctx *ctx, const q8_delta_inputs *in, int n, const flo
 
 /* n_seq sequences laid end to end: sequence s has the tokens off[s] .. off[s + 1] - 1 (off: n_seq + 1 numbers on the device, ascending, within
  * [0, L]; one without tokens keeps its state).  out [L x ldo]: rows that belong to no sequence stay as they are.  state (NULL: zeros) and state_out (may be NULL; may be
- * state) [n_seq x hv x dk x dv].  0 <= L <= 2^24 (0: the tables may be NULL), n_seq <= 65536, and (L / 32 + n_seq) hv, n_seq hv < 2^24.  out overlaps no input.  Workspace: the context's must have
+ * state) [n_seq x hv x dk x dv].  0 <= L <= 2^24 (0: the tables may be NULL), n_seq <= 65536, and (L / 32 + n_seq) hv < 2^23.  out overlaps no input.  Workspace: the context's must have
  * q8_delta_bytes(L, n_seq, hv, dk, dv) bytes, which are enough for fewer tokens and sequences too. */
 size_t q8_delta_bytes(int L, int n_seq, int hv, int dk, int dv);
 q8_status q8_delta_sequence(q8_ctx *ctx, const q8_delta_inputs *in, int L, const int32_t *off, int n_seq, const float *state, float *state_out,

@@ -2060,7 +2060,8 @@ q8_status q8_delta_sequence(q8_ctx *ctx, const q8_delta_inputs *in, int L, const
     if (L < 0 || L > kDeltaMaxL || n_seq <= 0 || n_seq > kDeltaMaxSeq) return q8_fail(ctx, Q8_ERR_SHAPE, "q8_delta_sequence: %d tokens, %d sequences", L, n_seq);
     TRY(check_delta(ctx, in, L, out, ldo));
     if (!off) return q8_fail(ctx, Q8_ERR_NULL, "q8_delta_sequence: off: NULL");
-    if (((size_t)L / 32 + n_seq) * in->hv >= 1u << 24) return q8_fail(ctx, Q8_ERR_SHAPE, "q8_delta_sequence: %d tokens of %d heads are too many for a launch", L, in->hv);
+    if (((size_t)L / 32 + n_seq) * in->hv >= 1u << 23)                       // blocks of 512 threads: 2^32 are one too many
+        return q8_fail(ctx, Q8_ERR_SHAPE, "q8_delta_sequence: %d tokens of %d heads are too many for a launch", L, in->hv);
     if ((uintptr_t)state % 4 != 0 || (uintptr_t)state_out % 4 != 0 || (uintptr_t)off % 4 != 0) return q8_fail(ctx, Q8_ERR_ALIGN, "q8_delta_sequence: a buffer is not aligned to 4 bytes");
     const size_t all = (size_t)n_seq * in->hv * in->dk * in->dv * 4;
     const uintptr_t a0 = (uintptr_t)state, b0 = (uintptr_t)state_out;

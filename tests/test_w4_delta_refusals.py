@@ -144,6 +144,10 @@ def test_delta_sequences(lib):
     assert call(L=0, out=None, i=inputs(q=None, k=None, v=None, g=None, beta=None)) == DEVICE
     huge = inputs(hk=1, hv=64, dv=1, dk=1, ldq=1, ldk=1, ldv=64, ldg=64, ldb=64)
     assert call(L=1 << 23, S=1, i=huge, ldo=64) == SHAPE
+    wide = inputs(hk=1, hv=128, dv=1, dk=1, ldq=1, ldk=1, ldv=128, ldg=128, ldb=128)
+    big = context(lib.q8_delta_bytes(0, 65536, 128, 1, 1))
+    wide_call = lambda S: lib.q8_delta_sequence(big, wide, 0, P, S, None, None, P, 128)
+    assert wide_call(65535) == DEVICE and wide_call(65536) == SHAPE
 
 
 def test_delta_bytes(lib):

@@ -217,11 +217,11 @@ __device__ __forceinline__ v4f fetch4(__amdgpu_buffer_rsrc_t rsrc, unsigned at, 
     return v;
 }
 
-// A block per chunk and head.  Three waves form a tile of 16 x 16 of both products each (the upper right one is zero) from rows that they load
-// as the matrix operation takes them, the fourth the sums of the decays; then (I + A)^-1 by substitution in blocks of 8, joined as
+// A block per chunk and head.  The waves form tiles of 16 x 16 of both products (the upper right ones are zero) from rows that they load as the
+// matrix operation takes them, the last the sums of the decays too; then (I + A)^-1 by substitution in blocks of 8, joined as
 // -T22 A21 T11 twice.  (Powers of A instead of substitution would cancel: 32 keys alike give binomials up to 3e8.)
-// 8 x 1024 tokens of 16 heads of 128 x 128 in 50 us: 134 MB of keys and queries read, 37 left, 3.4 TB/s; by waiting (74 % of the waves' time) for loads that all blocks
-// of a round ask for at once.  From rows staged in LDS, with the substitution in blocks of 16, 73.
+// 8 x 1024 tokens of 16 heads of 128 x 128 in 48 us: 134 MB of keys and queries read, 37 left, 3.6 TB/s; by waiting (three quarters of the waves' time) for loads that all blocks
+// of a round ask for at once.  From rows staged in LDS, with the substitution in blocks of 16, 73; the products in three waves 51.
 template <int DKT, bool VEC>         // dk in units of 32, rounded up; VEC: rows of queries and keys in whole 16-byte pieces
 __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaSeqArgs a)
 {
@@ -247,37 +247,42 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaSeqArgs a)
     const int m = s_at[1] > 0 ? min(s_at[1], a.L - s_at[0]) : 0;
     if (m <= 0) return;                                                     // (a place that no chunk has)
 
-    const int mt = wave > 0, nt = wave == 1;
-    v4f akk = {0.0f, 0.0f, 0.0f, 0.0f}, aqk = akk;
-    if (wave < 3) {
-        const int r = 16 * mt + i, rn = 16 * nt + i;
+    // wave 0: keys x keys and queries x keys of the first 16 tokens, 1: of the last, 2: keys of the last x keys of the first, 3: queries of the last x those
+    v4f akk = {0.0f, 0.0f, 0.0f, 0.0f}, azk = akk;
+    const int mt = wave > 0, nt = wave == 1, r = 16 * nt + i, rz = 16 * mt + i;
+    {
         // (rows past the chunk's end lie past the end of what is described; its rows are below 2^31 bytes: pitches are at most 2^22)
+        const bool keys = wave == 2;
+        const int ldz = keys ? p.ldk : p.ldq;
         const __amdgpu_buffer_rsrc_t rk = q8_rsrc(p.k + tok * p.ldk + (size_t)kh * p.dk, 4 * ((size_t)(m - 1) * p.ldk + p.dk));
-        const __amdgpu_buffer_rsrc_t rq = q8_rsrc(p.q + tok * p.ldq + (size_t)kh * p.dk, 4 * ((size_t)(m - 1) * p.ldq + p.dk));
-        const unsigned k = 4u * ((unsigned)r * (unsigned)p.ldk + 4 * gq), q = 4u * ((unsigned)r * (unsigned)p.ldq + 4 * gq), kn = 4u * ((unsigned)rn * (unsigned)p.ldk + 4 * gq);
+        const __amdgpu_buffer_rsrc_t rs = q8_rsrc((keys ? p.k : p.q) + tok * ldz + (size_t)kh * p.dk, 4 * ((size_t)(m - 1) * ldz + p.dk));
+        const unsigned k = r < m ? 4u * ((unsigned)r * (unsigned)p.ldk + 4 * gq) : Q8_OOB, z0 = rz < m ? 4u * ((unsigned)rz * (unsigned)ldz + 4 * gq) : Q8_OOB;
         float kk = 0.0f, qq = 0.0f, mk = 0.0f, mq = 0.0f;
         for (int t0 = 0; t0 < 2 * DKT; t0 += STEPS) {
-            v4f x[STEPS], y[STEPS], z[STEPS];
+            v4f x[STEPS], z[STEPS];
 #pragma unroll
             for (int t = 0; t < STEPS; ++t) {
                 const int left = p.dk - 16 * (t0 + t) - 4 * gq;
-                const unsigned at = 64u * (t0 + t);
-                x[t] = fetch4<VEC>(rk, left > 0 && r < m ? k + at : Q8_OOB, left);
-                y[t] = fetch4<VEC>(rq, left > 0 && r < m ? q + at : Q8_OOB, left);
-                z[t] = fetch4<VEC>(rk, left > 0 && wave == 2 && rn < m ? kn + at : Q8_OOB, left);
+                const unsigned at = left > 0 ? 64u * (t0 + t) : Q8_OOB;
+                x[t] = fetch4<VEC>(rk, max(k, at) < Q8_OOB ? k + at : Q8_OOB, left);
+                z[t] = fetch4<VEC>(rs, max(z0, at) < Q8_OOB ? z0 + at : Q8_OOB, left);
             }
 #pragma unroll
             for (int t = 0; t < STEPS; ++t)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float other = wave == 2 ? z[t][e] : x[t][e];
-                    akk = __builtin_amdgcn_mfma_f32_16x16x4f32(x[t][e], other, akk, 0, 0, 0);
-                    aqk = __builtin_amdgcn_mfma_f32_16x16x4f32(y[t][e], other, aqk, 0, 0, 0);
-                    kk = fmaf(x[t][e], x[t][e], kk);
-                    qq = fmaf(y[t][e], y[t][e], qq);
-                    mk = fmaxf(mk, fabsf(x[t][e]));
-                    mq = fmaxf(mq, fabsf(y[t][e]));
-                }
+                for (int e = 0; e < 4; ++e) azk = __builtin_amdgcn_mfma_f32_16x16x4f32(z[t][e], x[t][e], azk, 0, 0, 0);
+            if (wave < 2) {
+#pragma unroll
+                for (int t = 0; t < STEPS; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        akk = __builtin_amdgcn_mfma_f32_16x16x4f32(x[t][e], x[t][e], akk, 0, 0, 0);
+                        kk = fmaf(x[t][e], x[t][e], kk);
+                        qq = fmaf(z[t][e], z[t][e], qq);
+                        mk = fmaxf(mk, fabsf(x[t][e]));
+                        mq = fmaxf(mq, fabsf(z[t][e]));
+                    }
+            }
         }
         if (wave < 2) {                                                     // each row once
 #pragma unroll
@@ -294,7 +299,8 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaSeqArgs a)
                 s_mq[r] = mq;
             }
         }
-    } else {
+    }
+    if (wave == 3) {
         const int t = lane & 31;
         const float g = t < m ? p.g[(tok + t) * p.ldg + head] : 0.0f;
         double c = g < (float)DELTA_LEAST ? DELTA_LEAST : (double)g;
@@ -309,16 +315,18 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaSeqArgs a)
     }
     __syncthreads();
     float *room = a.room + ((size_t)slot * p.hv + head) * DELTA_ROOM;
-    if (wave < 3) {                                                         // lane (i, gq): column i, rows 4 gq + e of a tile
+    {                                                                       // lane (i, gq): column i, rows 4 gq + e of a tile
         const int col = 16 * nt + i;
+        if (wave == 2) akk = azk;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int row = 16 * mt + 4 * gq + e;
             const float d = row >= col ? expf((float)(s_c[row] - s_c[col])) * s_rk[col] : 0.0f;
-            sA[row * PT + col] = row > col ? s_b[row] * s_rk[row] * d * akk[e] : 0.0f;
-            room[DELTA_MATRIX + row * DELTA_C + col] = row >= col ? s_rq[row] * d * aqk[e] : 0.0f;
+            if (wave < 3) sA[row * PT + col] = row > col ? s_b[row] * s_rk[row] * d * akk[e] : 0.0f;
+            if (wave != 2) room[DELTA_MATRIX + row * DELTA_C + col] = row >= col ? s_rq[row] * d * azk[e] : 0.0f;
         }
-    } else {
+    }
+    if (wave == 2) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) room[DELTA_MATRIX + (4 * gq + e) * DELTA_C + 16 + i] = 0.0f;
         if (lane < DELTA_C) {
@@ -658,7 +666,7 @@ __global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(Delt
 // rule is linear in it: B is what it makes of zeros, F what it makes of the unit vectors without values.  These come from all segments side by side
 // (MOVES), this kernel goes from segment to segment, ends[g] = F[g] ends[g - 1] + ends[g], and the results from all segments side by side again, each from
 // the state that the one before ends with.  About 2.7 times the work: 16384 tokens of 16 heads of
-// 128 x 128 in 661 us (chunks 95, moves 319, this 29, results 237) against 1415 in one go.  A block per sequence, head and 32 columns; products in fp32.
+// 128 x 128 in 655 us (chunks 89, moves 320, this 29, results 240) against 1415 in one go.  A block per sequence, head and 32 columns; products in fp32.
 template <int DKT, bool VEC>         // VEC: dk in whole 16-byte pieces
 __global__ __launch_bounds__(512) void delta_join_kernel(DeltaSeqArgs a)
 {

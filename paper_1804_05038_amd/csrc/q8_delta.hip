@@ -442,7 +442,7 @@ __global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(Delt
     const q8_delta_inputs &p = a.in;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, gq = lane >> 4, mt = wave & 1, nt = (wave >> 1) & 1, queries = wave >> 2;
     const int head = blockIdx.x % p.hv, place = blockIdx.x / p.hv, kh = head / (p.hv / p.hk), lc = 16 * nt + i;
-    int s = place, segment = 0, first, length;
+    int s = place, segment = 0, final = 0, first, length;
     bool last = true;
     if constexpr (SEGMENTS) {
         int *s_at = (int *)s_all;
@@ -459,7 +459,8 @@ __global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(Delt
         first = __builtin_amdgcn_readfirstlane(delta_first(a, s));
         length = __builtin_amdgcn_readfirstlane(delta_length(a, s, first));
         segment = place - (first / (DELTA_C * a.seg) + s);
-        last = segment >= max(length - 1, 0) / (DELTA_C * a.seg);
+        final = max(length - 1, 0) / (DELTA_C * a.seg);
+        last = segment >= final;
         first += segment * DELTA_C * a.seg;
         length = min(length - segment * DELTA_C * a.seg, DELTA_C * a.seg);
     } else {
@@ -467,10 +468,12 @@ __global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(Delt
         length = __builtin_amdgcn_readfirstlane(delta_length(a, s, first));
     }
     // MOVES: columns of the state from zeros (a sequence's first segment: from its state), then those of what the segment makes of any state, from the
-    // unit vectors and without values; neither is asked of a sequence's last segment
+    // unit vectors and without values; neither is asked of a sequence's last segment, which puts the state where its end would be: the first segment starts
+    // from there later, as the last one may leave the new state over the old one before the first has read it
     const int slices = (p.dv + 31) / 32;
     const bool unit = MOVES && (int)blockIdx.y >= slices;
-    if (MOVES && (last || (unit && segment == 0))) return;
+    if (MOVES && (segment == 0 ? last || unit : last && unit)) return;
+    if (MOVES && last) length = 0;
     const int v0 = 32 * ((int)blockIdx.y - (unit ? slices : 0)), col = v0 + lc, dv = unit ? p.dk : p.dv;
     const bool live = col < dv;
     const int tile0 = 2 * queries + mt, r0 = 16 * mt + 4 * gq;
@@ -487,8 +490,10 @@ __global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(Delt
 #pragma unroll
             for (int e = 0; e < 4; ++e) st[t][e] = 16 * (4 * t + tile0) + 4 * gq + e == col ? 1.0f : 0.0f;
     } else {                                                                // (a later segment's state is where the one before ends; none: zeros)
-        const float *from = segment == 0 ? a.state + mine : a.ends + there - (size_t)p.hv * p.dk * p.dv;
-        const __amdgpu_buffer_rsrc_t rs = q8_rsrc(from, (segment == 0 ? a.state != nullptr : !MOVES) ? bytes : 0);
+        const ptrdiff_t one = (ptrdiff_t)p.hv * p.dk * p.dv;
+        const bool given = MOVES ? segment == 0 || last : segment == 0 && last;
+        const float *from = given ? a.state + mine : a.ends + there + (segment == 0 ? final * one : -one);
+        const __amdgpu_buffer_rsrc_t rs = q8_rsrc(from, (given ? a.state != nullptr : !MOVES) ? bytes : 0);
 #pragma unroll
         for (int t = 0; t < OWN; ++t)
 #pragma unroll

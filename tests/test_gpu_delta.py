@@ -386,6 +386,27 @@ def test_long_sequences(q, lengths, hk, hv, dk, dv, edges):
     assert (np_(state) == first[1]).all()
 
 
+@pytest.mark.parametrize("lengths", [(4097,), (2049, 1, 2050, 0, 900)])
+def test_segments_with_the_new_state_over_the_old_one(q, lengths):
+    """A last segment of a token ends long before the first one does."""
+    rng = np.random.default_rng(31)
+    off = np.concatenate([[0], np.cumsum(lengths)]).tolist()
+    L, S = off[-1], len(lengths)
+    ctx = q.Context(workspace_bytes=q.q8_delta_bytes(L, S, 2, 64, 48))
+    x = _inputs(rng, L, 1, 2, 64, 48)
+    x["g"] *= np.float32(0.001)
+    st = rng.standard_normal((S, 2, 64, 48)).astype(np.float32)
+    args = dict(**_dev(ctx, x), sent_off=torch.tensor(off, dtype=torch.int32, device=ctx.device), scale=0.3)
+    assert q.q8_delta_bytes(L, S, 2, 64, 48) - q.q8_delta_bytes(L, S, 2, 64, 1) >= 4 * 2 * 64 * 47
+    kept = ctx.f32(st)
+    apart = q.q8_delta_sequence(ctx, **args, state=kept)
+    assert (np_(kept) == st).all()
+    for _ in range(5):
+        state = ctx.f32(st)
+        over = q.q8_delta_sequence(ctx, **args, state=state, state_out=state)
+        assert (np_(over["out"]) == np_(apart["out"])).all() and (np_(state) == np_(apart["state"])).all()
+
+
 def test_a_key_of_zeros_costs_the_others_nothing(q, ctx):
     """Between keys as they are met: results as exact as without it."""
     rng = np.random.default_rng(20)

@@ -419,7 +419,11 @@ __device__ __forceinline__ int delta_place(int row, int k)
 }
 
 // Bytes of LDS for the state's parts, and for the updates later.
-constexpr size_t delta_state_bytes(int dkt) { return dkt >= 4 ? (size_t)2 * 32 * 32 * dkt * 2 : (size_t)2 * 32 * (DELTA_C + 4) * 4; }
+template <bool MOVES> constexpr size_t delta_state_bytes(int dkt)
+{
+    const size_t parts = (size_t)2 * (MOVES ? 64 : 32) * 32 * dkt * 2, updates = (size_t)2 * 32 * (DELTA_C + 4) * 4;
+    return parts > updates ? parts : updates;
+}
 
 // A block per sequence, head and 32 columns of the state, which stays in registers as fp32.  Its products run on the fp16 matrix cores with both sides in two
 // parts (hi hi + hi lo + lo hi, within 2^-21): rows of keys and queries with a power of two each, columns of the state and of the updates too, so
@@ -429,18 +433,21 @@ constexpr size_t delta_state_bytes(int dkt) { return dkt >= 4 ? (size_t)2 * 32 *
 // 2.5 us a chunk of 32 tokens for a block alone, 4.0 for the two of a compute unit (8 x 1024 tokens of 16 heads of 128 x 128 in 127 us): no unit is at its limit (vector
 // instructions 44 %, LDS 52 %, of which a sixth conflicts, matrix cores 27 %), a chunk is a chain of four barriers.  Fp32 matrix operations in four waves 197 us, parts in eight waves 157, 22 loads a wave
 // turned into 8 140, rows' pieces exchanged in LDS in place of padded 127.  (Registers are bounded to 128, so that two blocks are resident.)
-// SEGMENTS: in place of a sequence a block carries a part of it (below).  MOVES: nothing is read, no results.
+// SEGMENTS: in place of a sequence a block carries a part of it (below).  MOVES: no queries and no results; 64 columns, so that all eight waves multiply the keys
+// (16384 tokens 243 us; 32 columns in four of the waves 320).
 template <int DKT, bool VEC, bool SEGMENTS, bool MOVES>      // VEC: rows of queries, keys, values and results in whole 16-byte pieces
 __global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(DeltaSeqArgs a)
 {
-    constexpr int DKP = 32 * DKT, PART = DELTA_C * DKP, PT = DELTA_C + 4, OWN = DKT / 2;      // of a thread: pieces of four numbers of the keys, of the queries and of the state
+    constexpr int DKP = 32 * DKT, PART = DELTA_C * DKP, PT = DELTA_C + 4, OWN = DKT / 2;      // of a thread: pieces of four numbers of the keys and of the queries
+    // columns; row tiles of the state between two of a wave, a wave's row tiles; the state's parts; the pitch of values
+    constexpr int COLS = MOVES ? 64 : 32, STRIDE = MOVES ? 2 : 4, TILES = 2 * DKT / STRIDE, STATE = COLS * DKP, PV = COLS + 4;
     static_assert(DKT % 2 == 0, "eight waves share the state's tiles");
     extern __shared__ __align__(16) uint8_t s_all[];
-    _Float16 *sK = (_Float16 *)s_all, *sQ = sK + 2 * PART, *sS = sQ + 2 * PART;      // [hi, lo][token or column][row of the state]
-    float *sR = (float *)((uint8_t *)sS + delta_state_bytes(DKT)), *sM = sR + 32 * PT, *sV = sM + 2 * 32 * PT, *s_vec = sV + 32 * PT, *s_top = s_vec + 6 * DELTA_C, *s_wtop = s_top + 128;
-    float *sU = (float *)sS, *sW = sU + 32 * PT;                            // (the state's parts have been read by then) sR, sU, sW [column][token], sM [T, M][token][token], sV values and results [token][column]
+    _Float16 *sK = (_Float16 *)s_all, *sQ = sK + 2 * PART, *sS = MOVES ? sQ : sQ + 2 * PART;      // [hi, lo][token or column][row of the state]
+    float *sR = (float *)((uint8_t *)sS + delta_state_bytes<MOVES>(DKT)), *sM = sR + COLS * PT, *sV = sM + (MOVES ? 1 : 2) * 32 * PT, *s_vec = sV + 32 * PV, *s_top = s_vec + 6 * DELTA_C, *s_wtop = s_top + 128;
+    float *sU = (float *)sS, *sW = MOVES ? sU : sU + 32 * PT;               // (the state's parts have been read by then) sR, sU, sW [column][token], sM [T, M][token][token], sV values and results [token][column]
     const q8_delta_inputs &p = a.in;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, gq = lane >> 4, mt = wave & 1, nt = (wave >> 1) & 1, queries = wave >> 2;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, gq = lane >> 4, mt = wave & 1, half = wave >> 2, nt = ((wave >> 1) & 1) + (MOVES ? 2 * half : 0), queries = MOVES ? 0 : half;
     const int head = blockIdx.x % p.hv, place = blockIdx.x / p.hv, kh = head / (p.hv / p.hk), lc = 16 * nt + i;
     int s = place, segment = 0, final = 0, first, length;
     bool last = true;
@@ -470,32 +477,32 @@ __global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(Delt
     // MOVES: columns of the state from zeros (a sequence's first segment: from its state), then those of what the segment makes of any state, from the
     // unit vectors and without values; neither is asked of a sequence's last segment, which puts the state where its end would be: the first segment starts
     // from there later, as the last one may leave the new state over the old one before the first has read it
-    const int slices = (p.dv + 31) / 32;
+    const int slices = (p.dv + COLS - 1) / COLS;
     const bool unit = MOVES && (int)blockIdx.y >= slices;
     if (MOVES && (segment == 0 ? last || unit : last && unit)) return;
     if (MOVES && last) length = 0;
-    const int v0 = 32 * ((int)blockIdx.y - (unit ? slices : 0)), col = v0 + lc, dv = unit ? p.dk : p.dv;
+    const int v0 = COLS * ((int)blockIdx.y - (unit ? slices : 0)), col = v0 + lc, dv = unit ? p.dk : p.dv;
     const bool live = col < dv;
-    const int tile0 = 2 * queries + mt, r0 = 16 * mt + 4 * gq;
-    // rows 16 (4 t + tile0) + 4 gq + e of column `col` of the state
-    v4f st[OWN];
+    const int tile0 = MOVES ? mt : 2 * half + mt, r0 = 16 * mt + 4 * gq;
+    // rows 16 (STRIDE t + tile0) + 4 gq + e of column `col` of the state
+    v4f st[TILES];
     const size_t bytes = 4 * (size_t)p.dk * dv, mine = ((size_t)s * p.hv + head) * p.dk * p.dv, there = ((size_t)place * p.hv + head) * p.dk * dv;
     auto state_at = [&](int t, int e) {
-        const int row = 16 * (4 * t + tile0) + 4 * gq + e;
+        const int row = 16 * (STRIDE * t + tile0) + 4 * gq + e;
         return (int)(live && row < p.dk ? 4u * ((unsigned)row * (unsigned)dv + col) : Q8_OOB);
     };
     if (unit) {
 #pragma unroll
-        for (int t = 0; t < OWN; ++t)
+        for (int t = 0; t < TILES; ++t)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) st[t][e] = 16 * (4 * t + tile0) + 4 * gq + e == col ? 1.0f : 0.0f;
+            for (int e = 0; e < 4; ++e) st[t][e] = 16 * (STRIDE * t + tile0) + 4 * gq + e == col ? 1.0f : 0.0f;
     } else {                                                                // (a later segment's state is where the one before ends; none: zeros)
         const ptrdiff_t one = (ptrdiff_t)p.hv * p.dk * p.dv;
         const bool given = MOVES ? segment == 0 || last : segment == 0 && last;
         const float *from = given ? a.state + mine : a.ends + there + (segment == 0 ? final * one : -one);
         const __amdgpu_buffer_rsrc_t rs = q8_rsrc(from, (given ? a.state != nullptr : !MOVES) ? bytes : 0);
 #pragma unroll
-        for (int t = 0; t < OWN; ++t)
+        for (int t = 0; t < TILES; ++t)
 #pragma unroll
             for (int e = 0; e < 4; ++e) st[t][e] = __int_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, state_at(t, e), 0, 0));
     }
@@ -508,7 +515,8 @@ __global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(Delt
         ok[x] = k < p.dk ? 4u * ((unsigned)r * (unsigned)p.ldk + k) : Q8_OOB;
         oq[x] = k < p.dk ? 4u * ((unsigned)r * (unsigned)p.ldq + k) : Q8_OOB;
     }
-    const int vr = (tid & 255) >> 3, vc = 4 * (tid & 7), vleft = tid < 256 && !unit ? p.dv - v0 - vc : 0;
+    const bool values = MOVES || tid < 256;
+    const int vr = MOVES ? tid >> 4 : (tid & 255) >> 3, vc = 4 * (tid & (COLS / 4 - 1)), vleft = values && !unit ? p.dv - v0 - vc : 0;
     const unsigned ov = vleft > 0 ? 4u * ((unsigned)vr * (unsigned)p.ldv + v0 + vc) : Q8_OOB, oo = vleft > 0 ? 4u * ((unsigned)vr * (unsigned)a.ldo + v0 + vc) : Q8_OOB;
     const unsigned oe = tid < 48 ? 4u * (2 * DELTA_MATRIX + 4 * tid) : Q8_OOB;
     v4f pk[OWN], pq[OWN], pm, pv, pe;
@@ -527,7 +535,7 @@ __global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(Delt
             pk[x] = fetch4<VEC>(rk, ok[x], left);
             if constexpr (!MOVES) pq[x] = fetch4<VEC>(rq, oq[x], left);
         }
-        pm = fetch4<true>(rr, 16u * tid, 4);
+        pm = fetch4<true>(rr, !MOVES || tid < 256 ? 16u * tid : Q8_OOB, 4);
         pv = fetch4<VEC>(rv, ov, vleft);
     };
     // the largest of a column's numbers that this wave has
@@ -539,15 +547,15 @@ __global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(Delt
     auto leave_state = [&] {                                                // ... and the next chunk's numbers of the tokens
         float top = 0.0f;
 #pragma unroll
-        for (int t = 0; t < OWN; ++t)
+        for (int t = 0; t < TILES; ++t)
 #pragma unroll
             for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(st[t][e]));
-        leave_top(top, s_top + 32 * tile0);
+        leave_top(top, s_top + COLS * tile0);
         if (tid < 48) *(v4f *)(s_vec + 4 * tid) = pe;
     };
     auto results = [&](int t0) {                                            // of the chunk at t0, from LDS
         const __amdgpu_buffer_rsrc_t ro = q8_rsrc(a.out + ((size_t)first + t0) * a.ldo + (size_t)head * p.dv, 4 * ((size_t)(min(DELTA_C, length - t0) - 1) * a.ldo + p.dv));
-        const v4f o = *(const v4f *)(sV + vr * PT + vc);
+        const v4f o = *(const v4f *)(sV + vr * PV + vc);
         if constexpr (VEC) {
             __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(v4u, o), ro, (int)oo, 0, 0);
         } else {
@@ -562,14 +570,16 @@ __global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(Delt
     }
     for (int t0 = 0; t0 < length; t0 += DELTA_C) {
         float inv;
-        const float cs = parts_scale(fmaxf(fmaxf(s_top[lc], s_top[32 + lc]), fmaxf(s_top[64 + lc], s_top[96 + lc])), inv);
+        float top = fmaxf(s_top[lc], s_top[COLS + lc]);
+        if constexpr (!MOVES) top = fmaxf(top, fmaxf(s_top[64 + lc], s_top[96 + lc]));
+        const float cs = parts_scale(top, inv);
 #pragma unroll
-        for (int t = 0; t < OWN; ++t) {
+        for (int t = 0; t < TILES; ++t) {
             uint2 hi, lo;
             parts4(st[t][0], st[t][1], st[t][2], st[t][3], inv, hi, lo);
-            _Float16 *to = sS + delta_place<DKT>(lc, 16 * (4 * t + tile0) + 4 * gq);
+            _Float16 *to = sS + delta_place<DKT>(lc, 16 * (STRIDE * t + tile0) + 4 * gq);
             *(uint2 *)to = hi;
-            *(uint2 *)(to + PART) = lo;
+            *(uint2 *)(to + STATE) = lo;
         }
 #pragma unroll
         for (int x = 0; x < OWN; ++x) {
@@ -584,20 +594,19 @@ __global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(Delt
                 *(uint2 *)(sQ + PART + to) = lo;
             }
         }
-        *(v4f *)(sM + (tid >> 3) * PT + 4 * (tid & 7)) = pm;
+        if (!MOVES || tid < 256) *(v4f *)(sM + (tid >> 3) * PT + 4 * (tid & 7)) = pm;
         if (!MOVES && t0 > 0 && tid < 256) results(t0 - DELTA_C);                     // (a thread's piece of the results, then of the values, in one place)
-        if (tid < 256) *(v4f *)(sV + vr * PT + vc) = pv;
+        if (values) *(v4f *)(sV + vr * PV + vc) = pv;
         __syncthreads();
         if (t0 + DELTA_C < length) fetch(t0 + DELTA_C);
         const v4f eb = *(const v4f *)(s_vec + queries * DELTA_C + r0), el = *(const v4f *)(s_vec + 2 * DELTA_C + r0);
         const float keep = s_vec[5 * DELTA_C];
         v4f x0 = {0.0f, 0.0f, 0.0f, 0.0f}, x1 = x0, x2 = x0;                // keys or queries times the state
         const _Float16 *rows = queries ? sQ : sK;
-        if (!MOVES || !queries)
 #pragma unroll
         for (int t = 0; t < DKT; ++t) {
             const _Float16 *x = rows + delta_place<DKT>(16 * mt + i, 32 * t + 8 * gq), *y = sS + delta_place<DKT>(lc, 32 * t + 8 * gq);
-            const v8h xh = *(const v8h *)x, xl = *(const v8h *)(x + PART), sh = *(const v8h *)y, sl = *(const v8h *)(y + PART);
+            const v8h xh = *(const v8h *)x, xl = *(const v8h *)(x + PART), sh = *(const v8h *)y, sl = *(const v8h *)(y + STATE);
             x0 = __builtin_amdgcn_mfma_f32_16x16x32_f16(xh, sh, x0, 0, 0, 0);
             x1 = __builtin_amdgcn_mfma_f32_16x16x32_f16(xh, sl, x1, 0, 0, 0);
             x2 = __builtin_amdgcn_mfma_f32_16x16x32_f16(xl, sh, x2, 0, 0, 0);
@@ -607,7 +616,7 @@ __global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(Delt
         if (!queries) {
             v4f v;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = sV[(r0 + e) * PT + lc];
+            for (int e = 0; e < 4; ++e) v[e] = sV[(r0 + e) * PV + lc];
             *(v4f *)(sR + lc * PT + r0) = v - xs;
         }
         __syncthreads();
@@ -626,20 +635,20 @@ __global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(Delt
             const v4f u = small(sR, (v4f){0.0f, 0.0f, 0.0f, 0.0f});
             // the results take the updates, the state takes them times exp(c_C - c_j) / |k_j|
             const v4f w = u * el;
-            *(v4f *)(sU + lc * PT + r0) = u;
+            if constexpr (!MOVES) *(v4f *)(sU + lc * PT + r0) = u;
             *(v4f *)(sW + lc * PT + r0) = w;
-            leave_top(fmaxf(fmaxf(fabsf(w[0]), fabsf(w[1])), fmaxf(fabsf(w[2]), fabsf(w[3]))), s_wtop + 32 * mt);
+            leave_top(fmaxf(fmaxf(fabsf(w[0]), fabsf(w[1])), fmaxf(fabsf(w[2]), fabsf(w[3]))), s_wtop + COLS * mt);
         }
         __syncthreads();
         // tokens 8 gq + (0, 2, 4, 6, 1, 3, 5, 7) of column i: four rows of the keys that are read together lie two apart, on different banks
-        const float cw = parts_scale(fmaxf(s_wtop[lc], s_wtop[32 + lc]), inv);
+        const float cw = parts_scale(fmaxf(s_wtop[lc], s_wtop[COLS + lc]), inv);
         const v4f z0 = *(const v4f *)(sW + lc * PT + 8 * gq), z1 = *(const v4f *)(sW + lc * PT + 8 * gq + 4);
         union { uint2 u[2]; v8h h; } wh, wl;
         parts4(z0[0], z0[2], z1[0], z1[2], inv, wh.u[0], wl.u[0]);
         parts4(z0[1], z0[3], z1[1], z1[3], inv, wh.u[1], wl.u[1]);
 #pragma unroll
-        for (int t = 0; t < OWN; ++t) {
-            const int row = 8 * gq + 2 * (i >> 2), c = 16 * (4 * t + tile0) + 4 * (i & 3);
+        for (int t = 0; t < TILES; ++t) {
+            const int row = 8 * gq + 2 * (i >> 2), c = 16 * (STRIDE * t + tile0) + 4 * (i & 3);
             const _Float16 *k0 = sK + delta_place<DKT>(row, c), *k1 = sK + delta_place<DKT>(row + 1, c);
             const v8h kh_ = both(read_transposed(k0), read_transposed(k1));
             const v8h kl = both(read_transposed(k0 + PART), read_transposed(k1 + PART));
@@ -654,7 +663,7 @@ __global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(Delt
         if (!MOVES && queries) {
             const v4f o = small(sU, xs);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sV[(r0 + e) * PT + lc] = o[e];
+            for (int e = 0; e < 4; ++e) sV[(r0 + e) * PV + lc] = o[e];
         }
         __syncthreads();
     }
@@ -662,7 +671,7 @@ __global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(Delt
     float *to = MOVES ? (unit ? a.moves : a.ends) + there : a.state_out + mine;
     const __amdgpu_buffer_rsrc_t rs = q8_rsrc(to, MOVES || (last && a.state_out) ? bytes : 0);
 #pragma unroll
-    for (int t = 0; t < OWN; ++t)
+    for (int t = 0; t < TILES; ++t)
 #pragma unroll
         for (int e = 0; e < 4; ++e) __builtin_amdgcn_raw_buffer_store_b32(__float_as_int(st[t][e]), rs, state_at(t, e), 0, 0);
 }
@@ -671,7 +680,7 @@ __global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(Delt
 // rule is linear in it: B is what it makes of zeros, F what it makes of the unit vectors without values.  These come from all segments side by side
 // (MOVES), this kernel goes from segment to segment, ends[g] = F[g] ends[g - 1] + ends[g], and the results from all segments side by side again, each from
 // the state that the one before ends with.  About 2.7 times the work: 16384 tokens of 16 heads of
-// 128 x 128 in 655 us (chunks 89, moves 320, this 29, results 240) against 1415 in one go.  A block per sequence, head and 32 columns; products in fp32.
+// 128 x 128 in 567 us (chunks 89, moves 243, this 29, results 245) against 1415 in one go.  A block per sequence, head and 32 columns; products in fp32.
 template <int DKT, bool VEC>         // VEC: dk in whole 16-byte pieces
 __global__ __launch_bounds__(512) void delta_join_kernel(DeltaSeqArgs a)
 {
@@ -753,8 +762,10 @@ static int delta_segment(int L, int S, int hv, int dv)
 template <int DKT> static q8_status launch_sequence(q8_ctx *ctx, const DeltaSeqArgs &a)
 {
     static Q8OncePerDevice once[6];
-    constexpr size_t smem = 2 * 2 * 32 * 32 * DKT * sizeof(_Float16) + delta_state_bytes(DKT) + (4 * 32 * (DELTA_C + 4) + 6 * DELTA_C + 192) * sizeof(float);
+    constexpr size_t keys = 2 * 32 * 32 * DKT * sizeof(_Float16), whole = 2 * keys + delta_state_bytes<false>(DKT) + (4 * 32 * (DELTA_C + 4) + 6 * DELTA_C + 192) * sizeof(float),
+                     move = keys + delta_state_bytes<true>(DKT) + (3 * 32 * (DELTA_C + 4) + 32 * 68 + 6 * DELTA_C + 256) * sizeof(float);
     auto carry = [&](void (*kernel)(DeltaSeqArgs), int form, int rows, int slices) {
+        const size_t smem = form == 2 || form == 3 ? move : whole;
         const q8_status st = q8i_lds(ctx, once[form], (const void *)kernel, smem, "delta sequence");
         if (st) return st;
         hipLaunchKernelGGL(kernel, dim3((unsigned)((size_t)rows * a.in.hv), slices), dim3(512), smem, ctx->stream, a);
@@ -767,8 +778,8 @@ template <int DKT> static q8_status launch_sequence(q8_ctx *ctx, const DeltaSeqA
         if ((st = q8i_launch_check(ctx, "delta sequence"))) return st;
     }
     if (!a.seg) return a.vec ? carry(delta_carry_kernel<DKT, true, false, false>, 0, a.S, slices) : carry(delta_carry_kernel<DKT, false, false, false>, 1, a.S, slices);
-    const int more = (a.in.dk + 31) / 32;
-    st = a.vec ? carry(delta_carry_kernel<DKT, true, true, true>, 2, a.segs, slices + more) : carry(delta_carry_kernel<DKT, false, true, true>, 3, a.segs, slices + more);
+    const int moves = (a.in.dv + 63) / 64 + (a.in.dk + 63) / 64;
+    st = a.vec ? carry(delta_carry_kernel<DKT, true, true, true>, 2, a.segs, moves) : carry(delta_carry_kernel<DKT, false, true, true>, 3, a.segs, moves);
     if (st) return st;
     void (*const join)(DeltaSeqArgs) = a.in.dk % 4 == 0 ? delta_join_kernel<DKT, true> : delta_join_kernel<DKT, false>;
     hipLaunchKernelGGL(join, dim3((unsigned)((size_t)a.S * a.in.hv), slices), dim3(512), 0, ctx->stream, a);

@@ -748,15 +748,23 @@ __global__ __launch_bounds__(512) void delta_join_kernel(DeltaSeqArgs a)
     }
 }
 
-// Chunks of a segment, 0 where sequences are carried whole (us; chunks one after the other cost 2.6 each, blocks side by side 3.75 for 512 at a time):
-// few blocks, long sequences, and segments that give each compute unit two blocks.
-#define DELTA_FEW 96
-static int delta_segment(int L, int S, int hv, int dv)
+// Chunks of a segment, 0 where sequences are carried whole, by what each costs in the time of a chunk of a block alone (2.0, 2.6 and 3.3 us for dk up to 64, 128 and
+// 256), for sequences of the same length: moves and results take `each` a chunk, blocks side by side 1.45 (dk above 128: one block to a compute unit, 1.15), the
+// states from segment to segment `join`, launches 6.  Segments give all compute units work and are no shorter than makes the join as long as they are.
+// us, in segments against whole, dk = dv: 16 heads of 128, 16384 tokens 560 against 1338, 1536 tokens 100 and 126, 768 tokens 74 and 69; 32 of 128, 16384
+// 1065 and 1422; 1 of 128, 16384 220 (of 4 chunks each 600) and 1178; 64 of 64, 4096 233 and 290; 4 of 256, 16384 695 and 1701, 1536 182 and 164.
+// Over 64 sizes the chosen form was within 10 % of the best.
+#define DELTA_FEW 176                // (above: two passes of shorter segments cost more than one)
+static int delta_side(int dk) { return dk > 128 ? 256 : 512; }              // blocks that are resident
+static int delta_segment(int L, int S, int hv, int dk, int dv)
 {
     const long long heads = (long long)hv * ((dv + 31) / 32), chunks = L / DELTA_C;
     if (heads * S > DELTA_FEW || chunks < 24ll * S) return 0;
-    const long long parts = 512 / heads, seg = (chunks + parts - 1) / parts;
-    return 2 * std::max(seg, 4ll) * S > chunks ? 0 : (int)std::max(seg, 4ll);
+    const long long parts = delta_side(dk) / heads;
+    const double n = (double)chunks / S, join = dk <= 64 ? 1.2 : dk <= 128 ? 1.7 : 12.0;
+    const long long seg = std::max(std::max((chunks + parts - 1) / parts, 4ll), (long long)sqrt(0.5 * n * join));
+    const double each = dk > 128 ? 1.15 : chunks * heads <= 256 * seg ? 1.05 : 1.45;
+    return 2 * seg * S > chunks || 2 * each * seg + join * (n / seg - 2) + 6 >= n ? 0 : (int)seg;
 }
 
 template <int DKT> static q8_status launch_sequence(q8_ctx *ctx, const DeltaSeqArgs &a)
@@ -796,23 +804,23 @@ static int delta_segments(int L, int S, int seg) { return L / (DELTA_C * seg) + 
 
 size_t q8i_delta_room(int L, int S, int hv, int dk, int dv)
 {
-    const int seg = delta_segment(L, S, hv, dv);
+    const int seg = delta_segment(L, S, hv, dk, dv);
     return (delta_chunk_room(L, S, hv) + (seg ? delta_segment_room(delta_segments(L, S, seg), hv, dk, dv) : 0)) * sizeof(float);
 }
 
-// ... of any call with up to L tokens and S sequences: fewer sequences may go in segments where S do not.  Segments are at most a part of the 512 for
+// ... of any call with up to L tokens and S sequences: fewer sequences may go in segments where S do not.  Segments are at most a part of the resident blocks for
 // each sequence's heads and slices, and of four chunks at least, besides one for each sequence.
 size_t q8i_delta_most_room(int L, int S, int hv, int dk, int dv)
 {
     const int heads = hv * ((dv + 31) / 32);
     size_t room = delta_chunk_room(L, S, hv);
-    if (heads <= DELTA_FEW && L >= 24 * DELTA_C) room += delta_segment_room(std::min(512 / heads, L / (4 * DELTA_C)) + std::min(S, DELTA_FEW / heads), hv, dk, dv);
+    if (heads <= DELTA_FEW && L >= 24 * DELTA_C) room += delta_segment_room(std::min(delta_side(dk) / heads, L / (4 * DELTA_C)) + std::min(S, DELTA_FEW / heads), hv, dk, dv);
     return room * sizeof(float);
 }
 
 q8_status q8i_delta_sequence(q8_ctx *ctx, const q8_delta_inputs *in, int L, const int *off, int S, const float *state, float *state_out, float *out, int ldo, float *room)
 {
-    DeltaSeqArgs a = {*in, off, S, L, L / DELTA_C + S, room, state, state_out, out, ldo, 0, 0, delta_segment(L, S, in->hv, in->dv), 0, nullptr, nullptr};
+    DeltaSeqArgs a = {*in, off, S, L, L / DELTA_C + S, room, state, state_out, out, ldo, 0, 0, delta_segment(L, S, in->hv, in->dk, in->dv), 0, nullptr, nullptr};
     if (a.seg) {
         a.segs = delta_segments(L, S, a.seg);
         a.ends = room + delta_chunk_room(L, S, in->hv);

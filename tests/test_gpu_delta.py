@@ -386,6 +386,22 @@ def test_long_sequences(q, lengths, hk, hv, dk, dv, edges):
     assert (np_(state) == first[1]).all()
 
 
+@pytest.mark.parametrize("hk,hv,dk,dv", [(1, 1, 130, 40), (1, 1, 256, 20)])
+def test_long_sequences_of_wide_heads(q, hk, hv, dk, dv):
+    """Passing states on costs these more: segments from longer sequences on."""
+    rng = np.random.default_rng(dk)
+    L, off = 8192, [0, 8190]
+    ctx = q.Context(workspace_bytes=q.q8_delta_bytes(L, 1, hv, dk, dv))
+    x = _inputs(rng, L, hk, hv, dk, dv)
+    x["g"] *= np.float32(0.01)
+    st = rng.standard_normal((1, hv, dk, dv)).astype(np.float32)
+    out = torch.zeros(L, hv, dv, device=ctx.device)
+    got = q.q8_delta_sequence(ctx, **_dev(ctx, x), sent_off=torch.tensor(off, dtype=torch.int32, device=ctx.device), scale=0.3, state=ctx.f32(st), out=out)
+    want, bound = ref.sequence(**x, off=off, scale=0.3, state=st), ref.sequence_bound(**x, off=off, scale=0.3, state=st)
+    # (a segment's matrix multiplies a state once more, as above)
+    _close(got, want, (bound[0] * (1 + np.sqrt(dk)), bound[1] * (1 + np.sqrt(dk))), dk)
+
+
 @pytest.mark.parametrize("lengths", [(4097,), (2049, 1, 2050, 0, 900)])
 def test_segments_with_the_new_state_over_the_old_one(q, lengths):
     """A last segment of a token ends long before the first one does."""

@@ -220,7 +220,7 @@ __device__ __forceinline__ v4f fetch4(__amdgpu_buffer_rsrc_t rsrc, unsigned at, 
 // A block per chunk and head.  The waves form tiles of 16 x 16 of both products (the upper right ones are zero) from rows that they load as the
 // matrix operation takes them, the last the sums of the decays too; then (I + A)^-1 by substitution in blocks of 8, joined as
 // -T22 A21 T11 twice.  (Powers of A instead of substitution would cancel: 32 keys alike give binomials up to 3e8.)
-// 8 x 1024 tokens of 16 heads of 128 x 128 in 48 us: 134 MB of keys and queries read, 37 left, 3.6 TB/s; by waiting (three quarters of the waves' time) for loads that all blocks
+// 8 x 1024 tokens of 16 heads of 128 x 128 in 48 us: 134 MB of keys and queries read, 37 left, 3.6 TB/s; by waiting (half of the waves' time) for loads that all blocks
 // of a round ask for at once.  From rows staged in LDS, with the substitution in blocks of 16, 73; the products in three waves 51.
 template <int DKT, bool VEC>         // dk in units of 32, rounded up; VEC: rows of queries and keys in whole 16-byte pieces
 __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaSeqArgs a)

@@ -219,7 +219,8 @@ __device__ __forceinline__ v4f fetch4(__amdgpu_buffer_rsrc_t rsrc, unsigned at, 
 
 // A block per chunk and head.  The waves form tiles of 16 x 16 of both products (the upper right ones are zero) from rows that they load as the
 // matrix operation takes them, the last the sums of the decays too; then (I + A)^-1 by substitution in blocks of 8, joined as
-// -T22 A21 T11 twice.  (Powers of A instead of substitution would cancel: 32 keys alike give binomials up to 3e8.)
+// -T22 A21 T11 twice.  (Powers of A instead of substitution would cancel: 32 keys alike give binomials up to 3e8.)  A row takes nothing from later tokens' rows,
+// not even times the zeros above the diagonal: these may be infinite or no numbers.
 // 8 x 1024 tokens of 16 heads of 128 x 128 in 48 us: 134 MB of keys and queries read, 37 left, 3.6 TB/s; by waiting (half of the waves' time) for loads that all blocks
 // of a round ask for at once.  From rows staged in LDS, with the substitution in blocks of 16, 73; the products in three waves 51.
 template <int DKT, bool VEC>         // dk in units of 32, rounded up; VEC: rows of queries and keys in whole 16-byte pieces
@@ -373,7 +374,7 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaSeqArgs a)
         if (tid < 128) {
             v = 0.0f;
 #pragma unroll
-            for (int l = 0; l < 8; ++l) v = fmaf(sT[(b + 8 + r) * PT + b + 8 + l], sX[(b / 2 + l) * PX + c], v);
+            for (int l = 0; l < 8; ++l) v = fmaf(sT[(b + 8 + r) * PT + b + 8 + l], sX[(b / 2 + min(l, r)) * PX + c], v);
             sT[(b + 8 + r) * PT + b + c] = -v;
         }
     }
@@ -387,13 +388,16 @@ __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaSeqArgs a)
         __syncthreads();
         v = 0.0f;
 #pragma unroll
-        for (int l = 0; l < 16; ++l) v = fmaf(sT[(16 + r) * PT + 16 + l], sX[l * PX + c], v);
+        for (int l = 0; l < 16; ++l) v = fmaf(sT[(16 + r) * PT + 16 + l], sX[min(l, r) * PX + c], v);
         sT[(16 + r) * PT + c] = -v;
     }
     __syncthreads();
     {
         const int r = tid >> 3, c = 4 * (tid & 7);
-        *(v4f *)(room + r * DELTA_C + c) = *(const v4f *)(sT + r * PT + c) * *(const v4f *)(s_b + c);
+        v4f t = *(const v4f *)(sT + r * PT + c) * *(const v4f *)(s_b + c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) t[e] = c + e <= r ? t[e] : 0.0f;
+        *(v4f *)(room + r * DELTA_C + c) = t;
     }
 }
 
@@ -661,7 +665,32 @@ __global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(Delt
         }
         leave_state();
         if (!MOVES && queries) {
-            const v4f o = small(sU, xs);
+            v4f o = small(sU, xs);
+            // A number of a column of R that is not finite is in all of the column's updates and results, and one of the updates in all results: in earlier rows
+            // times the zeros above the diagonal.  The column's new state is not finite in truth either; the earlier results are formed again here, without what
+            // comes after them.  (Looked at here alone, behind the chain from state to state: looked at in both products it cost 3 % of 16384 tokens.)
+            if (__builtin_expect(!(fabsf(o[0]) < INFINITY), 0)) {
+                int l = lane;                                               // (addresses formed here: kept from chunk to chunk they would cost registers)
+                asm volatile("" : "+v"(l));
+                const int r = 16 * mt + 4 * (l >> 4), at = (16 * nt + (l & 15)) * PT;
+                const float *y = sR + at;
+                int bad = 0;
+                while (bad < DELTA_C && fabsf(y[bad]) < INFINITY) ++bad;
+                if (bad == DELTA_C)
+                    for (bad = 0; bad < DELTA_C && fabsf(sU[at + bad]) < INFINITY;) ++bad;
+                if (bad > r && bad < DELTA_C) {                             // (of rows r .. r + 3 those from a bad one on are so again)
+                    o = xs;
+#pragma unroll 1
+                    for (int j = 0; j < r + 4; ++j) {
+                        float u = 0.0f;
+#pragma unroll 1
+                        for (int k = 0; k <= j; ++k) u = fmaf(sM[j * PT + k], y[k], u);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (j <= r + e) o[e] = fmaf(sM[(32 + r + e) * PT + j], u, o[e]);
+                    }
+                }
+            }
 #pragma unroll
             for (int e = 0; e < 4; ++e) sV[(r0 + e) * PV + lc] = o[e];
         }

@@ -615,7 +615,8 @@ __global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(Delt
             x1 = __builtin_amdgcn_mfma_f32_16x16x32_f16(xh, sl, x1, 0, 0, 0);
             x2 = __builtin_amdgcn_mfma_f32_16x16x32_f16(xl, sh, x2, 0, 0, 0);
         }
-        const v4f xs = eb * ((x0 + (x1 + x2)) * cs);
+        // (times the power of two of the column before the rows' factors where it is below one, after them where it is above: nothing but the result passes fp32's range)
+        const v4f xs = (x0 + (x1 + x2)) * fminf(cs, 1.0f) * eb * fmaxf(cs, 1.0f);
         // lane (i, gq): column i, tokens r0 + (0 .. 3)
         if (!queries) {
             v4f v;

@@ -12,6 +12,9 @@ typedef _Float16 v2h __attribute__((ext_vector_type(2)));
 
 #define W4_BLOCK 128                 // columns of a block: 64 bytes of codes, one, two or four groups
 #define W4_SPLIT 512                 // bytes of a block of a vector in its two fp16 parts
+// A group's sum without scales is below 2^25 (128 weights of 15, parts below 2^14).  Words of scales above this (s = 2^93; its low bits are the zero point) could
+// take the sums of 512 groups past fp32's range before the vector's power of two brings them back: these go another way.
+#define W4_LARGE 0x6e000000u
 
 // ------------------------------------------------------------------------------ quantization ----
 
@@ -239,6 +242,7 @@ __global__ __launch_bounds__(1024) void w4_stream_kernel(W4GemmArgs a)
     v4f *s_sum = (v4f *)(s_scale + 16 * a.nb);
     const unsigned magic = w4_magic();
     v4f total = {0.0f, 0.0f, 0.0f, 0.0f};
+    unsigned most = 0;                                                      // the largest word of scales of this lane's rows
     const uint8_t *px = s_x + (size_t)min(i, n - 1) * a.pitch + 16 * g;
     // rows r0 .. r0 + 15 of all vectors, dropped past the end instead of branches (pitches are at most 2^24)
     auto store = [&](int r0, v4f y, float add) {
@@ -281,6 +285,7 @@ __global__ __launch_bounds__(1024) void w4_stream_kernel(W4GemmArgs a)
                     const unsigned e = (at + s) * PER + t / (4 / PER) < a.ng ? cs[word >> 2][word & 3] : 0u;
                     w4_zeros(e, z1, z2);
                     sw = __uint_as_float(e & 0xffff0000u);
+                    most = max(most, e);
                 }
                 const v8h wv = w4_expand(cw[s][t], z1, z2, magic);
                 const v4f none = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -295,6 +300,37 @@ __global__ __launch_bounds__(1024) void w4_stream_kernel(W4GemmArgs a)
             }
         }
         if (!last) continue;
+        if (__builtin_expect(__any(most > W4_LARGE), 0)) {
+            // scales so large that a sum times one may have passed fp32's range: these rows' columns again, the vectors' powers of two first where they are below one
+            total = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
+            const size_t row = (size_t)min(16 * from + i, a.rows - 1);
+            const uint8_t *pw = a.W + row * a.ldw + 16 * g;
+            const unsigned *ps = a.sw + row * a.lds;
+#pragma unroll 1
+            for (int k = b0; k < b1; ++k) {
+                const v4u c = *(const v4u *)(pw + 64 * k);
+                const v4f sx = *(const v4f *)(s_scale + k * 16 + 4 * g);
+                v4f hi = {0.0f, 0.0f, 0.0f, 0.0f}, lo = hi;
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const int word = k * PER + t / (4 / PER);
+                    const unsigned e = word < a.ng ? ps[word] : 0u;
+                    v2h z1, z2;
+                    w4_zeros(e, z1, z2);
+                    const v8h wv = w4_expand(c[t], z1, z2, magic);
+                    const uint8_t *x = px + k * W4_SPLIT + 64 * t;
+                    hi = __builtin_amdgcn_mfma_f32_16x16x32_f16(*(const v8h *)x, wv, hi, 0, 0, 0);
+                    lo = __builtin_amdgcn_mfma_f32_16x16x32_f16(*(const v8h *)(x + W4_SPLIT / 2), wv, lo, 0, 0, 0);
+                    if (t % (4 / PER) != 4 / PER - 1) continue;
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) {
+                        total[v] = fmaf((hi[v] + lo[v]) * fminf(sx[v], 1.0f) * __uint_as_float(e & 0xffff0000u), fmaxf(sx[v], 1.0f), total[v]);
+                        hi[v] = lo[v] = 0.0f;
+                    }
+                }
+            }
+        }
+        most = 0;
         const v4f sum = total;
         total = (v4f){0.0f, 0.0f, 0.0f, 0.0f};
         if (split > 1) { s_sum[wave * 64 + lane] = sum; break; }
@@ -455,6 +491,7 @@ __global__ __launch_bounds__(64 * WM * WN * KS, TM * TN <= 4 ? 2 : 1) void w4_ge
             for (int e = 0; e < 16; ++e) acc[t][u][e] = 0.0f;
     const int lx = (32 * wn * TN + i) * 256, twist = i & 15;
     v2h z1[TM], z2[TM];
+    unsigned most = 0;                                                      // the largest word of scales of this lane's rows
     const unsigned magic = w4_magic();
     // half a block: operations t = 2 half, 2 half + 1
     auto multiply = [&](auto half_) {
@@ -519,6 +556,7 @@ __global__ __launch_bounds__(64 * WM * WN * KS, TM * TN <= 4 ? 2 : 1) void w4_ge
                 if constexpr (PER == 1) word = sc[t];
                 else word = sc[t][p];
                 cs[t][p] = b * PER + p < a.ng ? word : 0u;
+                most = max(most, cs[t][p]);
             }
         }
         q8_stores_performed();                                              // (what this wave asked for is in LDS: the barrier alone does not wait for it)
@@ -532,11 +570,13 @@ __global__ __launch_bounds__(64 * WM * WN * KS, TM * TN <= 4 ? 2 : 1) void w4_ge
         if (b < a.nb) multiply(std::integral_constant<int, 1>());
     }
     if constexpr (KS > 1) {
-        // the groups' sums, a group's where its stages were: [wave][t][u][e][lane]
-        static_assert(STAGE * 2 >= TM * TN * 16 * THREADS * 4, "a group's sums fit where its stages were");
+        // the groups' sums, a group's where its stages were: [wave][t][u][e][lane], and its largest words: [thread]
+        constexpr int WORDS = TM * TN * 16 * THREADS;
+        static_assert(STAGE * 2 >= (WORDS + THREADS) * 4, "a group's sums fit where its stages were");
         __syncthreads();
         float *mine = (float *)s_x + wave * TM * TN * 1024 + lane;
         if (ks > 0) {
+            ((unsigned *)s_x)[WORDS + tid] = most;
 #pragma unroll
             for (int t = 0; t < TM; ++t)
 #pragma unroll
@@ -549,12 +589,55 @@ __global__ __launch_bounds__(64 * WM * WN * KS, TM * TN <= 4 ? 2 : 1) void w4_ge
 #pragma unroll
         for (int g = 1; g < KS; ++g) {
             const float *o = (const float *)(s_all + g * 2 * STAGE) + wave * TM * TN * 1024 + lane;
+            most = max(most, ((const unsigned *)(s_all + g * 2 * STAGE))[WORDS + tid]);
 #pragma unroll
             for (int t = 0; t < TM; ++t)
 #pragma unroll
                 for (int u = 0; u < TN; ++u)
 #pragma unroll
                     for (int e = 0; e < 16; ++e) acc[t][u][e] += o[((t * TN + u) * 16 + e) * 64];
+        }
+    }
+    // Scales so large that sums may have passed fp32's range before the vectors' powers of two: this wave's tile again, by the wave for itself and with the parts
+    // from memory, each group's sums times both, the power of two first where it is below one.  (A tile of vectors at a time: no more registers than the loop above.)
+    const bool again = __any(most > W4_LARGE);
+    if (__builtin_expect(again, 0)) {
+#pragma unroll
+        for (int u = 0; u < TN; ++u) {
+            const uint8_t *pv = a.parts + (size_t)min(c0 + 32 * (wn * TN + u) + i, a.n - 1) * a.nb * W4_SPLIT + 16 * h;
+#pragma unroll
+            for (int m = 0; m < TM; ++m) acc[m][u] = (v16f){};
+#pragma unroll 1
+            for (int b = 0; b < a.nb; ++b, pv += W4_SPLIT) {
+                codes(b);
+#pragma unroll
+                for (int m = 0; m < TM; ++m)
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        unsigned word;                                      // (past the last group: anything)
+                        if constexpr (PER == 1) word = sc[m];
+                        else word = sc[m][t / EACH];
+                        word = b * PER + t / EACH < a.ng ? word : 0u;
+                        w4_zeros(word, z1[m], z2[m]);
+#pragma unroll
+                        for (int p = 0; p < 2; ++p) {
+                            const v8h wv = w4_expand(w[m][p][t], z1[m], z2[m], magic);
+                            const v16f none = {};
+                            sum[0][0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const v8h *)(pv + 64 * t + 32 * p), wv, t % EACH == 0 && p == 0 ? none : sum[0][0], 0, 0, 0);
+                            sum[0][0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const v8h *)(pv + W4_SPLIT / 2 + 64 * t + 32 * p), wv, sum[0][0], 0, 0, 0);
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+                        if (t % EACH != EACH - 1) continue;
+                        const float sw = __uint_as_float(word & 0xffff0000u);
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const v4f f = *(const v4f *)(a.sx + c0 + 32 * (wn * TN + u) + 8 * q + 4 * h);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[m][u][4 * q + e] = fmaf(sum[0][0][4 * q + e] * fminf(f[e], 1.0f) * sw, fmaxf(f[e], 1.0f), acc[m][u][4 * q + e]);
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+            }
         }
     }
     // lane (i, h): row i of a row tile, vectors 8 q + 4 h + (0 .. 3) of a tile of vectors.
@@ -564,7 +647,10 @@ __global__ __launch_bounds__(64 * WM * WN * KS, TM * TN <= 4 ? 2 : 1) void w4_ge
 #pragma unroll
     for (int u = 0; u < TN; ++u)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) sx[u][q] = *(const v4f *)(a.sx + c0 + 32 * (wn * TN + u) + 8 * q + 4 * h);
+        for (int q = 0; q < 4; ++q) {
+            const v4f f = *(const v4f *)(a.sx + c0 + 32 * (wn * TN + u) + 8 * q + 4 * h), one = {1.0f, 1.0f, 1.0f, 1.0f};
+            sx[u][q] = again ? one : f;
+        }
     float bias[TM];
 #pragma unroll
     for (int t = 0; t < TM; ++t) bias[t] = a.bias ? a.bias[min(row + 32 * t, a.rows - 1)] : -0.0f;       // (y + -0 is y)

@@ -2,6 +2,7 @@
 // dk x dv numbers; one token for n slots, and whole sequences laid end to end.
 #include "q8_internal.h"
 #include "q8_parts.h"
+#include "q8_route.h"
 
 #include <algorithm>
 #include <math.h>
@@ -179,7 +180,7 @@ q8_status q8i_delta_step(q8_ctx *ctx, const q8_delta_inputs *in, int n, const fl
 // T = (I + A)^-1 diag(b):  U = T (V - exp(c) K S),  O = exp(c) Q S + (D_ij q_i k_j, j <= i) U,  S' = exp(c_C) S + (exp(c_C - c_j) k_j)^T U.
 // A first launch forms T and the masked products of queries and keys of all chunks side by side, a second one carries the states
 // from chunk to chunk, a block per sequence, head and 32 columns of the state.
-#define DELTA_C 32
+#define DELTA_C Q8_DELTA_C
 #define DELTA_MATRIX (DELTA_C * DELTA_C)
 // What the first launch leaves of a chunk and head, in floats: T, M, then per token (6 x 32) exp(c) / |k|, exp(c) scale / |q| and exp(c_C - c) / |k|, each
 // times the power of two of its row, the inverses of those powers of the key's and the query's row, and exp(c_C)
@@ -778,25 +779,6 @@ __global__ __launch_bounds__(512) void delta_join_kernel(DeltaSeqArgs a)
     }
 }
 
-// Chunks of a segment, 0 where sequences are carried whole, by what each costs in the time of a chunk of a block alone (2.0, 2.6 and 3.3 us for dk up to 64, 128 and
-// 256), for sequences of the same length: moves and results take `each` a chunk, blocks side by side 1.45 (dk above 128: one block to a compute unit, 1.15), the
-// states from segment to segment `join`, launches 6.  Segments give all compute units work and are no shorter than makes the join as long as they are.
-// us, in segments against whole, dk = dv: 16 heads of 128, 16384 tokens 560 against 1338, 1536 tokens 100 and 126, 768 tokens 74 and 69; 32 of 128, 16384
-// 1065 and 1422; 1 of 128, 16384 220 (of 4 chunks each 600) and 1178; 64 of 64, 4096 233 and 290; 4 of 256, 16384 695 and 1701, 1536 182 and 164.
-// Over 64 sizes the chosen form was within 10 % of the best.
-#define DELTA_FEW 176                // (above: two passes of shorter segments cost more than one)
-static int delta_side(int dk) { return dk > 128 ? 256 : 512; }              // blocks that are resident
-static int delta_segment(int L, int S, int hv, int dk, int dv)
-{
-    const long long heads = (long long)hv * ((dv + 31) / 32), chunks = L / DELTA_C;
-    if (heads * S > DELTA_FEW || chunks < 24ll * S) return 0;
-    const long long parts = delta_side(dk) / heads;
-    const double n = (double)chunks / S, join = dk <= 64 ? 1.2 : dk <= 128 ? 1.7 : 12.0;
-    const long long seg = std::max(std::max((chunks + parts - 1) / parts, 4ll), (long long)sqrt(0.5 * n * join));
-    const double each = dk > 128 ? 1.15 : chunks * heads <= 256 * seg ? 1.05 : 1.45;
-    return 2 * seg * S > chunks || 2 * each * seg + join * (n / seg - 2) + 6 >= n ? 0 : (int)seg;
-}
-
 template <int DKT> static q8_status launch_sequence(q8_ctx *ctx, const DeltaSeqArgs &a)
 {
     static Q8OncePerDevice once[6];
@@ -834,7 +816,7 @@ static int delta_segments(int L, int S, int seg) { return L / (DELTA_C * seg) + 
 
 size_t q8i_delta_room(int L, int S, int hv, int dk, int dv)
 {
-    const int seg = delta_segment(L, S, hv, dk, dv);
+    const int seg = q8_delta_segment(L, S, hv, dk, dv);
     return (delta_chunk_room(L, S, hv) + (seg ? delta_segment_room(delta_segments(L, S, seg), hv, dk, dv) : 0)) * sizeof(float);
 }
 
@@ -844,13 +826,13 @@ size_t q8i_delta_most_room(int L, int S, int hv, int dk, int dv)
 {
     const int heads = hv * ((dv + 31) / 32);
     size_t room = delta_chunk_room(L, S, hv);
-    if (heads <= DELTA_FEW && L >= 24 * DELTA_C) room += delta_segment_room(std::min(delta_side(dk) / heads, L / (4 * DELTA_C)) + std::min(S, DELTA_FEW / heads), hv, dk, dv);
+    if (heads <= Q8_DELTA_FEW && L >= 24 * DELTA_C) room += delta_segment_room(std::min(q8_delta_side(dk) / heads, L / (4 * DELTA_C)) + std::min(S, Q8_DELTA_FEW / heads), hv, dk, dv);
     return room * sizeof(float);
 }
 
 q8_status q8i_delta_sequence(q8_ctx *ctx, const q8_delta_inputs *in, int L, const int *off, int S, const float *state, float *state_out, float *out, int ldo, float *room)
 {
-    DeltaSeqArgs a = {*in, off, S, L, L / DELTA_C + S, room, state, state_out, out, ldo, 0, 0, delta_segment(L, S, in->hv, in->dk, in->dv), 0, nullptr, nullptr};
+    DeltaSeqArgs a = {*in, off, S, L, L / DELTA_C + S, room, state, state_out, out, ldo, 0, 0, q8_delta_segment(L, S, in->hv, in->dk, in->dv), 0, nullptr, nullptr};
     if (a.seg) {
         a.segs = delta_segments(L, S, a.seg);
         a.ends = room + delta_chunk_room(L, S, in->hv);

@@ -1,6 +1,9 @@
-// q8_route.h -- which kernel a panel product (q8i_gemm_jobs) takes: plain integer arithmetic on its sizes, the same in a host
-// build, so that the tests of the kernels can be checked against the rule that the library follows.
+// q8_route.h -- which kernel a panel product (q8i_gemm_jobs) takes, a product of 4-bit weights, and how long the segments of the gated delta rule
+// over sequences are: plain arithmetic on sizes, the same in a host build, so that the tests of the kernels can be checked against the
+// rules that the library follows.
 #pragma once
+
+#include <math.h>
 
 enum q8_panel_kernel {
     Q8_ROUTE_STAGED,           // gemm_block_kernel
@@ -105,4 +108,71 @@ static inline int q8_part_rows(const q8_panel_shape *s)
     for (int t = 0; t < s->njobs; ++t) { tiles += (s->rows[t] + 15) / 16; blocks += (s->rows[t] + 63) / 64; }
     if (blocks * groups > 256) return 0;
     return tiles * groups <= 256 ? 1 : tiles * groups <= 512 ? 2 : 4;
+}
+
+// ---- products of 4-bit weights ----
+
+enum q8_w4_kernel {
+    Q8_W4_STREAM,              // w4_stream_kernel; the others w4_gemm_kernel, rows x vectors of a block, and groups of waves that share the columns
+    Q8_W4_32X32_FOUR,
+    Q8_W4_64X32_FOUR,
+    Q8_W4_64X32_TWO,
+    Q8_W4_128X32,
+    Q8_W4_128X64,
+    Q8_W4_128X96,
+    Q8_W4_256X64
+};
+
+#define Q8_W4_STREAM_BLOCKS 160
+
+// apart: results that do not lie over the vectors, pitches up to 2^24.
+// Few vectors: every block makes the vectors' parts for itself, which saves a launch and costs time with their number.
+// Tiles by what each costs (us, both launches; rows x columns x vectors / group).  Where 64 x 32 tiles are few and rows longer than a block, groups of waves
+// share the columns: 64 x 32 in four groups while they are at most one round (4096 x 2048 x 128 / 128 13.9 against 23.6 in 128 x 32, 1024 x 1024 x 256 / 64 11.2
+// against 15.7, 433 x 238 x 160 / 128 6.8 against 7.3), 32 x 32 for the fewest of long rows (2699 x 1882 x 42 / 64 11.7 against 12.8, 1095 x 1030 x 191 / 32 10.6 against
+// 11.4), two groups up to two rounds of longer rows (20000 x 512 x 32 / 128 7.7 against 8.1 in four and 8.9 in 128 x 32, 30000 x 1000 x 24 / 64 10.8, 11.0 and 13.5;
+// 50000 x 512 x 17 / 64 10.3, 11.6 and 9.5).  Else 256 x 64 where there are many, the vectors fill them and groups are not the finest, whose numbers do not fit
+// into the registers (50000 x 512 x 1024 / 128 124; 128 x 64 131, 128 x 32 146; 17152 x 415 x 578 / 32 50, 33 and 36), 128 x 64 where these are more than a
+// round (50000 x 512 x 40 / 128 12.3 against 13.6 in 128 x 32; 8000 x 1024 x 200 / 64 17.7 against 15.9), 128 x 96 for 65 to 96 vectors of many rows
+// (50000 x 512 x 66 / 64 17.5 against 18.7 in 128 x 32 and 22.8 in 128 x 64, 50000 x 1024 x 77 / 32 29.4, 33.4 and 40.4, 63644 x 256 x 90 / 128 15.4, 16.9 and 17.2; 41000
+// x 620 x 66 / 64 20.4, 18.3 and 21.8), and 128 x 32.  Of 80 drawn sizes the chosen form was within 10 % of the best in 79, within 5 % in 71.
+static inline int q8_w4_route(int rows, int cols, int n, int group, int apart)
+{
+    const int nb = (cols + 127) / 128;
+    const long long few = (rows + 63) / 64 * (long long)((n + 31) / 32), wide = (n + 63) / 64;
+    if (n <= 16 && (long long)n * nb <= Q8_W4_STREAM_BLOCKS && apart) return Q8_W4_STREAM;
+    if (nb >= 6 && few <= 128) return Q8_W4_32X32_FOUR;
+    if (nb >= 2 && few <= 256) return Q8_W4_64X32_FOUR;
+    if (nb >= 3 && few <= 512) return Q8_W4_64X32_TWO;
+    if (n > 64 && n <= 96 && (rows + 127) / 128 >= 320) return Q8_W4_128X96;
+    if (wide * 320 <= 8ll * n) {
+        if (group > 32 && (rows + 255) / 256 * wide >= 1024) return Q8_W4_256X64;
+        if ((rows + 127) / 128 * wide >= 320) return Q8_W4_128X64;
+    }
+    return Q8_W4_128X32;
+}
+
+// ---- the gated delta rule over sequences ----
+
+#define Q8_DELTA_C 32                // tokens of a chunk
+#define Q8_DELTA_FEW 176             // blocks (heads x slices of 32 columns x sequences); above, two passes of shorter segments cost more than one
+static inline int q8_delta_side(int dk) { return dk > 128 ? 256 : 512; }    // blocks that are resident
+
+// Chunks of a segment, 0 where sequences are carried whole, by what each costs in the time of a chunk of a block alone (2.0, 2.6 and 3.3 us for dk up to 64, 128 and
+// 256), for sequences of the same length: moves and results take `each` a chunk, blocks side by side 1.45 (dk above 128: one block to a compute unit, 1.15), the
+// states from segment to segment `join`, launches 6.  Segments give all compute units work and are no shorter than makes the join as long as they are.
+// us, in segments against whole, dk = dv: 16 heads of 128, 16384 tokens 560 against 1338, 1536 tokens 100 and 126, 768 tokens 74 and 69; 32 of 128, 16384
+// 1065 and 1422; 1 of 128, 16384 220 (of 4 chunks each 600) and 1178; 64 of 64, 4096 233 and 290; 4 of 256, 16384 695 and 1701, 1536 182 and 164.
+// Over 64 sizes, with up to seven lengths each, the chosen one was within 8 % of the best.
+static inline int q8_delta_segment(int L, int S, int hv, int dk, int dv)
+{
+    const long long heads = (long long)hv * ((dv + 31) / 32), chunks = L / Q8_DELTA_C;
+    if (heads * S > Q8_DELTA_FEW || chunks < 24ll * S) return 0;
+    const long long parts = q8_delta_side(dk) / heads;
+    const double n = (double)chunks / S, join = dk <= 64 ? 1.2 : dk <= 128 ? 1.7 : 12.0;
+    long long seg = (chunks + parts - 1) / parts, least = (long long)sqrt(0.5 * n * join);
+    if (least < 4) least = 4;
+    if (seg < least) seg = least;
+    const double each = dk > 128 ? 1.15 : chunks * heads <= 256 * seg ? 1.05 : 1.45;
+    return 2 * seg * S > chunks || 2 * each * seg + join * (n / seg - 2) + 6 >= n ? 0 : (int)seg;
 }

@@ -2,6 +2,7 @@
 // product with fp32 vectors, Y[j][i] = sum_g s[i,g] sum_{k in g} (c[i,k] - z[i,g]) X[j][k] + bias[i].
 #include "q8_internal.h"
 #include "q8_parts.h"
+#include "q8_route.h"
 
 #include <math.h>
 #include <type_traits>
@@ -161,7 +162,7 @@ struct W4GemmArgs {
 
 // ------------------------------------------------------------------------- few vectors ----
 
-#define W4_STREAM_BLOCKS 160         // blocks of all vectors together, at most: their parts, pitches, scales (a vector has at least a block) and the waves' sums fit
+#define W4_STREAM_BLOCKS Q8_W4_STREAM_BLOCKS      // of all vectors together, at most: their parts, pitches, scales (a vector has at least a block) and the waves' sums fit
 #define W4_STREAM_LDS (W4_STREAM_BLOCKS * W4_SPLIT + 16 * 16 + 64 * W4_STREAM_BLOCKS + 1024 * 16)
 
 // Up to 16 vectors (at 16-byte boundaries): the codes go from memory to registers once; the vectors lie in LDS in parts, put there by every block for
@@ -689,41 +690,29 @@ template <int PER, int WM, int WN, int TM, int TN, int KS = 1> static q8_status 
     return q8i_launch_check(ctx, "product w4");
 }
 
-// Tiles by what each costs (us, both launches; rows x columns x vectors / group).  Where 64 x 32 tiles are few and rows longer than a block, groups of waves
-// share the columns: 64 x 32 in four groups while they are at most one round (4096 x 2048 x 128 / 128 13.9 against 23.6 in 128 x 32, 1024 x 1024 x 256 / 64 11.2
-// against 15.7, 433 x 238 x 160 / 128 6.8 against 7.3), 32 x 32 for the fewest of long rows (2699 x 1882 x 42 / 64 11.7 against 12.8, 1095 x 1030 x 191 / 32 10.6 against
-// 11.4), two groups up to two rounds of longer rows (20000 x 512 x 32 / 128 7.7 against 8.1 in four and 8.9 in 128 x 32, 30000 x 1000 x 24 / 64 10.8, 11.0 and 13.5;
-// 50000 x 512 x 17 / 64 10.3, 11.6 and 9.5).  Else 256 x 64 where there are many, the vectors fill them and groups are not the finest, whose numbers do not fit
-// into the registers (50000 x 512 x 1024 / 128 124; 128 x 64 131, 128 x 32 146; 17152 x 415 x 578 / 32 50, 33 and 36), 128 x 64 where these are more than a
-// round (50000 x 512 x 40 / 128 12.3 against 13.6 in 128 x 32; 8000 x 1024 x 200 / 64 17.7 against 15.9), 128 x 96 for 65 to 96 vectors of many rows
-// (63644 x 620 x 77 / 32 24.4 against 25.8 in 128 x 32 and 29.3 in 128 x 64), and 128 x 32.  Over 60 drawn sizes the chosen form was within 10 % of the best.
-template <int PER> static q8_status gemm_w4_tiles(q8_ctx *ctx, W4GemmArgs &a)
+// (the rule: q8_route.h)
+template <int PER> static q8_status gemm_w4_tiles(q8_ctx *ctx, W4GemmArgs &a, int route)
 {
-    auto tiles = [&](int r, int v) { return (long long)((a.rows + r - 1) / r) * ((a.n + v - 1) / v); };
-    const long long few = tiles(64, 32);
-    if (a.nb >= 6 && few <= 128) return launch_w4<PER, 1, 1, 1, 1, 4>(ctx, a);
-    if (a.nb >= 2 && few <= 256) return launch_w4<PER, 2, 1, 1, 1, 4>(ctx, a);
-    if (a.nb >= 3 && few <= 512) return launch_w4<PER, 2, 1, 1, 1, 2>(ctx, a);
-    if (a.n > 64 && a.n <= 96 && tiles(128, 96) >= 320) return launch_w4<PER, 4, 1, 1, 3>(ctx, a);
-    if ((a.n + 63) / 64 * 320ll <= 8ll * a.n) {
-        if constexpr (PER < 4) {
-            if (tiles(256, 64) >= 1024) return launch_w4<PER, 4, 1, 2, 2>(ctx, a);
-        }
-        if (tiles(128, 64) >= 320) return launch_w4<PER, 4, 1, 1, 2>(ctx, a);
+    if constexpr (PER < 4) {
+        if (route == Q8_W4_256X64) return launch_w4<PER, 4, 1, 2, 2>(ctx, a);
     }
-    return launch_w4<PER, 4, 1, 1, 1>(ctx, a);
+    switch (route) {
+    case Q8_W4_32X32_FOUR: return launch_w4<PER, 1, 1, 1, 1, 4>(ctx, a);
+    case Q8_W4_64X32_FOUR: return launch_w4<PER, 2, 1, 1, 1, 4>(ctx, a);
+    case Q8_W4_64X32_TWO: return launch_w4<PER, 2, 1, 1, 1, 2>(ctx, a);
+    case Q8_W4_128X96: return launch_w4<PER, 4, 1, 1, 3>(ctx, a);
+    case Q8_W4_128X64: return launch_w4<PER, 4, 1, 1, 2>(ctx, a);
+    default: return launch_w4<PER, 4, 1, 1, 1>(ctx, a);
+    }
 }
-
-// Every block makes the vectors' parts for itself, which saves a launch and costs time with their number.
-static bool gemm_w4_streams(int n, int nb) { return n <= 16 && (long long)n * nb <= W4_STREAM_BLOCKS; }
 
 size_t q8i_gemm_w4_scales(int n) { return ((size_t)n + 255) / 256 * 256; }
 
 size_t q8i_gemm_w4_parts(int n, int cols) { return (size_t)n * ((cols + W4_BLOCK - 1) / W4_BLOCK) * W4_SPLIT; }
 
-template <int PER> static q8_status gemm_w4(q8_ctx *ctx, W4GemmArgs &a, bool streams)
+template <int PER> static q8_status gemm_w4(q8_ctx *ctx, W4GemmArgs &a, int route)
 {
-    if (!streams) return gemm_w4_tiles<PER>(ctx, a);
+    if (route != Q8_W4_STREAM) return gemm_w4_tiles<PER>(ctx, a, route);
     const int tiles = (a.rows + 15) / 16;
     int split = 1;
     while (split < 8 && a.nb > 4 * split && tiles * split < 2048) split *= 2;
@@ -740,11 +729,11 @@ q8_status q8i_gemm_w4(q8_ctx *ctx, const q8_mat_w4 *W, const float *X, int n, in
     if (n == 1) a.ldx = a.cols, a.ldy = a.rows;                             // (pitches that nothing uses, but bounds are formed with)
     // (results over the vectors: these are read first, as a whole)
     const uintptr_t x0 = (uintptr_t)X, x1 = x0 + 4 * ((size_t)(n - 1) * ldx + a.cols), y0 = (uintptr_t)Y, y1 = y0 + 4 * ((size_t)(n - 1) * ldy + a.rows);
-    const bool streams = gemm_w4_streams(n, a.nb) && ldx <= 1 << 24 && a.ldy <= 1 << 24 && !(x0 < y1 && y0 < x1);
-    if (!streams) {
+    const int route = q8_w4_route(W->rows, W->cols, n, W->group, ldx <= 1 << 24 && a.ldy <= 1 << 24 && !(x0 < y1 && y0 < x1));
+    if (route != Q8_W4_STREAM) {
         hipLaunchKernelGGL(w4_parts_kernel, dim3(n), dim3(256), 0, ctx->stream, X, a.cols, ldx, a.nb, parts, sx);
         const q8_status st = q8i_launch_check(ctx, "parts w4");
         if (st) return st;
     }
-    return per == 4 ? gemm_w4<4>(ctx, a, streams) : per == 2 ? gemm_w4<2>(ctx, a, streams) : gemm_w4<1>(ctx, a, streams);
+    return per == 4 ? gemm_w4<4>(ctx, a, route) : per == 2 ? gemm_w4<2>(ctx, a, route) : gemm_w4<1>(ctx, a, route);
 }

@@ -78,7 +78,7 @@ def test_sequence(q, what, value, hk, hv, dk, dv, t):
 @pytest.mark.parametrize("what,value", [("v", INF), ("k", NAN), ("q", NAN), ("beta", NAN), ("g", NAN)])
 @pytest.mark.parametrize("t", [3, 1500, 2047])
 def test_long_sequence(q, what, value, t):
-    """In segments (test_delta_route has the rule): one sequence of 2048 tokens."""
+    """In segments (test_w4_delta_route has the rule): one sequence of 2048 tokens."""
     rng = np.random.default_rng(t)
     hk, hv, dk, dv, off = 2, 2, 32, 40, [0, 2048]
     x = _inputs(rng, 2048, hk, hv, dk, dv)

@@ -16,8 +16,8 @@ def q():
     return q
 
 
-# rows, columns, vectors: up to 16 vectors in one launch (rows in one part and in several), then tiles with the columns in four, four and two groups of waves, and in one
-FORMS = [(70, 400, 1), (70, 400, 5), (300, 1500, 16), (1500, 1100, 40), (700, 300, 150), (9000, 500, 90), (20000, 200, 50), (60000, 130, 66), (1300, 130, 1000)]
+# rows, columns, vectors: up to 16 vectors in one launch (rows in one part and in several), then every form of the tiles (test_w4_delta_route has the rule)
+FORMS = [(70, 400, 1), (70, 400, 5), (300, 1500, 16), (1500, 1100, 40), (700, 300, 150), (9000, 500, 90), (20000, 200, 50), (60000, 130, 66), (1300, 130, 1000), (12000, 300, 250), (16500, 150, 1000)]
 
 
 @pytest.mark.parametrize("rows,cols,n", FORMS)

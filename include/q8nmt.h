@@ -677,7 +677,8 @@ q8_status output_logits_w4(q8_ctx *ctx, const q8_readout_weights *ro, const q8_m
  * multiplied by `scale` either way.  g <= 0 (the logarithm of the decay; -inf or the lowest value: the state is forgotten), b in [0, 2], keys of at
  * most unit length keep states bounded; other values are computed as written.  A number that is not finite is in what its token and later ones of its sequence
  * (its slot) and head read and leave (of a value or a state: in its column), in nothing else.  All numbers fp32 (in a
- * sequence, keys and queries whose largest number is below 2^-100, and columns of the state or of a chunk's updates below that, count as zeros in products).  Row t of every table is
+ * sequence, keys and queries whose largest number is below 2^-100, and columns of the state or of a chunk's updates below that, count as zeros in products);
+ * with normalize, keys and queries are up to 2^50 long; without, products of keys and of queries with keys stay in fp32's range.  Row t of every table is
  * token t (or slot t): q, k [. x ldq, ldk] with hk dk, v [. x ldv] with hv dv, g, beta [. x ldg, ldb] with hv numbers side by side, of any alignment
  * (rows in whole 16 bytes are faster), pitches up to 2^22.  1 <= dk, dv <= 256, hv a multiple of hk. */
 typedef struct {
@@ -688,8 +689,9 @@ typedef struct {
     int normalize;
 } q8_delta_inputs;
 
-/* One token for n slots: out [n x ldo] (hv dv numbers a slot) and state_out [n x hv x dk x dv].  Slot j starts from state[parent[j]], the search's
- * back pointers (parent: n numbers on the device; NULL: from state[j], and slots == n); a parent outside [0, slots), or state == NULL: from zeros.
+/* One token for n slots: out [n x ldo] (hv dv numbers a slot) and state_out [n x hv x dk x dv].  Slot j starts from state[parent[j]], the slot of the step before that
+ * its hypothesis goes on from (parent: n numbers on the device, from the caller's own choice of hypotheses: q8_beam_update keeps its back pointers
+ * to itself and moves rows of s; NULL: from state[j], and slots == n); a parent outside [0, slots), or state == NULL: from zeros.
  * Without parents state_out may be state; else they must not overlap.  out overlaps no input. */
 q8_status q8_delta_step(q8_ctx *ctx, const q8_delta_inputs *in, int n, const float *state, int slots, const int32_t *parent, float *state_out,
                         float *out, int ldo);

@@ -1221,7 +1221,7 @@ def _state(t, name, shape):
 
 def q8_delta_step(ctx, q, k, v, g, beta, state=None, scale=1.0, normalize=True, parent=None, state_out=None, out=None, bind=False):
     """One token of the gated delta rule for n slots: q, k [n, hk, dk], v [n, hv, dv], g, beta [n, hv], state [slots, hv, dk, dv] (None: zeros),
-    parent [n] int32 or None.  Returns dict(out [n, hv, dv], state [n, hv, dk, dv]); without state_out and without parents the
+    parent [n] int32 (the slot that each goes on from) or None.  Returns dict(out [n, hv, dv], state [n, hv, dk, dv]); without state_out and without parents the
     state is updated in place."""
     c = _delta_inputs(ctx, q, k, v, g, beta, scale, normalize)
     n, hv, dv = v.shape

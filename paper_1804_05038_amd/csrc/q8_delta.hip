@@ -69,7 +69,7 @@ struct DeltaStepArgs {
 template <int LPR, int R>
 __global__ __launch_bounds__(256) void delta_step_kernel(DeltaStepArgs a)
 {
-    constexpr int GROUPS = 256 / LPR, WAVE_GROUPS = 64 / LPR > 0 ? 64 / LPR : 1;
+    constexpr int GROUPS = 256 / LPR;
     __shared__ __align__(16) float s_k[GROUPS * R], s_q[GROUPS * R];
     __shared__ v4f s_part[4][2][LPR];
     const q8_delta_inputs &p = a.in;
@@ -222,8 +222,9 @@ __device__ __forceinline__ v4f fetch4(__amdgpu_buffer_rsrc_t rsrc, unsigned at, 
 // matrix operation takes them, the last the sums of the decays too; then (I + A)^-1 by substitution in blocks of 8, joined as
 // -T22 A21 T11 twice.  (Powers of A instead of substitution would cancel: 32 keys alike give binomials up to 3e8.)  A row takes nothing from later tokens' rows,
 // not even times the zeros above the diagonal: these may be infinite or no numbers.
-// 8 x 1024 tokens of 16 heads of 128 x 128 in 48 us: 134 MB of keys and queries read, 37 left, 3.6 TB/s; by waiting (half of the waves' time) for loads that all blocks
-// of a round ask for at once.  From rows staged in LDS, with the substitution in blocks of 16, 73; the products in three waves 51.
+// 8 x 1024 tokens of 16 heads of 128 x 128 in 51 us (median of 20 launches; the least 48): 134 MB of keys and queries read, 37 left, 3.3 TB/s; by waiting (half of the
+// waves' time) for loads that all blocks of a round ask for at once.  Least times: from rows staged in LDS, with the substitution in blocks of 16, 73; the products in
+// three waves 51.
 template <int DKT, bool VEC>         // dk in units of 32, rounded up; VEC: rows of queries and keys in whole 16-byte pieces
 __global__ __launch_bounds__(256) void delta_chunk_kernel(DeltaSeqArgs a)
 {
@@ -435,11 +436,11 @@ template <bool MOVES> constexpr size_t delta_state_bytes(int dkt)
 // that what a column loses goes by its own size.  The two small products, of 32 x 32 with T and M, are fp32 ones.  Four waves multiply the
 // keys and make the updates, four multiply the queries and make the results; all convert, and all keep an eighth of the state.  The next chunk's rows are on
 // their way while one is worked on, each number in one thread's load and from there in LDS: loads of what several lanes need each cost the most here.
-// 2.5 us a chunk of 32 tokens for a block alone, 4.0 for the two of a compute unit (8 x 1024 tokens of 16 heads of 128 x 128 in 127 us): no unit is at its limit (vector
-// instructions 44 %, LDS 52 %, of which a sixth conflicts, matrix cores 27 %), a chunk is a chain of four barriers.  Fp32 matrix operations in four waves 197 us, parts in eight waves 157, 22 loads a wave
+// 2.5 us a chunk of 32 tokens for a block alone, 4.2 for the two of a compute unit (8 x 1024 tokens of 16 heads of 128 x 128 in 133 us, median of 20 launches; the least
+// 129): no unit is at its limit (vector instructions 45 %, LDS 51 %, of which a sixth conflicts, matrix cores 26 %), a chunk is a chain of four barriers.  Least times: fp32 matrix operations in four waves 197 us, parts in eight waves 157, 22 loads a wave
 // turned into 8 140, rows' pieces exchanged in LDS in place of padded 127.  (Registers are bounded to 128, so that two blocks are resident.)
 // SEGMENTS: in place of a sequence a block carries a part of it (below).  MOVES: no queries and no results; 64 columns, so that all eight waves multiply the keys
-// (16384 tokens 243 us; 32 columns in four of the waves 320).
+// (16384 tokens 248 us; 32 columns in four of the waves 320).
 template <int DKT, bool VEC, bool SEGMENTS, bool MOVES>      // VEC: rows of queries, keys, values and results in whole 16-byte pieces
 __global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(DeltaSeqArgs a)
 {
@@ -711,7 +712,7 @@ __global__ __launch_bounds__(512, DKT <= 4 ? 4 : 2) void delta_carry_kernel(Delt
 // rule is linear in it: B is what it makes of zeros, F what it makes of the unit vectors without values.  These come from all segments side by side
 // (MOVES), this kernel goes from segment to segment, ends[g] = F[g] ends[g - 1] + ends[g], and the results from all segments side by side again, each from
 // the state that the one before ends with.  About 2.7 times the work: 16384 tokens of 16 heads of
-// 128 x 128 in 567 us (chunks 89, moves 243, this 29, results 245) against 1415 in one go.  A block per sequence, head and 32 columns; products in fp32.
+// 128 x 128 in 580 us a call among others against 1373 in one go (one after the other under a profiler, medians: chunks 92, moves 248, this 30, results 261).  A block per sequence, head and 32 columns; products in fp32.
 template <int DKT, bool VEC>         // VEC: dk in whole 16-byte pieces
 __global__ __launch_bounds__(512) void delta_join_kernel(DeltaSeqArgs a)
 {

@@ -1,5 +1,5 @@
 // q8_parts.h -- fp32 numbers as the sum of two fp16 numbers, for products on the fp16 matrix cores that are as exact as sums in fp32: times a
-// power of two that puts the largest of them below 2^14, a number is hi + lo within 2^-22 of itself (2^-39 of the largest where that is more).
+// power of two that puts the largest of them below 2^14, a number is hi + lo within 2^-22 of itself (2^-38 of the largest where that is more).
 #pragma once
 
 #include "q8_device.h"

@@ -134,8 +134,8 @@ enum q8_w4_kernel {
 // 50000 x 512 x 17 / 64 10.3, 11.6 and 9.5).  Else 256 x 64 where there are many, the vectors fill them and groups are not the finest, whose numbers do not fit
 // into the registers (50000 x 512 x 1024 / 128 124; 128 x 64 131, 128 x 32 146; 17152 x 415 x 578 / 32 50, 33 and 36), 128 x 64 where these are more than a
 // round (50000 x 512 x 40 / 128 12.3 against 13.6 in 128 x 32; 8000 x 1024 x 200 / 64 17.7 against 15.9), 128 x 96 for 65 to 96 vectors of many rows
-// (50000 x 512 x 66 / 64 17.5 against 18.7 in 128 x 32 and 22.8 in 128 x 64, 50000 x 1024 x 77 / 32 29.4, 33.4 and 40.4, 63644 x 256 x 90 / 128 15.4, 16.9 and 17.2; 41000
-// x 620 x 66 / 64 20.4, 18.3 and 21.8), and 128 x 32.  Of 80 drawn sizes the chosen form was within 10 % of the best in 79, within 5 % in 71.
+// (50000 x 512 x 66 / 64 16.4 against 18.3 in 128 x 32 and 22.1 in 128 x 64, 50000 x 1024 x 77 / 32 29.3, 34.1 and 40.3, 63644 x 256 x 90 / 128 14.4, 16.6 and 16.3; 33658
+// x 512 x 77 / 32 17.4, 16.3 and 18.4), and 128 x 32.  Of 80 drawn sizes the chosen form was within 10 % of the best in 78, within 5 % in 71, the worst at 12 %.
 static inline int q8_w4_route(int rows, int cols, int n, int group, int apart)
 {
     const int nb = (cols + 127) / 128;
@@ -161,9 +161,9 @@ static inline int q8_delta_side(int dk) { return dk > 128 ? 256 : 512; }    // b
 // Chunks of a segment, 0 where sequences are carried whole, by what each costs in the time of a chunk of a block alone (2.0, 2.6 and 3.3 us for dk up to 64, 128 and
 // 256), for sequences of the same length: moves and results take `each` a chunk, blocks side by side 1.45 (dk above 128: one block to a compute unit, 1.15), the
 // states from segment to segment `join`, launches 6.  Segments give all compute units work and are no shorter than makes the join as long as they are.
-// us, in segments against whole, dk = dv: 16 heads of 128, 16384 tokens 560 against 1338, 1536 tokens 100 and 126, 768 tokens 74 and 69; 32 of 128, 16384
-// 1065 and 1422; 1 of 128, 16384 220 (of 4 chunks each 600) and 1178; 64 of 64, 4096 233 and 290; 4 of 256, 16384 695 and 1701, 1536 182 and 164.
-// Over 64 sizes, with up to seven lengths each, the chosen one was within 8 % of the best.
+// us, in segments against whole, dk = dv: 16 heads of 128, 16384 tokens 575 against 1373, 1536 tokens 100 and 130, 768 tokens 72 and 70; 32 of 128, 16384
+// 1094 and 1450; 1 of 128, 16384 222 (of 6 chunks each 434) and 1201; 64 of 64, 4096 237 and 293; 4 of 256, 16384 703 and 1774, 1536 183 and 170.
+// Over 64 sizes, with up to eight lengths each, the chosen one was within 7 % of the best.
 static inline int q8_delta_segment(int L, int S, int hv, int dk, int dv)
 {
     const long long heads = (long long)hv * ((dv + 31) / 32), chunks = L / Q8_DELTA_C;

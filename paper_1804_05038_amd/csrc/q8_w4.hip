@@ -169,9 +169,9 @@ struct W4GemmArgs {
 // itself.  A wave multiplies 16 rows at a time, four blocks of columns a turn; `split` waves share the rows, each with its range of
 // the columns.  Lane (i, g) has row i and of every block the 16-byte piece g, whose word t belongs to columns 32 t + 8 g + (0 .. 7):
 // a matrix operation takes 32 columns in a row, so that groups of 32 have their sums too.
-// 50000 x 512 x 5 in 6.7 us (14.6 MB, 3.1 us at a copy's rate; the smallest call takes 3.6): a chain of the vectors' way, their parts, a barrier, the
+// 50000 x 512 x 5 in 6.9 us (14.6 MB, 3.1 us at a copy's rate; the smallest call takes 3.5): a chain of the vectors' way, their parts, a barrier, the
 // codes' expansion (nine instructions for eight weights) and the stores.  With the codes asked for before the vectors 8.7, as loads come back in order; vectors first
-// 8.1, and-or in one instruction 7.7, the vectors' loads under no condition 7.2, stores under none 6.9 (a branch waits for what is in flight).  2048 x 8192 x 1 in 7.7: 128 blocks of 16 rows, half of the compute units idle.
+// 8.1, and-or in one instruction 7.7, the vectors' loads under no condition 7.2, stores under none 6.9 (a branch waits for what is in flight).  2048 x 8192 x 1 in 7.9: 128 blocks of 16 rows, half of the compute units idle.
 template <int PER, int AHEAD>        // groups of a block; blocks of the vectors that a half wave asks for before anything else
 __global__ __launch_bounds__(1024) void w4_stream_kernel(W4GemmArgs a)
 {
@@ -349,7 +349,7 @@ __global__ __launch_bounds__(1024) void w4_stream_kernel(W4GemmArgs a)
 }
 
 // split: waves for a row's columns, a power of two, at most `waves`.  A part is a multiple of four blocks of columns, so that the last ones
-// may have none: these leave no sums, and none are added.
+// may have none: these leave zeros, which are not added.
 template <int PER> static q8_status launch_stream_w4(q8_ctx *ctx, W4GemmArgs &a, int waves, int split)
 {
     static Q8OncePerDevice once;
@@ -438,8 +438,9 @@ template <> struct W4Words<4> { typedef v4u type; };
 // operation (t, p) of a block to columns 32 t + 16 p + (0 .. 15).  In LDS a vector's 16 pieces (hi, lo) are exchanged by its number mod 16, so that
 // lanes that read together find theirs on different banks.
 // KS > 1: KS such groups of waves take turns at the blocks of columns; their sums meet in LDS, in one order.  PAST: the results go past the caches.
-// 50000 x 512 x 1024 in 102 us, 109 with the parts' launch: 105 GFLOP in two products, 1.03 PFLOP/s where the library's largest fp16 product has 1.09, beside 205 MB
-// of results; 140 while each store stood in a branch of its own and waited for the one before.  63644 x 620 x 77 in 20 (45 MB).
+// 50000 x 512 x 1024 in 104 us (least of 20 launches; the median 111), 112 with the parts' launch in calls among others: 105 GFLOP in two products, 1.0 PFLOP/s where the
+// library's largest fp16 product has 1.09, beside 205 MB of results; 140 while each store stood in a branch of its own and waited for the one before.  63644 x 620 x 77 in
+// 21.7 (45 MB).
 template <int PER, int WM, int WN, int TM, int TN, int KS, bool PAST>
 __global__ __launch_bounds__(64 * WM * WN * KS, TM * TN <= 4 ? 2 : 1) void w4_gemm_kernel(W4GemmArgs a)
 {

@@ -44,6 +44,26 @@ def test_large_columns(q, L, dk, dv):
 
 
 @pytest.mark.parametrize("L", [1, 40, 1200])
+@pytest.mark.parametrize("step", [False, True])
+def test_long_keys_and_queries_of_unit_length(q, L, step):
+    """Lengths from 1 to 2^50 before they become one."""
+    rng = np.random.default_rng(L)
+    dk, dv = 48, 36
+    x = _inputs(rng, L, 1, 2, dk, dv)
+    for f in ("k", "q"):
+        x[f] *= (2.0 ** rng.uniform(0, 50, (L, 1, 1)) / np.linalg.norm(x[f], axis=2, keepdims=True)).astype(np.float32)
+    x["g"] *= np.float32(0.01)
+    ctx = q.Context(workspace_bytes=q.q8_delta_bytes(L, 1, 2, dk, dv))
+    if step:
+        S = rng.standard_normal((L, 2, dk, dv)).astype(np.float32)
+        got, want = q.q8_delta_step(ctx, **_dev(ctx, x), state=ctx.f32(S)), ref.step(**x, state=S)
+    else:
+        got = q.q8_delta_sequence(ctx, **_dev(ctx, x), sent_off=torch.tensor([0, L], dtype=torch.int32, device=ctx.device))
+        want = ref.sequence(**x, off=[0, L])
+    _by_columns((np_(got["out"]), np_(got["state"])), want, dk)
+
+
+@pytest.mark.parametrize("L", [1, 40, 1200])
 @pytest.mark.parametrize("ks,qs,vs", [(1e-12, 1e-3, 1e36), (1.0, 1e34, 1e-12), (1e-15, 1e5, 1e30), (1.0, 1e-30, 1e36)])
 def test_lengths_against_columns(q, L, ks, qs, vs):
     """Keys and queries as they are given, short ones with large columns and long ones with small columns.  Keys of 1e-12 leave next to nothing of a value:

@@ -292,6 +292,14 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t q8_rsrc(const void *base, size
 }
 #define Q8_OOB 0x80000000u           // past the end of every descriptor used here (sizes stay below 2^31)
 
+// Sixteen bytes a lane from memory to LDS at `at` + 16 lane (a wave's address), without passing through registers.
+__device__ __forceinline__ void q8_to_lds(__amdgpu_buffer_rsrc_t rsrc, uint8_t *at, unsigned offset, int step)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)at, 16, offset, step, 0, 0);
+#endif
+}
+
 // Quantizes n (<= NMAX) fp32 vectors X[j * ldx + k], k < K, into LDS bytes
 // xq[j * ld + k] (ld % 16 == 0, bytes [K, ld) zeroed) and their scales into s_scale[j].
 // s_red needs NMAX * (blockDim.x / 64) floats.  Ends with a block barrier.

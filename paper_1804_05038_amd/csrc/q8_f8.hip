@@ -165,14 +165,6 @@ __device__ __forceinline__ void f8_expand(v4i c, float s, v8bf &lo, v8bf &hi)
 // together (eight rows) find theirs on different banks.
 __device__ __forceinline__ int f8_twist(int row) { return row & 7; }
 
-// Sixteen bytes a lane from memory to LDS at `at` + 16 lane (a wave's address), without passing through registers.
-__device__ __forceinline__ void f8_to_lds(__amdgpu_buffer_rsrc_t rsrc, uint8_t *at, unsigned offset, int step)
-{
-#if defined(__HIP_DEVICE_COMPILE__)
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)at, 16, offset, step, 0, 0);
-#endif
-}
-
 // Block of WM x WN waves, each with 32 TM rows x 32 TN vectors; stages of 128 columns go from memory to LDS without passing
 // through registers, one on its way while the one before is multiplied.
 // The codes are multiplied as bf16 values, because the matrix cores' own 8-bit floating point sums lose bits: products of a
@@ -218,19 +210,19 @@ __global__ __launch_bounds__(64 * WM * WN * KS) void f8_gemm_kernel(F8GemmArgs a
         uint8_t *at = s_f8 + stage * STAGE + wave * 1024;
         if (step < full) {
 #pragma unroll
-            for (int u = 0; u < LW; ++u) f8_to_lds(rw, at + u * THREADS * 16, ow[u], step * F8_BLOCK);
+            for (int u = 0; u < LW; ++u) q8_to_lds(rw, at + u * THREADS * 16, ow[u], step * F8_BLOCK);
 #pragma unroll
-            for (int u = 0; u < LX; ++u) f8_to_lds(rx, at + ROWS * F8_BLOCK + u * THREADS * 16, ox[u], step * F8_BLOCK);
+            for (int u = 0; u < LX; ++u) q8_to_lds(rx, at + ROWS * F8_BLOCK + u * THREADS * 16, ox[u], step * F8_BLOCK);
         } else {                                                            // pieces past the columns: the row's first in their place
 #pragma unroll
             for (int u = 0; u < LW; ++u) {
                 const int p = u * THREADS + tid, c = 16 * ((p & 7) ^ f8_twist(p >> 3));
-                f8_to_lds(rw, at + u * THREADS * 16, step * F8_BLOCK + c < kend ? ow[u] + step * F8_BLOCK : ow[u] - c, 0);
+                q8_to_lds(rw, at + u * THREADS * 16, step * F8_BLOCK + c < kend ? ow[u] + step * F8_BLOCK : ow[u] - c, 0);
             }
 #pragma unroll
             for (int u = 0; u < LX; ++u) {
                 const int p = u * THREADS + tid, c = 16 * ((p & 7) ^ f8_twist(p >> 3));
-                f8_to_lds(rx, at + ROWS * F8_BLOCK + u * THREADS * 16, step * F8_BLOCK + c < kend ? ox[u] + step * F8_BLOCK : ox[u] - c, 0);
+                q8_to_lds(rx, at + ROWS * F8_BLOCK + u * THREADS * 16, step * F8_BLOCK + c < kend ? ox[u] + step * F8_BLOCK : ox[u] - c, 0);
             }
         }
     };

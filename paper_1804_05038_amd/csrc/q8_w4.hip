@@ -411,14 +411,6 @@ __global__ __launch_bounds__(256) void w4_parts_kernel(const float *X, int cols,
     }
 }
 
-// Sixteen bytes a lane from memory to LDS at `at` + 16 lane (a wave's address), without passing through registers.
-__device__ __forceinline__ void w4_to_lds(__amdgpu_buffer_rsrc_t rsrc, uint8_t *at, unsigned offset, int step)
-{
-#if defined(__HIP_DEVICE_COMPILE__)
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)at, 16, offset, step, 0, 0);
-#endif
-}
-
 // The tile of a block.  Consecutive blocks run on different XCDs, each with an L2 cache of its own: each XCD gets a range of the tiles in a row, those
 // of the same rows one after the other, so that it reads its rows' codes from memory once.
 __device__ __forceinline__ unsigned w4_tile_of()
@@ -463,7 +455,7 @@ __global__ __launch_bounds__(64 * WM * WN * KS, TM * TN <= 4 ? 2 : 1) void w4_ge
     auto request = [&](int stage) {
         uint8_t *at = s_x + (stage & 1) * STAGE + wave * 1024;
 #pragma unroll
-        for (int u = 0; u < LX; ++u) w4_to_lds(rx, at + u * THREADS * 16, ox[u], (stage >> 1) * W4_SPLIT + (stage & 1) * 128);
+        for (int u = 0; u < LX; ++u) q8_to_lds(rx, at + u * THREADS * 16, ox[u], (stage >> 1) * W4_SPLIT + (stage & 1) * 128);
     };
     const uint8_t *pw[TM];
     const unsigned *ps[TM];

@@ -675,8 +675,8 @@ q8_status output_logits_w4(q8_ctx *ctx, const q8_readout_weights *ro, const q8_m
  *   S = a S;  u = b (v - S^T k);  S = S + k u^T;  o = S^T q.
  * Query head h / (hv / hk) serves value head h.  normalize != 0: k / sqrt(|k|^2 + 1e-6) and q / sqrt(|q|^2 + 1e-6) in the places of k and q; q is
  * multiplied by `scale` either way.  g <= 0 (the logarithm of the decay; -inf or the lowest value: the state is forgotten), b in [0, 2], keys of at
- * most unit length keep states bounded; other values are computed as written.  A number that is not finite is in what its token and later ones of its sequence
- * (its slot) and head read and leave (of a value or a state: in its column), in nothing else.  All numbers fp32 (in a
+ * most unit length keep states bounded; other values are computed as written.  A number that is not finite reaches, of its sequence (its slot) and the
+ * heads that it serves, what its token and later ones read and leave (of a value or a state: its column alone), and nothing else.  All numbers fp32 (in a
  * sequence, keys and queries whose largest number is below 2^-100, and columns of the state or of a chunk's updates below that, count as zeros in products);
  * with normalize, keys and queries are up to 2^50 long; without, products of keys and of queries with keys stay in fp32's range.  Row t of every table is
  * token t (or slot t): q, k [. x ldq, ldk] with hk dk, v [. x ldv] with hv dv, g, beta [. x ldg, ldb] with hv numbers side by side, of any alignment
